@@ -49,7 +49,14 @@ typedef enum {
                                 than MMSKV_NOALLOC_SCRATCH_BYTES of scratch */
 } mmskv_status;
 
-typedef enum { MMSKV_F32 = 0, MMSKV_BF16 = 1 } mmskv_dtype;
+/* The 8-bit types are those of a paged cache's rows (mmskv_pages); every other
+ * tensor is fp32 or bf16. */
+typedef enum {
+    MMSKV_F32 = 0,
+    MMSKV_BF16 = 1,
+    MMSKV_E4M3 = 2, /* 8-bit float, 4 exponent and 3 mantissa bits, largest 448 (OCP) */
+    MMSKV_I8 = 3    /* two's complement, -127..127 */
+} mmskv_dtype;
 
 typedef enum {
     MMSKV_VOTE = 0, /* the paper's rule: tau-set votes + lambda * anchor */
@@ -378,6 +385,93 @@ typedef enum {
  * 0 <= window <= T, sinks >= 0, pool odd >= 1, T <= 2^24. */
 int mmshiftkv_shape_scores(const mmskv_shape *shape, int32_t kind, int32_t window, int32_t pool, int32_t sinks,
                            const float *mass, float *score, void *stream);
+
+/* ---- Paged cache: what a decoder runs on after the selection (Appendix B:
+ * retained tokens inserted through the standard cache update).  Rows of K and
+ * V, in bf16 or quantised as they are written, in pages that a table assigns
+ * to the sequences; each KV head has its own number of rows, as the budgets of
+ * the selection are per head.
+ *
+ * Row t of (b, c) is row t % page of page p = table[b * max_pages + t / page]:
+ * element ((p * Hkv + c) * page + t % page) * d + j of k (and v), and, in the
+ * 8-bit types, scale (p * Hkv + c) * page + t % page.  A row stands for its
+ * values times its scale.  Sequences may share pages that are only read; a row
+ * that two entries of one write name is written by both, in no order.  Entries
+ * outside [0, n_pages) name no page: their rows are not written, and are zero
+ * when they are read or attended to.
+ *   k, v              [n_pages, Hkv, page, d] dtype, 16-byte aligned
+ *   k_scale, v_scale  [n_pages, Hkv, page] fp32; not read for MMSKV_BF16
+ *   table             [B, max_pages] int32, contiguous; max_pages * page <= 2^30
+ *   page              rows of a page: a power of two, 16..1024
+ *   dtype             MMSKV_BF16, MMSKV_E4M3 or MMSKV_I8
+ * (others -> MMSKV_EUNSUPPORTED).  Rows that nothing has written may hold any
+ * bits, NaN included: no call reads behind the lengths that it is given. */
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    const int32_t *table;
+    int32_t n_pages, page, max_pages, dtype;
+} mmskv_pages;
+
+/* Writes rows into a paged cache, quantised there: row j < min(counts[b,c], n)
+ * of (b, c) becomes its cached row start[b,c] + j.  The source of row j is
+ * token idx[b,c,j] (idx as returned by mmshiftkv_select_topk: the kept tokens;
+ * entries outside [0, T) give zero rows), or token j without idx (then
+ * n <= T: a chunk of new tokens, or a whole prompt).  Positions below 0 or not
+ * in the table's max_pages * page rows are not written.  Nothing else of the
+ * pages changes.  With a = max |x_j| of the source row, in fp32:
+ *   MMSKV_BF16  y = bf16(x)
+ *   MMSKV_E4M3  scale 2^e, the smallest power of two >= 2^-126 with
+ *               a <= 448 * 2^e; y = e4m3(x / 2^e): a power of two costs a
+ *               float type no precision, and the division is exact
+ *   MMSKV_I8    a' = max(a, 2^-100), scale a' / 127, y = rint(x * (127 / a'))
+ * every rounding to nearest even.
+ * Reads shape->B, Hkv, T and d (64 or 128); Hq and W are ignored.
+ *   k, v    [B, Hkv, T, d] dtype (fp32 or bf16), strides k_strides / v_strides
+ *   idx     [B, Hkv, n] int32 or NULL;  counts, start  [B, Hkv] int32 or NULL
+ *           (NULL: n rows, from row 0) */
+int mmshiftkv_cache_write(const mmskv_shape *shape, const mmskv_pages *pages, const void *k, const void *v,
+                          int32_t dtype, const mmskv_strides *k_strides, const mmskv_strides *v_strides,
+                          const int32_t *idx, const int32_t *counts, const int32_t *start, int32_t n,
+                          void *stream);
+
+/* Reads a paged cache back: row t < lens[b,c] of (b, c), times its scale in
+ * fp32, rounded once to dtype; rows t >= lens[b,c] are zero-filled.  The
+ * result has the layout that mmshiftkv_score and mmshiftkv_gather_kv take.
+ * Reads shape->B, Hkv, T (rows of the result) and d (64 or 128).
+ *   lens          [B, Hkv] int32, taken as if clamped to [0, max_pages * page]
+ *   k_out, v_out  [B, Hkv, T, d] dtype (fp32 or bf16), strides
+ *                 k_out_strides / v_out_strides, rows not overlapping */
+int mmshiftkv_cache_read(const mmskv_shape *shape, const mmskv_pages *pages, const int32_t *lens, int32_t dtype,
+                         void *k_out, const mmskv_strides *k_out_strides, void *v_out,
+                         const mmskv_strides *v_out_strides, void *stream);
+
+/* Attention of a chunk of n new tokens per sequence over a paged cache that
+ * holds their keys and values already (n = 1: a decoding step).  Of sequence b
+ * the first nq = min(q_counts[b], n) queries are there (q_counts NULL: n);
+ * with len = lens[b,c] (clamped to [0, min(T, max_pages * page)]), query i of
+ * head h (KV head c = h / Gh) sees the cached rows
+ *   t <= len - nq + i   (causal = 1: the chunk's rows are the last nq)
+ *   t < len             (causal = 0)
+ *   out[b,h,i,:] = sum_t p_t v_t,  p = softmax over the rows it sees of
+ *                  q . k_t / sqrt(d)
+ * with k, v the cached values times their scales.  bf16 products (exact for
+ * the 8-bit values; the scales are applied in fp32 to the logits and to p),
+ * fp32 accumulation and softmax, p rounded to bf16 for its product with v,
+ * the result rounded once.  A query that sees no row gives zeros, and so do
+ * the rows i >= nq of out.
+ * Reads shape->B, Hq, Hkv, T (an upper bound of lens, which fixes how the work
+ * is split) and d; W is ignored.
+ *   q    [B, Hq, n, d] bf16, strides q_strides;  q_counts [B] int32 or NULL
+ *   out  [B, Hq, n, d] bf16, strides out_strides, rows not overlapping
+ * Workspace: mmshiftkv_chunk_attention_workspace bytes (256-byte aligned; 0
+ * for an invalid shape); they never fall as B, T or n grows.  It needs no
+ * clearing; calls that may overlap in time need workspaces of their own. */
+size_t mmshiftkv_chunk_attention_workspace(const mmskv_shape *shape, int32_t n);
+int mmshiftkv_chunk_attention(const mmskv_shape *shape, const mmskv_pages *pages, const uint16_t *q,
+                              const mmskv_strides *q_strides, const int32_t *q_counts, const int32_t *lens,
+                              int32_t n, int32_t causal, uint16_t *out, const mmskv_strides *out_strides,
+                              void *workspace, size_t workspace_bytes, void *stream);
 
 /* Human-readable text for an mmskv_status value (static storage). */
 const char *mmshiftkv_status_string(int status);

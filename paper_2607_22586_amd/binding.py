@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libmmshiftkv.so")
 
 MMSKV_OK, MMSKV_EINVAL, MMSKV_EUNSUPPORTED, MMSKV_EWORKSPACE, MMSKV_EHIP, MMSKV_ESCRATCH = 0, -1, -2, -3, -4, -5
 NOALLOC_SCRATCH_BYTES = 32 << 20
-MMSKV_F32, MMSKV_BF16 = 0, 1
+MMSKV_F32, MMSKV_BF16, MMSKV_E4M3, MMSKV_I8 = 0, 1, 2, 3
 MMSKV_VOTE, MMSKV_MASS = 0, 1
 
 EXPORTED = ("mmshiftkv_build_proxies", "mmshiftkv_score_workspace", "mmshiftkv_score",
@@ -29,7 +29,8 @@ EXPORTED = ("mmshiftkv_build_proxies", "mmshiftkv_score_workspace", "mmshiftkv_s
             "mmshiftkv_version", "mmshiftkv_hidden_stats_workspace", "mmshiftkv_hidden_stats",
             "mmshiftkv_hidden_proxies", "mmshiftkv_project_proxies", "mmshiftkv_decode_workspace",
             "mmshiftkv_decode_check", "mmshiftkv_window_rows", "mmshiftkv_shape_scores",
-            "mmshiftkv_score_noalloc")
+            "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
+            "mmshiftkv_chunk_attention_workspace", "mmshiftkv_chunk_attention")
 
 
 class Shape(ctypes.Structure):
@@ -50,6 +51,12 @@ class Params(ctypes.Structure):
                 ("tau", ctypes.c_double), ("lambda_", ctypes.c_double),
                 ("std_ddof", ctypes.c_int32), ("layer", ctypes.c_int32),
                 ("seed", ctypes.c_uint64), ("mode", ctypes.c_int32), ("keep_last", ctypes.c_int32)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class MMShiftKVError(RuntimeError):
@@ -100,6 +107,12 @@ def load_library(path: str | None = None):
     lib.mmshiftkv_decode_check.argtypes = [PS, I32, V, V, I32, PT, V, V, I32, V, V, V, V, V, SZ, V]
     lib.mmshiftkv_window_rows.argtypes = [PS, I32, V, I32, PT, V, V, V]
     lib.mmshiftkv_shape_scores.argtypes = [PS, I32, I32, I32, I32, V, V, V]
+    PG = ctypes.POINTER(Pages)
+    lib.mmshiftkv_cache_write.argtypes = [PS, PG, V, V, I32, PT, PT, V, V, V, I32, V]
+    lib.mmshiftkv_cache_read.argtypes = [PS, PG, V, I32, V, PT, V, PT, V]
+    lib.mmshiftkv_chunk_attention_workspace.argtypes = [PS, I32]
+    lib.mmshiftkv_chunk_attention_workspace.restype = SZ
+    lib.mmshiftkv_chunk_attention.argtypes = [PS, PG, V, PT, V, V, I32, I32, V, PT, V, SZ, V]
     lib.mmshiftkv_status_string.argtypes = [ctypes.c_int]
     lib.mmshiftkv_status_string.restype = ctypes.c_char_p
     lib.mmshiftkv_version.restype = ctypes.c_int
@@ -109,7 +122,8 @@ def load_library(path: str | None = None):
                  "mmshiftkv_select_vote", "mmshiftkv_select_pick", "mmshiftkv_gather_kv",
                  "mmshiftkv_hidden_stats", "mmshiftkv_hidden_proxies", "mmshiftkv_project_proxies",
                  "mmshiftkv_decode_check", "mmshiftkv_window_rows", "mmshiftkv_shape_scores",
-            "mmshiftkv_score_noalloc"):
+                 "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
+                 "mmshiftkv_chunk_attention"):
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
         _lib = lib
@@ -589,6 +603,154 @@ def gather_kv(k: torch.Tensor, v: torch.Tensor, sel: Selected, out=None):
             ctypes.byref(_strides4(v)), _p(sel.idx), _p(sel.counts), c_max, _p(out[0]), _p(out[1]),
             _stream(dev))
     _check("mmshiftkv_gather_kv", rc)
+    return out
+
+
+# ----------------------------------------------------------------------------
+# paged cache: rows written (and quantised), read back and attended to
+# ----------------------------------------------------------------------------
+_CACHE_DTYPES = {torch.bfloat16: MMSKV_BF16, torch.float8_e4m3fn: MMSKV_E4M3, torch.int8: MMSKV_I8}
+
+
+@dataclass
+class PagedCache:
+    """Pages of K and V rows (mmskv_pages): k and v [n_pages, Hkv, page, d] as bfloat16,
+    float8_e4m3fn or int8, the 8-bit ones with fp32 scales [n_pages, Hkv, page] (else None);
+    table [B, max_pages] int32, the pages of each sequence in order."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor | None
+    v_scale: torch.Tensor | None
+    table: torch.Tensor
+
+    @classmethod
+    def empty(cls, B: int, Hkv: int, T: int, d: int, dtype: torch.dtype = torch.bfloat16, page: int = 64,
+              device="cuda:0") -> "PagedCache":
+        """A cache of its own pages for B sequences of up to T rows (the rows are not cleared)."""
+        per = max(1, -(-int(T) // page))
+        shape = (B * per, Hkv, page, d)
+        k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        ks = vs = None
+        if dtype != torch.bfloat16:
+            ks, vs = (torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2))
+        return cls(k, v, ks, vs, torch.arange(B * per, dtype=torch.int32, device=device).view(B, per))
+
+    def c_pages(self) -> Pages:
+        k, v, table = self.k, self.v, self.table
+        if k.dtype not in _CACHE_DTYPES:
+            raise TypeError("expected bfloat16, float8_e4m3fn or int8 pages, got %s" % k.dtype)
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or not k.is_contiguous() \
+                or not v.is_contiguous():
+            raise ValueError("k and v pages must be contiguous [n_pages, Hkv, page, d] of one dtype")
+        if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
+            raise ValueError("the table must be a contiguous int32 [B, max_pages] tensor")
+        if k.dtype != torch.bfloat16:
+            for s in (self.k_scale, self.v_scale):
+                if s is None or s.dtype != torch.float32 or s.shape != k.shape[:3] or not s.is_contiguous():
+                    raise ValueError("8-bit pages need contiguous fp32 scales [n_pages, Hkv, page]")
+                _same_device(k, s)
+        _same_device(k, v, table)
+        return Pages(_p(k), _p(v), _p(self.k_scale), _p(self.v_scale), _p(table), k.shape[0], k.shape[2],
+                     table.shape[1], _CACHE_DTYPES[k.dtype])
+
+
+def _same_device(t, *others):
+    dev = _dev(t)
+    for o in others:
+        if o is not None and o.device != dev:
+            raise ValueError("tensors on different devices (%s, %s)" % (dev, o.device))
+    return dev
+
+
+def _int32(t, shape, what):
+    """A list of row numbers as the library takes it: contiguous int32 of that shape."""
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (what, shape))
+    return t
+
+
+def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor | None = None,
+                counts: torch.Tensor | None = None, idx: torch.Tensor | None = None):
+    """mmshiftkv_cache_write: rows of k, v [B, Hkv, T, d] (fp32 or bf16) into the cache, from row
+    start[b, c] (None: 0) of each head on: the first counts[b, c] (None: all) tokens, or those of
+    idx [B, Hkv, n] (a Selected's idx and counts: the kept tokens).  All row numbers int32."""
+    dev = _same_device(k, v, cache.k, start, counts, idx)
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v must have the same shape and dtype")
+    ks, vs = _strides4(k), _strides4(v)
+    B, Hkv, T, d = k.shape
+    if cache.k.shape[1] != Hkv or cache.k.shape[3] != d or cache.table.shape[0] != B:
+        raise ValueError("k does not match the cache's heads, row size or sequences")
+    n = T if idx is None else idx.shape[-1]
+    _int32(idx, (B, Hkv, n), "idx")
+    _int32(counts, (B, Hkv), "counts")
+    _int32(start, (B, Hkv), "start")
+    with _on(dev):
+        rc = load_library().mmshiftkv_cache_write(
+            ctypes.byref(_shape(B, 0, Hkv, T, 0, d)), ctypes.byref(cache.c_pages()), _p(k), _p(v), _dtype_code(k),
+            ctypes.byref(ks), ctypes.byref(vs), _p(idx), _p(counts), _p(start), n, _stream(dev))
+    _check("mmshiftkv_cache_write", rc)
+
+
+def cache_read(cache: PagedCache, lens: torch.Tensor, T: int, dtype: torch.dtype = torch.bfloat16, out=None):
+    """mmshiftkv_cache_read: (k, v) [B, Hkv, T, d] of the first lens[b, c] cached rows of each head
+    (zeros behind them), as bfloat16 or float32; `out` may hold preallocated (k, v)."""
+    dev = _same_device(cache.k, lens)
+    B, Hkv, d = cache.table.shape[0], cache.k.shape[1], cache.k.shape[3]
+    _int32(lens, (B, Hkv), "lens")
+    if out is None:
+        out = tuple(torch.empty((B, Hkv, T, d), dtype=dtype, device=dev) for _ in range(2))
+    ko, vo = out
+    _same_device(cache.k, ko, vo)
+    if tuple(ko.shape) != (B, Hkv, T, d) or vo.shape != ko.shape or ko.dtype != dtype or vo.dtype != dtype:
+        raise ValueError("preallocated k/v do not match")
+    with _on(dev):
+        rc = load_library().mmshiftkv_cache_read(
+            ctypes.byref(_shape(B, 0, Hkv, T, 0, d)), ctypes.byref(cache.c_pages()), _p(lens), _dtype_code(ko),
+            _p(ko), ctypes.byref(_strides4(ko)), _p(vo), ctypes.byref(_strides4(vo)), _stream(dev))
+    _check("mmshiftkv_cache_read", rc)
+    return ko, vo
+
+
+def chunk_attention_workspace(B, Hq, Hkv, T, d, n) -> int:
+    return int(load_library().mmshiftkv_chunk_attention_workspace(ctypes.byref(_shape(B, Hq, Hkv, T, 0, d)), int(n)))
+
+
+def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_counts: torch.Tensor | None = None,
+                    T: int | None = None, causal: bool = True, workspace: torch.Tensor | None = None,
+                    out: torch.Tensor | None = None) -> torch.Tensor:
+    """mmshiftkv_chunk_attention: the outputs [B, Hq, n, d] bf16 of the chunk's queries q [B, Hq, n, d]
+    bf16 (n = 1: a decoding step) over the first lens[b, c] cached rows of each head, the chunk's own
+    among them; q_counts[b] (None: n) queries of sequence b are there.  T is an upper bound of lens
+    (None: what the table can hold).  The result is laid out as q is unless `out` is given."""
+    dev = _same_device(q, cache.k, lens, q_counts, workspace, out)
+    if q.dtype != torch.bfloat16:
+        raise TypeError("q is bf16")
+    qs = _strides4(q)
+    B, Hq, n, d = q.shape
+    Hkv = cache.k.shape[1]
+    if cache.k.shape[3] != d or cache.table.shape[0] != B:
+        raise ValueError("q does not match the cache's row size or sequences")
+    _int32(lens, (B, Hkv), "lens")
+    _int32(q_counts, (B,), "q_counts")
+    T = cache.table.shape[1] * cache.k.shape[2] if T is None else int(T)
+    if out is None:
+        out = torch.empty_like(q)
+        if out.stride(3) != 1:
+            out = torch.empty((B, Hq, n, d), dtype=torch.bfloat16, device=dev)
+    elif out.dtype != torch.bfloat16 or out.shape != q.shape:
+        raise ValueError("preallocated out does not match")
+    shape = _shape(B, Hq, Hkv, T, 0, d)
+    lib = load_library()
+    ws = workspace
+    if ws is None:
+        ws = _ws(lib.mmshiftkv_chunk_attention_workspace(ctypes.byref(shape), int(n)), dev)
+    with _on(dev):
+        rc = lib.mmshiftkv_chunk_attention(
+            ctypes.byref(shape), ctypes.byref(cache.c_pages()), _p(q), ctypes.byref(qs), _p(q_counts), _p(lens),
+            n, int(bool(causal)), _p(out), ctypes.byref(_strides4(out)), _p(ws), ws.numel() * ws.element_size(),
+            _stream(dev))
+    _check("mmshiftkv_chunk_attention", rc)
     return out
 
 

@@ -11,8 +11,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmmshiftkv.so")
-SOURCES = ["api.hip", "proxies.hip", "score.hip", "select.hip", "gather.hip", "hidden.hip", "decode.hip", "baselines.hip"]
-HEADERS = ["common.hpp", "kernels.hpp", "normal.hpp"]
+SOURCES = ["api.hip", "proxies.hip", "score.hip", "select.hip", "gather.hip", "hidden.hip", "decode.hip", "baselines.hip",
+           "cache.hip", "chunk.hip"]
+HEADERS = ["common.hpp", "kernels.hpp", "normal.hpp", "pages.hpp"]
 ARCH = "gfx950"
 
 # Packed fp32 VALU instructions are disabled for every device compilation.

@@ -753,4 +753,185 @@ int mmshiftkv_project_proxies(const mmskv_hshape* shape, int32_t P, int32_t Hq, 
     return status_of(launch_project(a, static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+
+// A paged cache of Hkv heads of d values; fills the kernels' form of it.
+int check_pages(const mmskv_pages* p, int d, Pages* out) {
+    if (p == nullptr) return MMSKV_EINVAL;
+    if (p->k == nullptr || p->v == nullptr || p->table == nullptr) return MMSKV_EINVAL;
+    if (p->n_pages < 1 || p->max_pages < 1 || p->page < 1) return MMSKV_EINVAL;
+    if (p->dtype < MMSKV_F32 || p->dtype > MMSKV_I8) return MMSKV_EINVAL;
+    if (p->dtype == MMSKV_F32) return MMSKV_EUNSUPPORTED;
+    if (p->page < 16 || p->page > 1024 || (p->page & (p->page - 1)) != 0) return MMSKV_EUNSUPPORTED;
+    if (static_cast<int64_t>(p->max_pages) * p->page > (1 << 30)) return MMSKV_EUNSUPPORTED;
+    if (d != 64 && d != 128) return MMSKV_EUNSUPPORTED;
+    if (!aligned(p->k, 16) || !aligned(p->v, 16) || !aligned(p->table, 4)) return MMSKV_EINVAL;
+    if (p->dtype != MMSKV_BF16) {
+        if (p->k_scale == nullptr || p->v_scale == nullptr) return MMSKV_EINVAL;
+        if (!aligned(p->k_scale, 4) || !aligned(p->v_scale, 4)) return MMSKV_EINVAL;
+    }
+    out->k = p->k;
+    out->v = p->v;
+    out->k_scale = p->k_scale;
+    out->v_scale = p->v_scale;
+    out->table = p->table;
+    out->n_pages = p->n_pages;
+    out->max_pages = p->max_pages;
+    out->shift = 0;
+    while ((1 << out->shift) < p->page) ++out->shift;
+    out->cap = p->max_pages * p->page;
+    out->dtype = p->dtype;
+    return MMSKV_OK;
+}
+
+// B, Hkv, T and d of the cache calls (d is checked with the pages).
+int check_cache_shape(const mmskv_shape* s) {
+    if (s == nullptr) return MMSKV_EINVAL;
+    if (s->B < 1 || s->B > 65535 || s->Hkv < 1 || s->Hkv > 65535 || s->T < 1 || s->d < 1) return MMSKV_EINVAL;
+    return MMSKV_OK;
+}
+
+// Output rows that are written: a stride of 0 would put rows over each other.
+int check_out_rows(const void* base, const mmskv_strides* st, int eb, int nb, int nh, int nt) {
+    const int rc = check_rows(base, st, eb, true);
+    if (rc) return rc;
+    if ((nb > 1 && st->sb == 0) || (nh > 1 && st->sh == 0) || (nt > 1 && st->st == 0)) return MMSKV_EINVAL;
+    return MMSKV_OK;
+}
+
+int check_chunk(const mmskv_shape* s, int32_t n) {
+    int rc = check_heads(s);
+    if (rc) return rc;
+    if (s->d < 1 || n < 1) return MMSKV_EINVAL;
+    if (s->d != 64 && s->d != 128) return MMSKV_EUNSUPPORTED;
+    if (static_cast<int64_t>(s->Hq / s->Hkv) * n > (1 << 22)) return MMSKV_EUNSUPPORTED;
+    return MMSKV_OK;
+}
+
+size_t chunk_ws(const mmskv_shape* s, int32_t n) {
+    return chunk_workspace_bound(static_cast<int64_t>(s->B) * s->Hkv, s->Hq / s->Hkv * n, s->T, s->d);
+}
+
+}  // namespace
+
+int mmshiftkv_cache_write(const mmskv_shape* shape, const mmskv_pages* pages, const void* k, const void* v,
+                          int32_t dtype, const mmskv_strides* k_strides, const mmskv_strides* v_strides,
+                          const int32_t* idx, const int32_t* counts, const int32_t* start, int32_t n,
+                          void* stream) {
+    int rc = check_cache_shape(shape);
+    if (rc) return rc;
+    CacheWriteArgs a = {};
+    rc = check_pages(pages, shape->d, &a.pages);
+    if (rc) return rc;
+    const int eb = elem_bytes(dtype);
+    if (eb == 0 || k == nullptr || v == nullptr) return MMSKV_EINVAL;
+    if (n < 1 || (idx == nullptr && n > shape->T)) return MMSKV_EINVAL;
+    if (!aligned(idx, 4) || !aligned(counts, 4) || !aligned(start, 4)) return MMSKV_EINVAL;
+    rc = check_rows(k, k_strides, eb, true);
+    if (rc) return rc;
+    rc = check_rows(v, v_strides, eb, true);
+    if (rc) return rc;
+    a.k = k;
+    a.v = v;
+    a.dtype = dtype;
+    a.ksb = k_strides->sb;
+    a.ksh = k_strides->sh;
+    a.kst = k_strides->st;
+    a.vsb = v_strides->sb;
+    a.vsh = v_strides->sh;
+    a.vst = v_strides->st;
+    a.idx = idx;
+    a.counts = counts;
+    a.start = start;
+    a.B = shape->B;
+    a.Hkv = shape->Hkv;
+    a.T = shape->T;
+    a.d = shape->d;
+    a.n = n;
+    return status_of(launch_cache_write(a, static_cast<hipStream_t>(stream)));
+}
+
+int mmshiftkv_cache_read(const mmskv_shape* shape, const mmskv_pages* pages, const int32_t* lens, int32_t dtype,
+                         void* k_out, const mmskv_strides* k_out_strides, void* v_out,
+                         const mmskv_strides* v_out_strides, void* stream) {
+    int rc = check_cache_shape(shape);
+    if (rc) return rc;
+    CacheReadArgs a = {};
+    rc = check_pages(pages, shape->d, &a.pages);
+    if (rc) return rc;
+    const int eb = elem_bytes(dtype);
+    if (eb == 0 || lens == nullptr || !aligned(lens, 4) || k_out == nullptr || v_out == nullptr) return MMSKV_EINVAL;
+    rc = check_out_rows(k_out, k_out_strides, eb, shape->B, shape->Hkv, shape->T);
+    if (rc) return rc;
+    rc = check_out_rows(v_out, v_out_strides, eb, shape->B, shape->Hkv, shape->T);
+    if (rc) return rc;
+    a.lens = lens;
+    a.k = k_out;
+    a.v = v_out;
+    a.dtype = dtype;
+    a.ksb = k_out_strides->sb;
+    a.ksh = k_out_strides->sh;
+    a.kst = k_out_strides->st;
+    a.vsb = v_out_strides->sb;
+    a.vsh = v_out_strides->sh;
+    a.vst = v_out_strides->st;
+    a.B = shape->B;
+    a.Hkv = shape->Hkv;
+    a.T = shape->T;
+    a.d = shape->d;
+    return status_of(launch_cache_read(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t mmshiftkv_chunk_attention_workspace(const mmskv_shape* shape, int32_t n) {
+    if (check_chunk(shape, n) != MMSKV_OK) return 0;
+    return chunk_ws(shape, n);
+}
+
+int mmshiftkv_chunk_attention(const mmskv_shape* shape, const mmskv_pages* pages, const uint16_t* q,
+                              const mmskv_strides* q_strides, const int32_t* q_counts, const int32_t* lens,
+                              int32_t n, int32_t causal, uint16_t* out, const mmskv_strides* out_strides,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_chunk(shape, n);
+    if (rc) return rc;
+    ChunkArgs a = {};
+    rc = check_pages(pages, shape->d, &a.pages);
+    if (rc) return rc;
+    if (q == nullptr || lens == nullptr || out == nullptr || (causal != 0 && causal != 1)) return MMSKV_EINVAL;
+    if (!aligned(lens, 4) || !aligned(q_counts, 4)) return MMSKV_EINVAL;
+    rc = check_rows(q, q_strides, 2, true);
+    if (rc) return rc;
+    rc = check_out_rows(out, out_strides, 2, shape->B, shape->Hq, n);
+    if (rc) return rc;
+    const int64_t heads = static_cast<int64_t>(shape->B) * shape->Hkv;
+    a.q = q;
+    a.out = out;
+    a.qsb = q_strides->sb;
+    a.qsh = q_strides->sh;
+    a.qst = q_strides->st;
+    a.osb = out_strides->sb;
+    a.osh = out_strides->sh;
+    a.ost = out_strides->st;
+    a.q_counts = q_counts;
+    a.lens = lens;
+    a.B = shape->B;
+    a.Hq = shape->Hq;
+    a.Hkv = shape->Hkv;
+    a.d = shape->d;
+    a.Gh = shape->Hq / shape->Hkv;
+    a.n = n;
+    a.causal = causal;
+    a.max_len = shape->T < a.pages.cap ? shape->T : a.pages.cap;
+    a.rows = a.Gh * n;
+    a.scale = static_cast<float>(query_scale(shape->d));
+    a.splits = chunk_splits(heads, a.rows, a.max_len);
+    const size_t need = chunk_ws(shape, n);
+    if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < need) return MMSKV_EWORKSPACE;
+    const size_t part = static_cast<size_t>(a.splits) * heads * a.rows;
+    const size_t ml_off = align_up(part * a.d * sizeof(float));
+    if (a.splits > 1 && ml_off + part * sizeof(float2) > need) return MMSKV_EWORKSPACE;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ml_off);
+    return status_of(launch_chunk_attention(a, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

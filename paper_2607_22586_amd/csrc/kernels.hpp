@@ -162,6 +162,57 @@ struct ShapeArgs {
     int B, Hkv, T, kind, window, pool, sinks;
 };
 
+// A paged cache (mmskv_pages of the public header).
+struct Pages {
+    void* k; void* v;          // [n_pages, Hkv, page, d]
+    float* k_scale; float* v_scale;   // [n_pages, Hkv, page], 8-bit types
+    const int32_t* table;      // [B, max_pages]
+    int n_pages, max_pages;
+    int shift;                 // log2 of the rows of a page
+    int cap;                   // rows that a table row can name: max_pages << shift (at most 2^30)
+    int dtype;                 // 1 bf16, 2 e4m3, 3 int8
+};
+
+struct CacheWriteArgs {
+    Pages pages;
+    const void* k; const void* v;     // [B, Hkv, T, d]
+    int dtype;                 // 0 fp32, 1 bf16
+    int64_t ksb, ksh, kst, vsb, vsh, vst;
+    const int32_t* idx;        // [B, Hkv, n] or null
+    const int32_t* counts;     // [B, Hkv] or null
+    const int32_t* start;      // [B, Hkv] or null
+    int B, Hkv, T, d, n;
+};
+
+struct CacheReadArgs {
+    Pages pages;
+    const int32_t* lens;       // [B, Hkv]
+    void* k; void* v;          // [B, Hkv, T, d]
+    int dtype;                 // 0 fp32, 1 bf16
+    int64_t ksb, ksh, kst, vsb, vsh, vst;
+    int B, Hkv, T, d;
+};
+
+struct ChunkArgs {
+    Pages pages;
+    const uint16_t* q;         // [B, Hq, n, d] bf16
+    uint16_t* out;             // [B, Hq, n, d] bf16
+    int64_t qsb, qsh, qst, osb, osh, ost;
+    const int32_t* q_counts;   // [B] or null
+    const int32_t* lens;       // [B, Hkv]
+    int B, Hq, Hkv, d, Gh, n, causal;
+    int max_len;               // upper bound of lens: min(T, cap)
+    int rows;                  // Gh * n query rows of a KV head, row i * Gh + g: query i of its head g
+    int splits;                // workgroups that share a row tile's keys
+    float scale;               // log2(e) / sqrt(d)
+    float* part_o;             // [splits, B, Hkv, rows, d] sums of 2^(x - m) v (splits > 1)
+    float2* part_ml;           // [splits, B, Hkv, rows] (m, sum of 2^(x - m)), base 2
+};
+int chunk_splits(int64_t heads, int rows, int T);
+// Workspace bytes that suffice for every plan of a problem and never fall as
+// B, T or n grows.
+size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d);
+
 // Upper end of the lane sums (keys_per_sum terms of 2^s each) that the score
 // and decode kernels add relative to zero.  A row's total over T keys is
 // made of at most n = ceil(T / keys_per_sum) such sums, so with every one
@@ -197,5 +248,8 @@ hipError_t launch_project(const ProjectArgs& p, hipStream_t s);
 hipError_t launch_decode_check(const DecodeArgs& a, hipStream_t s);
 hipError_t launch_window_rows(const WindowArgs& a, hipStream_t s);
 hipError_t launch_shape_scores(const ShapeArgs& a, hipStream_t s);
+hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t s);
+hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t s);
+hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t s);
 
 }  // namespace mmskv

@@ -1,0 +1,398 @@
+"""The paged cache on the GPU: rows written (quantised bit for bit as defined),
+read back, and attended to, against plain 64-bit forms (tests/paged.py)."""
+import numpy as np
+import pytest
+import torch
+
+import paged
+from paper_2607_22586_amd import binding as bd
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+BF16, E4M3, I8, F32 = torch.bfloat16, torch.float8_e4m3fn, torch.int8, torch.float32
+KINDS = [BF16, E4M3, I8]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    bd.load_library()
+
+
+def rnd(seed, *shape, dtype=F32):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def i32(x):
+    return torch.as_tensor(x, dtype=torch.int32).to(DEV)
+
+
+def make_cache(B, Hkv, T, d, kind, page, seed=0, spare=2, fill=True):
+    """A cache whose pages lie in an order of their own and hold NaN (int8: -128) wherever nothing is written."""
+    per = max(1, -(-T // page))
+    n = B * per + spare
+    table = torch.randperm(n, generator=torch.Generator().manual_seed(seed))[:B * per].view(B, per)
+    shape = (n, Hkv, page, d)
+    if kind == I8:
+        k, v = (torch.full(shape, -128, dtype=I8, device=DEV) for _ in range(2))
+    elif kind == E4M3:
+        k, v = (torch.full(shape, 127, dtype=torch.uint8, device=DEV).view(E4M3) for _ in range(2))
+    else:
+        k, v = (torch.full(shape, float("nan"), dtype=BF16, device=DEV) for _ in range(2))
+    ks, vs = (None, None) if kind == BF16 else (torch.full(shape[:3], float("nan"), device=DEV) for _ in range(2))
+    return bd.PagedCache(k, v, ks, vs, i32(table))
+
+
+def raw(t):
+    return t.view(torch.uint8) if t.dtype == E4M3 else t.view(torch.int16) if t.dtype == BF16 else t
+
+
+def snapshot(cache):
+    return [None if t is None else raw(t).clone() if t.dtype != F32 else t.view(torch.int32).clone()
+            for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+
+
+def check_written(cache, before, k, v, counts, start, idx=None):
+    """Every written row bit for bit, and every other bit of the pools as before."""
+    want = [None if t is None else t.cpu().clone() for t in before]
+    table, page = cache.table.cpu().numpy(), cache.k.shape[2]
+    B, Hkv, T, d = k.shape
+    kind = cache.k.dtype
+    for b in range(B):
+        for c in range(Hkv):
+            for j in range(int(counts[b][c])):
+                t = int(start[b][c]) + j
+                if t < 0 or t >= table.shape[1] * page or not 0 <= table[b, t // page] < cache.k.shape[0]:
+                    continue
+                src = j if idx is None else int(idx[b, c, j])
+                for which, x in enumerate((k, v)):
+                    row = x[b, c, src].float().cpu().numpy() if 0 <= src < T else np.zeros(d, np.float32)
+                    y, s = paged.quantised(row, kind)
+                    if kind == E4M3:
+                        y = torch.from_numpy(paged.e4m3_codes(y).astype(np.uint8))
+                    elif kind == I8:
+                        y = torch.from_numpy(y.astype(np.int8))
+                    else:
+                        y = torch.from_numpy(y).to(BF16).view(torch.int16)
+                    at = (int(table[b, t // page]), c, t % page)
+                    want[which][at] = y
+                    if s is not None:
+                        want[2 + which][at] = torch.tensor(float(s), dtype=F32).view(torch.int32)
+    for name, got, w in zip(("k", "v", "k_scale", "v_scale"), snapshot(cache), want):
+        if w is None:
+            continue
+        got = got.cpu()
+        if kind == E4M3 and name in "kv":          # a zero may carry either sign
+            got, w = (torch.where(x == 128, torch.zeros_like(x), x) for x in (got, w))
+        if kind == BF16:
+            got, w = (torch.where(x == -32768, torch.zeros_like(x), x) for x in (got, w))
+        assert torch.equal(got, w), name
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("src", [F32, BF16])
+@pytest.mark.parametrize("B,Hkv,T,d,page,start", [
+    (1, 1, 1, 64, 16, 0), (2, 3, 37, 64, 16, 5), (1, 2, 130, 128, 64, 63), (3, 1, 17, 128, 1024, 1000)])
+def test_write_rows(kind, src, B, Hkv, T, d, page, start):
+    k, v = (rnd(s + T, B, Hkv, T, d) for s in (1, 2))
+    # rows of zeros, of values far apart, next to each end of fp32's range; ties of the int8 and e4m3 grids
+    k[0, 0, 0] = 0.0
+    v[-1, -1, -1] *= torch.exp2(torch.arange(d) % 40 - 30.0)
+    if T > 4:
+        k[0, 0, 1] *= 1e-41
+        k[0, 0, 2] *= 1e30
+        v[0, 0, 1] = torch.arange(d) * 0.5 - 127 + d / 4
+        v[0, 0, 2] = (16 + torch.arange(d) * 0.5)
+        k[0, 0, 3, :] = 448.0 * 2.0 ** -3
+        k[0, 0, 4, :] = 449.0
+    k, v = k.to(src), v.to(src)
+    cache = make_cache(B, Hkv, start + T, d, kind, page, seed=T)
+    before = snapshot(cache)
+    counts = [[max(0, T - 3 * b - c) for c in range(Hkv)] for b in range(B)]
+    starts = [[max(0, start - b - 2 * c) for c in range(Hkv)] for b in range(B)]
+    bd.cache_write(cache, k.to(DEV), v.to(DEV), start=i32(starts), counts=i32(counts))
+    check_written(cache, before, k, v, counts, starts)
+    if T == 37:                                    # all rows, from row 0; token-major sources
+        k2, v2 = (x.to(DEV).transpose(1, 2).contiguous().transpose(1, 2) for x in (k, v))
+        before = snapshot(cache)
+        bd.cache_write(cache, k2, v2)
+        check_written(cache, before, k, v, [[T] * Hkv] * B, [[0] * Hkv] * B)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_write_kept_rows_and_positions_outside(kind):
+    """Kept tokens (with entries outside the prompt), positions below 0 and behind the table, and table
+    entries outside the pool: zero rows for the first, nothing written for the others."""
+    B, Hkv, T, d, page, n = 2, 2, 300, 64, 16, 40
+    k, v = (rnd(s, B, Hkv, T, d, dtype=BF16) for s in (3, 4))
+    cache = make_cache(B, Hkv, 64, d, kind, page)
+    cache.table[1, 1] = -1
+    cache.table[1, 2] = cache.k.shape[0]
+    cache.table[0, 3] = 2 ** 31 - 1
+    idx = torch.randint(0, T, (B, Hkv, n), generator=torch.Generator().manual_seed(7)).sort(-1).values
+    idx[0, 0, 3], idx[1, 1, 5] = -1, T
+    counts = [[n, 17], [n + 9, -4]]                # clamped to [0, n]
+    starts = [[0, 50], [-6, 0]]
+    before = snapshot(cache)
+    bd.cache_write(cache, k.to(DEV), v.to(DEV), start=i32(starts), counts=i32(counts), idx=i32(idx))
+    check_written(cache, before, k, v, np.clip(counts, 0, n), starts, idx)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("B,Hkv,T,d,page", [(1, 1, 1, 128, 64), (2, 3, 77, 64, 16), (3, 2, 200, 128, 32)])
+def test_read_back(kind, out, B, Hkv, T, d, page):
+    k, v = (rnd(s, B, Hkv, T, d).to(DEV) for s in (5, 6))
+    cache = make_cache(B, Hkv, T, d, kind, page)
+    lens = [[max(0, T - 20 * b - 7 * c) for c in range(Hkv)] for b in range(B)]
+    lens[-1][-1] = T + 5000 if T > 1 else T        # clamped to what the table holds
+    bd.cache_write(cache, k, v)
+    if T > 64:
+        cache.table[0, 2] = -7                     # its rows are zero
+        lens[0][0] = -3
+    T2 = T + 13                                    # rows behind the lengths are zero
+    ko = torch.full((B, T2, Hkv, d), float("nan"), dtype=out, device=DEV).transpose(1, 2)
+    vo = torch.full((B, Hkv, T2, d), float("nan"), dtype=out, device=DEV)
+    bd.cache_read(cache, i32(lens), T2, out, out=(ko, vo))
+    for b in range(B):
+        for c in range(Hkv):
+            m = min(max(lens[b][c], 0), cache.table.shape[1] * page, T2)
+            # rows behind T were never written: not compared
+            m_known = min(m, T)
+            for got, x in zip((ko, vo), paged.cached_rows(cache, b, c, m_known)):
+                want = torch.from_numpy(x).float().to(out) if kind != BF16 else torch.from_numpy(x).to(out)
+                assert torch.equal(got[b, c, :m_known].cpu(), want)
+                assert (got[b, c, m:] == 0).all()
+    if out == BF16 and kind != I8:                 # powers of two: nothing is rounded on the way back
+        ko2, _ = bd.cache_read(cache, i32([[T] * Hkv] * B), T)
+        x = paged.cached_rows(cache, 0, 0, T)[0]
+        assert np.array_equal(ko2[0, 0].cpu().double().numpy(), x)
+
+
+def check_attention(cache, q, lens, q_counts=None, causal=True, T=None, out=None):
+    print("attend", tuple(q.shape), cache.k.dtype, tuple(cache.k.shape), flush=True)
+    got = bd.chunk_attention(q.to(DEV) if not q.is_cuda else q, cache, i32(lens),
+                             None if q_counts is None else i32(q_counts), T=T, causal=causal, out=out)
+    want, tol = paged.attention(cache, q, torch.as_tensor(lens), q_counts, causal)
+    got_ = got.cpu().double().numpy()
+    assert np.isfinite(got_).all()
+    off = np.abs(got_ - want)
+    assert (off <= tol).all(), (off - tol).max()
+    assert ((tol > 0) | (got_ == 0)).all()         # rows that see nothing, and rows that are not there
+    return got
+
+
+def filled(B, Hkv, T, d, kind, page, seed=0, wide=True):
+    cache = make_cache(B, Hkv, T, d, kind, page, seed)
+    k, v = (rnd(seed + s, B, Hkv, T, d) for s in (11, 12))
+    if wide:                                       # some large channels, rows of several sizes
+        k[..., ::17] *= 4.0
+        v *= torch.exp2((torch.arange(T) % 5 - 2.0))[:, None]
+    bd.cache_write(cache, k.to(DEV), v.to(DEV))
+    return cache
+
+
+# B, Hq, Hkv, T, d, page, n: one key and one query; tiles of keys ending in and on a page; rows of a head
+# below, at and above 16, 32 and 128; odd groups; a page wider than a tile; many splits
+CASES = [(1, 1, 1, 1, 64, 16, 1), (1, 4, 1, 63, 64, 16, 1), (2, 7, 1, 64, 128, 64, 1), (1, 28, 4, 321, 128, 64, 1),
+         (3, 16, 2, 65, 64, 32, 2), (1, 5, 5, 700, 128, 16, 3), (2, 12, 4, 129, 128, 128, 11),
+         (1, 3, 1, 128, 64, 1024, 43), (1, 14, 2, 500, 128, 64, 70), (1, 2, 2, 300, 64, 256, 300),
+         (1, 33, 1, 1500, 128, 32, 1), (2, 20, 1, 900, 64, 64, 7), (1, 7, 1, 5001, 128, 64, 1),
+         (1, 8, 1, 4100, 64, 16, 2)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("B,Hq,Hkv,T,d,page,n", CASES)
+def test_attention(kind, B, Hq, Hkv, T, d, page, n):
+    cache = filled(B, Hkv, T, d, kind, page, seed=T + n)
+    q = 1.5 * rnd(T, B, Hq, n, d)
+    lens = [[max(0, T - 31 * b - 5 * c) for c in range(Hkv)] for b in range(B)]
+    for causal in (True, False):
+        check_attention(cache, q.to(BF16), lens, None, causal)
+    if n > 1:
+        check_attention(cache, q.to(BF16), lens, [max(0, n - 1 - 2 * b) for b in range(B)], True, T=T)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 40])
+def test_attention_empty_rows(kind, n):
+    """Sequences and heads without cached rows, fewer cached rows than queries (the first queries see
+    nothing), counts of 0 and out of range, lengths out of range."""
+    B, Hkv, T, d = 5, 2, 200, 64
+    cache = filled(B, Hkv, T, d, kind, 32)
+    q = rnd(1, B, 6, n, d, dtype=BF16)
+    lens = [[0, 3], [1, 0], [T, T + 100000], [-5, 17], [150, 33]]
+    cache_rows = [[min(x, T) for x in row] for row in lens]
+    for counts in (None, [n, n, 0, n + 7, -2]):
+        for T_ in (T, None):
+            # (what the table holds behind T was never written: lens within T)
+            check_attention(cache, q, cache_rows, counts, True, T=T_)
+        check_attention(cache, q, cache_rows, counts, False, T=T)
+    got = bd.chunk_attention(q.to(DEV), cache, i32(lens), T=T)      # clamped to T
+    assert torch.equal(got, bd.chunk_attention(q.to(DEV), cache, i32(cache_rows), T=T))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 30])
+def test_attention_pages_outside_the_pool(kind, n):
+    cache = filled(2, 2, 400, 128, kind, 16)
+    cache.table[0, 3], cache.table[1, 0], cache.table[1, 24] = -1, cache.k.shape[0], 2 ** 31 - 1
+    check_attention(cache, rnd(2, 2, 6, n, 128, dtype=BF16), [[400, 60], [399, 17]])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 9])
+def test_attention_layouts(kind, n):
+    """Token-major and padded queries and outputs; nothing is written beside the rows of out."""
+    B, Hq, d = 2, 6, 64
+    cache = filled(B, 2, 150, d, kind, 64)
+    q = rnd(3, B, Hq, n, d, dtype=BF16).to(DEV)
+    lens = [[150, 99], [70, 150]]
+    want = check_attention(cache, q, lens)
+    tokens = q.transpose(1, 2).contiguous().transpose(1, 2)
+    got = bd.chunk_attention(tokens, cache, i32(lens))
+    assert torch.equal(got, want) and (n == 1 or got.stride() == tokens.stride())
+    wide = torch.full((B, n + 3, Hq + 1, d + 8), 7.0, dtype=BF16, device=DEV)
+    wide[:, 1:n + 1, :Hq, :d] = tokens.transpose(1, 2)
+    big = torch.full_like(wide, 7.0)
+    view = big[:, 1:n + 1, :Hq, :d].transpose(1, 2)
+    bd.chunk_attention(wide[:, 1:n + 1, :Hq, :d].transpose(1, 2), cache, i32(lens), out=view)
+    assert torch.equal(view, want)
+    view.fill_(7.0)
+    assert (big == 7.0).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_attention_large_logits(kind):
+    """Logits of several hundred, the largest key first or last: the running maximum moves by all of it."""
+    T, d = 333, 128
+    cache = make_cache(2, 1, T, d, kind, 64)
+    k, v = rnd(1, 2, 1, T, d), rnd(2, 2, 1, T, d)
+    k[0, 0, 0], k[1, 0, -1] = 30.0, 30.0
+    k[0, 0, 1:] -= 5.0
+    bd.cache_write(cache, k.to(DEV), v.to(DEV))
+    q = 3.0 + rnd(3, 2, 4, 1, d)
+    check_attention(cache, q.to(BF16), [[T], [T]])
+    check_attention(cache, (-q).to(BF16), [[T], [T]])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_offsets_past_32_bits(kind):
+    """Pages behind 4 GiB of a pool (and, for bf16, 2^31 elements)."""
+    d, page, T = 128, 1024, 1500
+    per_page = page * d * (2 if kind == BF16 else 1)
+    n = (1 << 32) // per_page + 4
+    raw_k, raw_v = (torch.empty((n, 1, page, d), dtype=torch.int16 if kind == BF16 else torch.uint8, device=DEV)
+                    for _ in range(2))
+    ks, vs = (None, None) if kind == BF16 else (torch.empty((n, 1, page), device=DEV) for _ in range(2))
+    cache = bd.PagedCache(raw_k.view(kind), raw_v.view(kind), ks, vs, i32([[n - 1, n - 3]]))
+    k, v = (rnd(s, 1, 1, T, d).to(DEV) for s in (8, 9))
+    bd.cache_write(cache, k, v)
+    ko, vo = bd.cache_read(cache, i32([[T]]), T, F32)
+    small = make_cache(1, 1, T, d, kind, 64)
+    bd.cache_write(small, k, v)
+    k2, v2 = bd.cache_read(small, i32([[T]]), T, F32)
+    assert torch.equal(ko, k2) and torch.equal(vo, v2)
+    q = rnd(4, 1, 5, 3, d, dtype=BF16).to(DEV)
+    assert torch.equal(bd.chunk_attention(q, cache, i32([[T]]), T=T), bd.chunk_attention(q, small, i32([[T]]), T=T))
+
+
+def test_same_bits_every_time_and_on_side_streams():
+    """No order of atomics in the results; two calls at once, each on its stream with a workspace of its own."""
+    cache = filled(2, 2, 3001, 128, E4M3, 64)
+    q = rnd(5, 2, 14, 1, 128, dtype=BF16).to(DEV)
+    lens = i32([[3001, 2000], [17, 2999]])
+    want = bd.chunk_attention(q, cache, lens)
+    streams = [torch.cuda.Stream(DEV) for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for rep in range(10):
+        for s in streams:
+            with torch.cuda.stream(s):
+                ws = torch.empty(bd.chunk_attention_workspace(2, 14, 2, 3008, 128, 1), dtype=torch.uint8, device=DEV)
+                got.append(bd.chunk_attention(q, cache, lens, workspace=ws, T=3008))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+
+
+def test_captured_steps():
+    """A decoding step (write, attend, lengths on) captured once and replayed, against the eager calls."""
+    B, Hq, Hkv, d, T = 2, 8, 2, 64, 400
+
+    def fresh():
+        cache = filled(B, Hkv, T, d, I8, 16, seed=3)
+        return cache, i32([[300, 20], [0, 250]])
+    ks, vs, qs = (rnd(s, 6, B, h, 1, d, dtype=BF16).to(DEV) for s, h in ((1, Hkv), (2, Hkv), (3, Hq)))
+    cache, lens = fresh()
+    want = []
+    for t in range(6):
+        bd.cache_write(cache, ks[t], vs[t], start=lens)
+        lens = lens + 1
+        want.append(bd.chunk_attention(qs[t], cache, lens).clone())
+    cache, lens = fresh()
+    k, v, q = ks[0].clone(), vs[0].clone(), qs[0].clone()
+    out = torch.empty_like(q)
+    ws = torch.empty(bd.chunk_attention_workspace(B, Hq, Hkv, 512, d, 1), dtype=torch.uint8, device=DEV)
+
+    def step():
+        bd.cache_write(cache, k, v, start=lens)
+        lens.add_(1)
+        bd.chunk_attention(q, cache, lens, workspace=ws, out=out)
+    keep = [x.clone() for x in (lens,)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    lens.copy_(keep[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    lens.copy_(keep[0])
+    for t in range(6):
+        for dst, src in ((k, ks), (v, vs), (q, qs)):
+            dst.copy_(src[t])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[t]), t
+        bd.chunk_attention(q, cache, lens)         # eager work between the replays
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_prompt_selection_and_decoding(kind):
+    """The calls together, as a serving program makes them: a prompt's K/V written chunk by chunk with the
+    chunks' attention, read back for the selection, the kept rows written to a small cache, and tokens
+    decoded on it."""
+    B, Hq, Hkv, T, d, page = 2, 4, 2, 700, 64, 64
+    k, v, q = (rnd(s, B, h, T, d, dtype=BF16) for s, h in ((21, Hkv), (22, Hkv), (23, Hq)))
+    prompt = make_cache(B, Hkv, T, d, kind, page)
+    done = 0
+    for n in (256, 300, 144):
+        part = [x[:, :, done:done + n].to(DEV) for x in (k, v, q)]
+        bd.cache_write(prompt, part[0], part[1], start=i32([[done] * Hkv] * B))
+        done += n
+        check_attention(prompt, part[2].cpu(), [[done] * Hkv] * B)
+    kr, vr = bd.cache_read(prompt, i32([[T] * Hkv] * B), T)
+    cfg = bd.SelectionConfig(P=64, G=4, seed=3)
+    budgets = torch.tensor([[90, 41], [64, 7]], dtype=torch.int32)
+    layer = bd.select_layer(q[:, :, -32:].to(DEV), kr, vr, 90, cfg, c_max=90, budgets=budgets)
+    kept = make_cache(B, Hkv, 120, d, kind, 16, seed=5)
+    bd.cache_write(kept, kr, vr, counts=layer.sel.counts, idx=layer.sel.idx)
+    lens = layer.sel.counts.clone()
+    assert torch.equal(lens.cpu(), budgets)
+    # (rows as the gather compacts them, quantised again)
+    ko, vo = bd.cache_read(kept, lens, 90)
+    for b in range(B):
+        for c in range(Hkv):
+            m = int(budgets[b, c])
+            for got, src in ((ko, layer.k_out), (vo, layer.v_out)):
+                y, s = paged.quantised(src[b, c, :m].float().cpu().numpy(), kind)
+                want = torch.from_numpy(y if s is None else y * s[:, None]).float().to(BF16)
+                assert torch.equal(got[b, c, :m].cpu(), want)
+    for t in range(3):
+        kn, vn = (rnd(30 + t + 10 * s, B, Hkv, 1, d, dtype=BF16).to(DEV) for s in range(2))
+        bd.cache_write(kept, kn, vn, start=lens)
+        lens = lens + 1
+        check_attention(kept, rnd(60 + t, B, Hq, 1, d, dtype=BF16), lens.cpu().tolist())

@@ -224,6 +224,372 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
                       pack_bf16(o[t][4 * w + 2] * inv, o[t][4 * w + 3] * inv)};
 }
 
+// ---- few rows -----------------------------------------------------------
+// Up to 64 rows of a (b, c): the keys are read from HBM once and little is
+// computed on them, so what counts is how many bytes are in flight.  Each wave
+// of a workgroup has key tiles of its own (one of every kWaves) and all rows,
+// in NR tiles of 16; it loads its tiles straight to LDS of its own, in two
+// stages of up to 8 KB of K and 8 KB of V, so that no wave waits for another
+// before the end and a CU has 64 KB on their way while it works on as many.
+// The rows stay as the cache holds them; 8-bit values are widened in registers.
+//   S^T = K Q^T  (v_mfma_f32_16x16x32_bf16, lane = query row lane % 16)
+//   O^T += V^T P^T
+// Row m of the s-th of two 16-key tiles of S^T is key 8 (m / 4) + 4 s + m % 4 of
+// their 32: with that order a lane's eight p are those of eight consecutive
+// keys, the ones that its transposing reads of V fetch.
+constexpr int kFewRows = 64;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ floatx4 mfma16(bf16x8 a, bf16x8 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Largest value / sum over the four lanes that hold a query row (lane % 16).
+__device__ __forceinline__ float quarter_max(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quarter_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+template <int D, int TYPE>
+struct FewTile {
+    static constexpr int kRow = D * kCacheBytes<TYPE>;          // bytes of a cached row: 64, 128 or 256
+    static constexpr int kCh = kRow / 16;                       // its 16-byte chunks
+    static constexpr int kKeys = kRow == 256 ? 32 : 64;         // keys of a stage
+    static constexpr int kTile = kKeys * kRow;                  // bytes of its K (and of its V)
+    static constexpr int kPer = 1024 / kRow;                    // rows of one load instruction: 4 to 16, on one page
+    static constexpr int kLoads = kKeys / kPer;                 // load instructions of K (and of V)
+    static constexpr bool kScaled = TYPE != kCacheBf16;
+    static constexpr int kGroups = kKeys / 16;                  // 16-row groups, each on one page
+    static constexpr int kAll = 2 * kLoads + (kScaled ? 2 : 0);
+    static constexpr int kStage = 2 * kTile + (kScaled ? 2 * kKeys * 4 : 0);
+    // byte of 16-byte chunk ch of row r (chunks permuted against bank conflicts)
+    static __device__ __forceinline__ int swz(int r) {
+        return kCh == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : kCh == 8 ? ((r >> 1) ^ (r >> 3)) & 7 : ((r >> 2) ^ (r >> 4)) & 3;
+    }
+    static __device__ __forceinline__ int at(int r, int ch) { return r * kRow + 16 * (ch ^ swz(r)); }
+};
+
+// Workgroup: 4 waves; (b, c) and a split of its keys.
+template <int D, int TYPE, int NR>
+__global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
+    using T = FewTile<D, TYPE>;
+    constexpr int KC = D / 32;             // 32-dim steps of S
+    constexpr int NT = D / 16;             // 16-dim tiles of O
+    constexpr int NS = T::kKeys / 16;      // 16-key tiles of S
+    constexpr int kLd = D + 4;             // floats of a row in the merge
+    constexpr int kMerge = NR * 16 * kLd * 4;
+    constexpr int kWaveLds = 2 * T::kStage > kMerge ? 2 * T::kStage : kMerge;
+    __shared__ __align__(16) char lds[kWaves][kWaveLds];
+    __shared__ __align__(16) char qs[NR * 16 * 2 * D];
+    __shared__ float2 ml[kWaves][NR * 16];
+
+    const int bc = blockIdx.x, b = bc / a.Hkv, c = bc - b * a.Hkv, split = blockIdx.y;
+    const int tid = threadIdx.x, lane = lane_id();
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int quarter = lane >> 4;
+    char* const base = lds[wave];
+
+    const int nq = a.q_counts ? min(max(a.q_counts[b], 0), a.n) : a.n;
+    const int len = min(max(a.lens[bc], 0), a.max_len);
+    const int end = nq > 0 ? len : 0;      // keys that the rows see together
+    const int tiles = (end + T::kKeys - 1) / T::kKeys, per = (tiles + a.splits - 1) / a.splits;
+    const int tile0 = split * per + wave, tile1 = min(split * per + per, tiles);
+
+    // lane's part of a load: row lane / kCh of kPer, chunk lane % kCh of the staged order
+    const int ld_row = lane / T::kCh;
+    // pages of the 16-row groups of a tile (-1: none), by scalar loads, whose
+    // waits are not those of the loads to LDS
+    struct Ids {
+        int id[T::kGroups];
+    };
+    auto pages_of = [&](int tile) {
+        typedef const int __attribute__((address_space(4))) * ctable;
+        const ctable row = (ctable)(a.pages.table) + static_cast<int64_t>(b) * a.pages.max_pages;
+        Ids ids;
+#pragma unroll
+        for (int g = 0; g < T::kGroups; ++g) {
+            const int j = (tile * T::kKeys + 16 * g) >> a.pages.shift;
+            const int id = row[min(j, a.pages.max_pages - 1)];
+            ids.id[g] = j < a.pages.max_pages && static_cast<uint32_t>(id) < static_cast<uint32_t>(a.pages.n_pages) ? id : -1;
+        }
+        return ids;
+    };
+    auto load_stage = [&](int tile, int stage, const Ids& ids) {
+        char* dst = base + stage * T::kStage;
+        const int t0 = tile * T::kKeys;
+#pragma unroll
+        for (int j = 0; j < T::kLoads; ++j) {
+            const int r = j * T::kPer;     // uniform; its kPer rows are on one page
+            const int id = ids.id[r / 16];
+            const int rr = r + ld_row;
+            const int off = ld_row * T::kRow + 16 * ((lane % T::kCh) ^ T::swz(rr));
+            const int64_t e = pool_row(a.pages, a.Hkv, c, id, t0 + r) * T::kRow;
+            const char* ks = id >= 0 ? static_cast<const char*>(a.pages.k) + e : reinterpret_cast<const char*>(kNoRows);
+            const char* vs = id >= 0 ? static_cast<const char*>(a.pages.v) + e : reinterpret_cast<const char*>(kNoRows);
+            load16_to_lds(ks + off, dst + j * 1024);
+            load16_to_lds(vs + off, dst + T::kTile + j * 1024);
+        }
+        if constexpr (T::kScaled) {        // kKeys is 64: a lane has the scales of one row
+            const int g = lane / 16;
+            const int id = g == 0 ? ids.id[0] : g == 1 ? ids.id[T::kGroups > 1 ? 1 : 0] : g == 2 ? ids.id[T::kGroups > 2 ? 2 : 0]
+                                                                                            : ids.id[T::kGroups - 1];
+            const int64_t pr = pool_row(a.pages, a.Hkv, c, id, t0 + lane);
+            const char* none = reinterpret_cast<const char*>(kNoRows);
+            load4_to_lds(id >= 0 ? reinterpret_cast<const char*>(a.pages.k_scale + pr) : none, dst + 2 * T::kTile);
+            load4_to_lds(id >= 0 ? reinterpret_cast<const char*>(a.pages.v_scale + pr) : none, dst + 2 * T::kTile + 256);
+        }
+    };
+
+    // the rows of all waves to LDS, 1 KB per instruction (missing ones as zeros), then two stages
+    constexpr int QC = D / 8;              // 16-byte chunks of a query row
+    const auto q_at = [](int r, int ch) { return r * 2 * D + 16 * (ch ^ ((QC == 16 ? r : r >> 1) & (QC - 1))); };
+#pragma unroll
+    for (int j = 0; j < NR * 16 * QC / kWave; j += kWaves) {
+        if (j + wave >= NR * 16 * QC / kWave) break;
+        const int r = (j + wave) * (kWave / QC) + lane / QC, i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
+        const int ch = (lane % QC) ^ ((QC == 16 ? r : r >> 1) & (QC - 1));
+        const bool there = r < a.rows && i < nq;
+        const char* src = there ? reinterpret_cast<const char*>(a.q + b * a.qsb + h * a.qsh + i * a.qst + 8 * ch)
+                                : reinterpret_cast<const char*>(kNoRows);
+        load16_to_lds(src, qs + (j + wave) * 1024);
+    }
+    Ids ids = pages_of(tile0);
+    if (tile0 < tile1) load_stage(tile0, 0, ids);
+    ids = pages_of(tile0 + kWaves);
+    if (tile0 + kWaves < tile1) load_stage(tile0 + kWaves, 1, ids);
+
+    // the last key that each of this lane's rows sees (below 0: none)
+    int last[NR];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+        const int r = 16 * x + (lane & 15), i = r / a.Gh;
+        last[x] = r < a.rows && i < nq ? (a.causal ? len - nq + i : len - 1) : -1;
+    }
+    // keys that every row sees
+    const int all_see = a.causal ? max(len - nq + 1, 0) : len;
+
+    floatx4 o[NR][NT];
+    float m[NR], l[NR];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+        m[x] = kNone;
+        l[x] = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[x][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    if (tile0 + kWaves < tile1) wait_vm<2 * T::kAll>();
+    else if (tile0 < tile1) wait_vm<T::kAll>();
+    else wait_vm<0>();
+    asm volatile("s_barrier" ::: "memory");
+    bf16x8 qf[NR][KC];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+        uint32_t at[KC];
+        u32x4 w[KC];
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) at[kc] = lds_address(qs) + q_at(16 * x + (lane & 15), 4 * kc + quarter);
+        read128(at, w);
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) qf[x][kc] = __builtin_bit_cast(bf16x8, w[kc]);
+    }
+
+    int stage = 0;
+    for (int tile = tile0; tile < tile1; tile += kWaves, stage ^= 1) {
+        if (tile + kWaves < tile1) wait_vm<T::kAll>();     // all but the next stage
+        else wait_vm<0>();
+        __builtin_amdgcn_sched_barrier(0);
+        ids = pages_of(tile + 2 * kWaves);
+        char* const kt = base + stage * T::kStage;
+        char* const vt = kt + T::kTile;
+        float* const ksc = reinterpret_cast<float*>(vt + T::kTile);
+        float* const vsc = ksc + T::kKeys;
+        const int key0 = tile * T::kKeys;
+        if (key0 + T::kKeys > end) {
+            // rows behind the last key may hold anything: zeros, with zero scales
+            for (int i = lane; i < T::kKeys * T::kCh; i += kWave)
+                if (key0 + i / T::kCh >= end) *reinterpret_cast<u32x4*>(vt + i * 16) = u32x4{0u, 0u, 0u, 0u};
+            if (T::kScaled && key0 + lane >= end) ksc[lane] = 0.f, vsc[lane] = 0.f;
+        }
+        // value e of s[x][u] is key key0 + 32 (u / 2) + 8 quarter + 4 (u % 2) + e
+        floatx4 s[NR][NS];
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+            for (int x = 0; x < NR; ++x) s[x][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+        constexpr int UB = 8 / KC;         // 16-key tiles of eight reads
+#pragma unroll
+        for (int u0 = 0; u0 < NS; u0 += UB) {
+            uint32_t at[8];
+            bf16x8 k[8];
+#pragma unroll
+            for (int z = 0; z < 8; ++z) {
+                const int u = u0 + z / KC, kc = z % KC;
+                const int row = 32 * (u >> 1) + 8 * ((lane & 15) >> 2) + 4 * (u & 1) + (lane & 3);
+                at[z] = lds_address(kt) + (T::kScaled ? T::at(row, 2 * kc + (quarter >> 1)) + 8 * (quarter & 1)
+                                                      : T::at(row, 4 * kc + quarter));
+            }
+            if constexpr (T::kScaled) {
+                u32x2 w[8];
+                read64(at, w);
+#pragma unroll
+                for (int z = 0; z < 8; ++z) {
+                    const u32x2 y0 = widen4<TYPE>(w[z][0]), y1 = widen4<TYPE>(w[z][1]);
+                    k[z] = __builtin_bit_cast(bf16x8, (u32x4{y0[0], y0[1], y1[0], y1[1]}));
+                }
+            } else {
+                u32x4 w[8];
+                read128(at, w);
+#pragma unroll
+                for (int z = 0; z < 8; ++z) k[z] = __builtin_bit_cast(bf16x8, w[z]);
+            }
+#pragma unroll
+            for (int z = 0; z < 8; ++z)
+#pragma unroll
+                for (int x = 0; x < NR; ++x) s[x][u0 + z / KC] = mfma16(k[z], qf[x][z % KC], s[x][u0 + z / KC]);
+        }
+        floatx4 kw[NS], vw[NS];
+        if constexpr (T::kScaled) {
+            static_assert(!T::kScaled || NS == 4, "eight reads of four scales");
+            uint32_t at[8];
+            u32x4 w[8];
+#pragma unroll
+            for (int z = 0; z < 8; ++z)
+                at[z] = lds_address(z < 4 ? ksc : vsc) + 4 * (32 * ((z & 3) >> 1) + 8 * quarter + 4 * (z & 1));
+            read128(at, w);
+#pragma unroll
+            for (int u = 0; u < NS; ++u) {
+                kw[u] = __builtin_bit_cast(floatx4, w[u]) * a.scale;
+                vw[u] = __builtin_bit_cast(floatx4, w[4 + u]);
+            }
+        }
+        const bool whole = key0 + T::kKeys <= all_see;
+        bf16x8 p[NR][NS / 2];
+#pragma unroll
+        for (int x = 0; x < NR; ++x) {
+            float mx = kNone;
+#pragma unroll
+            for (int u = 0; u < NS; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float y = s[x][u][e] * (T::kScaled ? kw[u][e] : a.scale);
+                    if (!whole) y = key0 + 32 * (u >> 1) + 8 * quarter + 4 * (u & 1) + e <= last[x] ? y : -INFINITY;
+                    s[x][u][e] = y;
+                    mx = fmaxf(mx, y);
+                }
+            mx = fmaxf(quarter_max(mx), m[x]);
+            const float f = fast_exp2(m[x] - mx);
+            m[x] = mx;
+            float sum = 0.f;
+#pragma unroll
+            for (int u = 0; u < NS; u += 2) {
+                u32x4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int z = u + (j >> 1), e = 2 * (j & 1);
+                    float p0 = fast_exp2(s[x][z][e] - mx), p1 = fast_exp2(s[x][z][e + 1] - mx);
+                    sum += p0 + p1;
+                    if (T::kScaled) p0 *= vw[z][e], p1 *= vw[z][e + 1];
+                    y[j] = pack_bf16(p0, p1);
+                }
+                p[x][u / 2] = __builtin_bit_cast(bf16x8, y);
+            }
+            l[x] = fmaf(l[x], f, sum);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[x][t] *= f;
+        }
+        // V^T: dims 16 t + lane % 16, keys 32 u + 8 quarter + 0 .. 7
+        // eight reads: four tiles t of one 32-key step (bf16: two reads each), or of both
+        constexpr int TB = T::kScaled ? 8 / (NS / 2) : 4;
+        constexpr int UV = T::kScaled ? NS / 2 : 1;
+#pragma unroll
+        for (int t0 = 0; t0 < NT; t0 += TB)
+#pragma unroll
+            for (int u0 = 0; u0 < NS / 2; u0 += UV) {
+                uint32_t at[8];
+                u32x2 w[8];
+#pragma unroll
+                for (int z = 0; z < 8; ++z) {
+                    const int t = t0 + z / 2, u = u0 + (T::kScaled ? z & 1 : 0);
+                    at[z] = lds_address(vt) + 8 * (lane & 1) +
+                            (T::kScaled ? T::at(32 * u + 8 * quarter + ((lane & 15) >> 1), t)
+                                        : T::at(32 * u + 8 * quarter + 4 * (z & 1) + ((lane & 15) >> 2),
+                                                2 * t + ((lane >> 1) & 1)));
+                }
+                if constexpr (T::kScaled) {
+                    read_transposed8(at, w);
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) {
+                        const u32x2 y0 = widen4<TYPE>(w[z][0]), y1 = widen4<TYPE>(w[z][1]);
+                        const bf16x8 v = __builtin_bit_cast(bf16x8, (u32x4{y0[0], y0[1], y1[0], y1[1]}));
+#pragma unroll
+                        for (int x = 0; x < NR; ++x) o[x][t0 + z / 2] = mfma16(v, p[x][z & 1], o[x][t0 + z / 2]);
+                    }
+                } else {
+                    read_transposed16(at, w);
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const bf16x8 v = __builtin_bit_cast(bf16x8, (u32x4{w[2 * z][0], w[2 * z][1], w[2 * z + 1][0],
+                                                                          w[2 * z + 1][1]}));
+#pragma unroll
+                        for (int x = 0; x < NR; ++x) o[x][t0 + z] = mfma16(v, p[x][u0], o[x][t0 + z]);
+                    }
+                }
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        // this stage has been read: the one after the next into its place
+        if (tile + 2 * kWaves < tile1) load_stage(tile + 2 * kWaves, stage, ids);
+    }
+
+    // join the waves: value e of o[x][t] is dim 16 t + 4 quarter + e of row 16 x + lane % 16
+    float* const ob = reinterpret_cast<float*>(base);
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+        const float sum = quarter_sum(l[x]);
+        if (quarter == 0) ml[wave][16 * x + lane] = make_float2(m[x], sum);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            *reinterpret_cast<floatx4*>(ob + (16 * x + (lane & 15)) * kLd + 16 * t + 4 * quarter) = o[x][t];
+    }
+    __syncthreads();
+    constexpr int G = D / 8;               // lanes of a row, 8 dims each
+    for (int it = tid; it < a.rows * G; it += kThreads) {
+        const int r = it / G, d0 = 8 * (it - r * G), i = r / a.Gh;
+        float M = kNone, L = 0.f, x[8] = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml[w][r].x);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float2 v = ml[w][r];
+            const float f = fast_exp2(v.x - M);
+            L = fmaf(v.y, f, L);
+            const float* src = reinterpret_cast<const float*>(lds[w]) + r * kLd + d0;
+            const floatx4 y0 = *reinterpret_cast<const floatx4*>(src), y1 = *reinterpret_cast<const floatx4*>(src + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = fmaf(y0[e], f, x[e]), x[4 + e] = fmaf(y1[e], f, x[4 + e]);
+        }
+        if (i >= nq) L = 0.f;              // (a row that is not there took part where nothing is masked)
+        if (a.splits > 1) {
+            const int64_t pr = (static_cast<int64_t>(split) * gridDim.x + bc) * a.rows + r;
+            float* po = a.part_o + pr * D + d0;
+            *reinterpret_cast<float4*>(po) = make_float4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<float4*>(po + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            if (d0 == 0) a.part_ml[pr] = make_float2(M, L);
+        } else {
+            const float inv = L > 0.f ? 1.f / L : 0.f;
+            const int h = c * a.Gh + (r - i * a.Gh);
+            u32x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = pack_bf16(x[2 * j] * inv, x[2 * j + 1] * inv);
+            *reinterpret_cast<u32x4*>(a.out + b * a.osb + h * a.osh + i * a.ost + d0) = v;
+        }
+    }
+}
+
 // Joins the splits of a row: the largest m as reference, every sum rescaled to
 // it.  A group of D / 8 lanes per row, 8 dims each.
 template <int D>
@@ -258,14 +624,25 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a) {
 constexpr int64_t kTarget = 2 * kPlanCus;  // workgroups that fill the chip
 constexpr int kMaxSplits = 128;
 
+template <int D, int TYPE>
+void attend(const ChunkArgs& a, hipStream_t s) {
+    const unsigned heads = static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hkv);
+    if (a.rows > kFewRows) {
+        const int tiles = (a.rows + kRows - 1) / kRows;
+        hipLaunchKernelGGL((chunk_kernel<D, TYPE>), dim3(heads, tiles, a.splits), dim3(kThreads), 0, s, a);
+        return;
+    }
+    const dim3 grid(heads, a.splits);
+    if (a.rows <= 16) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 1>), grid, dim3(kThreads), 0, s, a);
+    else if (a.rows <= 32) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 2>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 4>), grid, dim3(kThreads), 0, s, a);
+}
+
 template <int D>
 hipError_t launch(const ChunkArgs& a, hipStream_t s) {
-    const int tiles = (a.rows + kRows - 1) / kRows;
-    const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hkv), tiles, a.splits);
-    if (a.pages.dtype == kCacheBf16) hipLaunchKernelGGL((chunk_kernel<D, kCacheBf16>), grid, dim3(kThreads), 0, s, a);
-    else if (a.pages.dtype == kCacheE4m3)
-        hipLaunchKernelGGL((chunk_kernel<D, kCacheE4m3>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((chunk_kernel<D, kCacheI8>), grid, dim3(kThreads), 0, s, a);
+    if (a.pages.dtype == kCacheBf16) attend<D, kCacheBf16>(a, s);
+    else if (a.pages.dtype == kCacheE4m3) attend<D, kCacheE4m3>(a, s);
+    else attend<D, kCacheI8>(a, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
@@ -277,6 +654,12 @@ hipError_t launch(const ChunkArgs& a, hipStream_t s) {
 }  // namespace
 
 int chunk_splits(int64_t heads, int rows, int T) {
+    if (rows <= kFewRows) {
+        // one workgroup per CU; a split has four rounds of its four waves at least
+        const int64_t want = kPlanCus / heads, most = T / 1024;
+        const int64_t s = want < most ? want : most;
+        return static_cast<int>(s < 1 ? 1 : s < kMaxSplits ? s : kMaxSplits);
+    }
     const int64_t base = heads * ((rows + kRows - 1) / kRows);
     const int64_t want = (kTarget + base - 1) / base, most = (T + 255) / 256;
     const int64_t s = want < most ? want : most;

@@ -923,7 +923,7 @@ int mmshiftkv_chunk_attention(const mmskv_shape* shape, const mmskv_pages* pages
     a.max_len = shape->T < a.pages.cap ? shape->T : a.pages.cap;
     a.rows = a.Gh * n;
     a.scale = static_cast<float>(query_scale(shape->d));
-    a.splits = chunk_splits(heads, a.rows, a.max_len);
+    a.splits = chunk_splits(heads, a.rows, a.max_len, a.d, a.pages.dtype);
     const size_t need = chunk_ws(shape, n);
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < need) return MMSKV_EWORKSPACE;
     const size_t part = static_cast<size_t>(a.splits) * heads * a.rows;

@@ -591,29 +591,79 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
 }
 
 // Joins the splits of a row: the largest m as reference, every sum rescaled to
-// it.  A group of D / 8 lanes per row, 8 dims each.
-template <int D>
-__global__ void __launch_bounds__(256) chunk_join_kernel(ChunkArgs a) {
-    constexpr int LANES = D / 8;
-    const int lane = threadIdx.x % LANES;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
-    const int64_t heads = static_cast<int64_t>(a.B) * a.Hkv, rows = heads * a.rows;
-    if (row >= rows) return;
-    const int bc = static_cast<int>(row / a.rows), r = static_cast<int>(row - static_cast<int64_t>(bc) * a.rows);
-    float m = kNone;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[s * rows + row].x);
-    float l = 0.f, o[8] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 ml = a.part_ml[s * rows + row];
-        if (!(ml.y > 0.f)) continue;       // saw no key
-        const float f = fast_exp2(ml.x - m);
-        const float* po = a.part_o + (s * rows + row) * D + 8 * lane;
-        const float4 x = *reinterpret_cast<const float4*>(po), y = *reinterpret_cast<const float4*>(po + 4);
-        l = fmaf(ml.y, f, l);
-        o[0] = fmaf(x.x, f, o[0]), o[1] = fmaf(x.y, f, o[1]), o[2] = fmaf(x.z, f, o[2]), o[3] = fmaf(x.w, f, o[3]);
-        o[4] = fmaf(y.x, f, o[4]), o[5] = fmaf(y.y, f, o[5]), o[6] = fmaf(y.z, f, o[6]), o[7] = fmaf(y.w, f, o[7]);
+// it.  D / 8 lanes per row and group of splits, 8 dims each; SG groups share a
+// row's splits and add their sums through LDS.  All loads of a thread (kJoinPer
+// splits at a time, no branch between them) are on their way before the first
+// is needed: a loop that waited for each split took 0.8 us a split.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinPer = 8;
+
+template <int D, int SG>
+__global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
+    constexpr int LANES = D / 8, kRowThreads = LANES * SG, kPerBlock = kJoinThreads / kRowThreads;
+    __shared__ __align__(16) float sums[SG > 1 ? kJoinThreads : 1][8];
+    __shared__ float2 ml[SG > 1 ? kJoinThreads : 1];
+    const int lane = threadIdx.x % LANES, g = threadIdx.x / LANES % SG;
+    const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kPerBlock + threadIdx.x / kRowThreads;
+    const int64_t rd = min(row, rows - 1);             // (rows behind the last one read it and write nothing)
+    float m = kNone, l = 0.f, o[8] = {};
+    for (int s0 = g; s0 < a.splits; s0 += SG * kJoinPer) {
+        float2 v[kJoinPer];
+        float4 x[kJoinPer], y[kJoinPer];
+#pragma unroll
+        for (int j = 0; j < kJoinPer; ++j) {
+            const int64_t at = min(s0 + j * SG, a.splits - 1) * rows + rd;
+            const float* po = a.part_o + at * D + 8 * lane;
+            v[j] = a.part_ml[at];
+            x[j] = *reinterpret_cast<const float4*>(po);
+            y[j] = *reinterpret_cast<const float4*>(po + 4);
+        }
+        float mx = m;
+#pragma unroll
+        for (int j = 0; j < kJoinPer; ++j) {
+            if (s0 + j * SG >= a.splits) v[j] = make_float2(kNone, 0.f);
+            mx = fmaxf(mx, v[j].x);
+        }
+        const float f0 = fast_exp2(m - mx);
+        m = mx;
+        l *= f0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= f0;
+#pragma unroll
+        for (int j = 0; j < kJoinPer; ++j) {
+            const bool any = v[j].y > 0.f;             // a split that saw no key leaves m only
+            const float f = any ? fast_exp2(v[j].x - m) : 0.f;
+            const float z[8] = {x[j].x, x[j].y, x[j].z, x[j].w, y[j].x, y[j].y, y[j].z, y[j].w};
+            l = fmaf(v[j].y, f, l);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(any ? z[e] : 0.f, f, o[e]);
+        }
     }
+    if constexpr (SG > 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[threadIdx.x][e] = o[e];
+        ml[threadIdx.x] = make_float2(m, l);
+        __syncthreads();
+        if (g != 0) return;
+        float mx = kNone;
+#pragma unroll
+        for (int j = 0; j < SG; ++j) mx = fmaxf(mx, ml[threadIdx.x + j * LANES].x);
+        l = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < SG; ++j) {
+            const float2 v = ml[threadIdx.x + j * LANES];
+            const float f = fast_exp2(v.x - mx);
+            l = fmaf(v.y, f, l);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(sums[threadIdx.x + j * LANES][e], f, o[e]);
+        }
+    }
+    if (row >= rows) return;
     const float inv = l > 0.f ? 1.f / l : 0.f;
+    const int bc = static_cast<int>(row / a.rows), r = static_cast<int>(row - static_cast<int64_t>(bc) * a.rows);
     const int b = bc / a.Hkv, c = bc - b * a.Hkv, i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
     u32x4 v;
 #pragma unroll
@@ -645,21 +695,49 @@ hipError_t launch(const ChunkArgs& a, hipStream_t s) {
     else attend<D, kCacheI8>(a, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
-    const int per = 256 / (D / 8);
-    hipLaunchKernelGGL((chunk_join_kernel<D>), dim3(static_cast<unsigned>((rows + per - 1) / per)), dim3(256), 0, s, a);
+    // one round of loads of a row's splits (16 groups at most: two rounds above 128 splits)
+    const auto join = [&](auto groups) {
+        constexpr int SG = decltype(groups)::value, kPer = kJoinThreads / (D / 8 * SG);
+        const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
+        hipLaunchKernelGGL((chunk_join_kernel<D, SG>), dim3(static_cast<unsigned>((rows + kPer - 1) / kPer)),
+                           dim3(kJoinThreads), 0, s, a);
+    };
+    if (a.splits <= kJoinPer) join(CacheType<1>{});
+    else if (a.splits <= 4 * kJoinPer) join(CacheType<4>{});
+    else join(CacheType<16>{});
     return hipGetLastError();
 }
 
 }  // namespace
 
-int chunk_splits(int64_t heads, int rows, int T) {
-    if (rows <= kFewRows) {
-        // one workgroup per CU; a split has four rounds of its four waves at least
-        const int64_t want = kPlanCus / heads, most = T / 1024;
-        const int64_t s = want < most ? want : most;
-        return static_cast<int>(s < 1 ? 1 : s < kMaxSplits ? s : kMaxSplits);
+namespace {
+
+constexpr int kFewSplits = 64;             // splits of a head, few rows
+constexpr int kFewBlocks = 4 * kPlanCus;   // their workgroups, where there are splits
+
+// Splits for few rows.  A workgroup has a CU for itself, so that the launch
+// takes as many turns as there are workgroups per CU, each of its split's rounds
+// (a tile for each of the four waves) and about two rounds' time to begin; a join
+// costs about three.  (28 heads on 4, d = 128, bf16: of 1 / 6 / 12 / 64 splits one
+// is best at 384 rows, 7.2 us, six at 700, 8.2 against 10.5, twelve at 1100, 8.7
+// against 13.6, 64 at 16384, 14.7 against 138; for 16 sequences of 16384 rows
+// four, 98.4 against 105 with 6 and 167 with 1.)
+int few_splits(int64_t heads, int T, int keys) {
+    const int64_t rounds = (T + 4 * keys - 1) / (4 * keys);
+    int64_t best = 0;
+    int best_s = 1;
+    for (int s = 1; s <= kFewSplits && s <= rounds && (s == 1 || s * heads <= kFewBlocks); ++s) {
+        const int64_t turns = (heads * s + kPlanCus - 1) / kPlanCus;
+        const int64_t cost = turns * ((rounds + s - 1) / s + 2) + (s > 1 ? 3 : 0);
+        if (s == 1 || cost < best) best = cost, best_s = s;
     }
+    return best_s;
+}
+
+}  // namespace
+
+int chunk_splits(int64_t heads, int rows, int T, int d, int dtype) {
+    if (rows <= kFewRows) return few_splits(heads, T, d == 128 && dtype == kCacheBf16 ? 32 : 64);
     const int64_t base = heads * ((rows + kRows - 1) / kRows);
     const int64_t want = (kTarget + base - 1) / base, most = (T + 255) / 256;
     const int64_t s = want < most ? want : most;
@@ -667,10 +745,18 @@ int chunk_splits(int64_t heads, int rows, int T) {
 }
 
 size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d) {
-    // splits * heads * rows: fewer than 2 kTarget workgroups have splits
-    const int64_t most = static_cast<int64_t>(T) / 256 + 1 < kMaxSplits ? static_cast<int64_t>(T) / 256 + 1 : kMaxSplits;
-    int64_t part = heads * rows;
-    part = part > (2 * kTarget * kRows) / most ? 2 * kTarget * kRows : part * most;
+    // rows of partial sums: splits * heads * rows.  Few rows: kFewBlocks
+    // workgroups at most, a split for every 128 keys at most ...
+    const int64_t few_s = T / 128 + 1 < kFewSplits ? T / 128 + 1 : kFewSplits;
+    const int64_t few_b = heads > kFewBlocks / few_s ? kFewBlocks : heads * few_s;
+    int64_t part = few_b * (rows < kFewRows ? rows : kFewRows);
+    // ... more rows: fewer than 2 kTarget workgroups have splits
+    if (rows > kFewRows) {
+        const int64_t most = T / 256 + 1 < kMaxSplits ? T / 256 + 1 : kMaxSplits;
+        int64_t tile = heads * rows;
+        tile = tile > (2 * kTarget * kRows) / most ? 2 * kTarget * kRows : tile * most;
+        if (tile > part) part = tile;
+    }
     return static_cast<size_t>(part) * (d * sizeof(float) + sizeof(float2)) + 256;
 }
 

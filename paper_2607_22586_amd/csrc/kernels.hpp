@@ -208,7 +208,7 @@ struct ChunkArgs {
     float* part_o;             // [splits, B, Hkv, rows, d] sums of 2^(x - m) v (splits > 1)
     float2* part_ml;           // [splits, B, Hkv, rows] (m, sum of 2^(x - m)), base 2
 };
-int chunk_splits(int64_t heads, int rows, int T);
+int chunk_splits(int64_t heads, int rows, int T, int d, int dtype);
 // Workspace bytes that suffice for every plan of a problem and never fall as
 // B, T or n grows.
 size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d);

@@ -395,7 +395,9 @@ int mmshiftkv_shape_scores(const mmskv_shape *shape, int32_t kind, int32_t windo
  * Row t of (b, c) is row t % page of page p = table[b * max_pages + t / page]:
  * element ((p * Hkv + c) * page + t % page) * d + j of k (and v), and, in the
  * 8-bit types, scale (p * Hkv + c) * page + t % page.  A row stands for its
- * values times its scale.  Sequences may share pages that are only read; a row
+ * values times its scale; the scales of MMSKV_E4M3 are powers of two of 2^-126
+ * to 2^120 (what mmshiftkv_cache_write makes them; others give unspecified
+ * results).  Sequences may share pages that are only read; a row
  * that two entries of one write name is written by both, in no order.  Entries
  * outside [0, n_pages) name no page: their rows are not written, and are zero
  * when they are read or attended to.

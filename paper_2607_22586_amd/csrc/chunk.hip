@@ -55,12 +55,13 @@ template <int D, int TYPE>
 __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     constexpr int KC = D / 16;             // 16-dim steps of S
     constexpr int NT = D / 32;             // 32-dim tiles of O
-    constexpr int CH = D / 8;              // 16-byte chunks (8 values) of a staged row
-    constexpr int LD = kKeys * CH / kThreads;   // chunks of K (and of V) that a thread stages
-    constexpr bool SCALED = TYPE != kCacheBf16;
-    __shared__ __align__(16) char kt[kKeys * 2 * D];
-    __shared__ __align__(16) char vt[kKeys * 2 * D];
-    __shared__ __align__(16) float ksc[kKeys], vsc[kKeys];
+    constexpr int kRow = D * kCacheBytes<TYPE>;      // bytes of a cached row
+    constexpr int kCh = kRow / 16;                   // its 16-byte chunks
+    constexpr int kLoads = kRow / 64;                // 16-byte loads of a lane for its wave's 16 rows of K (and of V)
+    constexpr bool kScaled = TYPE == kCacheI8;       // scales applied to the logits and to p
+    __shared__ __align__(16) char kt[2][kKeys * 2 * D];
+    __shared__ __align__(16) char vt[2][kKeys * 2 * D];
+    __shared__ __align__(16) float ksc[2][kScaled ? kKeys : 4], vsc[2][kScaled ? kKeys : 4];
 
     const int bc = blockIdx.x, b = bc / a.Hkv, c = bc - b * a.Hkv;
     const int r0 = static_cast<int>(gridDim.y - 1 - blockIdx.y) * kRows;
@@ -76,11 +77,66 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     const int i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
     const bool there = r < a.rows && i < nq;
     const int last = !there ? -1 : (a.causal ? len - nq + i : len - 1);
+    // keys that all rows of the wave see (those that are not there aside)
+    const int all_see = a.causal ? len - nq + (r0 + 32 * wave) / a.Gh + 1 : len;
     // keys that the workgroup's rows see together, and this split's part of them
     const int i_end = min((min(r0 + kRows, a.rows) - 1) / a.Gh, nq - 1);
     const int end = i_end < r0 / a.Gh ? 0 : max(a.causal ? len - nq + i_end + 1 : len, 0);
     const int tiles = (end + kKeys - 1) / kKeys, per = (tiles + a.splits - 1) / a.splits;
     const int tile0 = split * per, tile1 = min(tile0 + per, tiles);
+
+    // A wave stages rows 16 wave .. + 15 of a tile, which are on one page: 16
+    // rows of kRow consecutive bytes of K and of V, by way of registers, so that
+    // the next tile's are on their way while this one is worked on.
+    u32x4 kr[kLoads], vr[kLoads];
+    float ksr[kLoads], vsr[kLoads];
+    auto load = [&](int tile) {
+        const int t = tile * kKeys + 16 * wave;
+        const int id = uniform_page(a.pages, b, t);
+        const int64_t pr = pool_row(a.pages, a.Hkv, c, id, t);
+        const char* none = reinterpret_cast<const char*>(kNoRows);
+        const char* ks = id >= 0 ? static_cast<const char*>(a.pages.k) + pr * kRow : none;
+        const char* vs = id >= 0 ? static_cast<const char*>(a.pages.v) + pr * kRow : none;
+        const int step = id >= 0 ? 1024 : 0;         // (1 KB stands for a page that is not there)
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            kr[j] = *reinterpret_cast<const u32x4*>(ks + j * step + 16 * lane);
+            vr[j] = *reinterpret_cast<const u32x4*>(vs + j * step + 16 * lane);
+        }
+        if constexpr (TYPE != kCacheBf16) {
+            const float* kss = id >= 0 ? a.pages.k_scale + pr : reinterpret_cast<const float*>(none);
+            const float* vss = id >= 0 ? a.pages.v_scale + pr : reinterpret_cast<const float*>(none);
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                ksr[j] = kss[j * (64 / kCh) + lane / kCh];
+                vsr[j] = vss[j * (64 / kCh) + lane / kCh];
+            }
+        }
+    };
+    auto store = [&](int tile, int buf) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int row = 16 * wave + j * (64 / kCh) + lane / kCh, ch = lane % kCh;
+            if (tile * kKeys + row >= end) {         // may hold anything
+                kr[j] = u32x4{0u, 0u, 0u, 0u};
+                vr[j] = kr[j];
+                if (TYPE != kCacheBf16) ksr[j] = vsr[j] = TYPE == kCacheE4m3 ? 1.f : 0.f;
+            }
+            if constexpr (TYPE == kCacheBf16) {
+                *reinterpret_cast<u32x4*>(kt[buf] + staged<D>(row, ch)) = kr[j];
+                *reinterpret_cast<u32x4*>(vt[buf] + staged<D>(row, ch)) = vr[j];
+            } else {
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const u32x2 k0 = widen4<TYPE>(kr[j][2 * w], ksr[j]), k1 = widen4<TYPE>(kr[j][2 * w + 1], ksr[j]);
+                    const u32x2 v0 = widen4<TYPE>(vr[j][2 * w], vsr[j]), v1 = widen4<TYPE>(vr[j][2 * w + 1], vsr[j]);
+                    *reinterpret_cast<u32x4*>(kt[buf] + staged<D>(row, 2 * ch + w)) = u32x4{k0[0], k0[1], k1[0], k1[1]};
+                    *reinterpret_cast<u32x4*>(vt[buf] + staged<D>(row, 2 * ch + w)) = u32x4{v0[0], v0[1], v1[0], v1[1]};
+                }
+                if (kScaled && ch == 0) ksc[buf][row] = ksr[j] * a.scale, vsc[buf][row] = vsr[j];
+            }
+        }
+    };
 
     bf16x8 qf[KC];
     {
@@ -95,37 +151,15 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         for (int j = 0; j < 16; ++j) o[t][j] = 0.f;
     float m = kNone, l = 0.f;
 
-    for (int tile = tile0; tile < tile1; ++tile) {
+    if (tile0 < tile1) {
+        load(tile0);
+        store(tile0, 0);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int tile = tile0; tile < tile1; ++tile, buf ^= 1) {
         const int key0 = tile * kKeys;
-        __syncthreads();                   // the previous tile has been read
-#pragma unroll
-        for (int j = 0; j < LD; ++j) {
-            const int row = (tid + j * kThreads) / CH, ch = tid % CH, t = key0 + row;
-            u32x4 kv = {0u, 0u, 0u, 0u}, vv = kv;
-            float ks = 0.f, vs = 0.f;
-            const int id = t < end ? page_of(a.pages, b, t) : -1;
-            if (id >= 0) {
-                const int64_t pr = pool_row(a.pages, a.Hkv, c, id, t);
-                const int64_t e = (pr * CH + ch) * 8;
-                if constexpr (SCALED) {
-                    const u32x2 kr = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.pages.k) + e);
-                    const u32x2 vr = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.pages.v) + e);
-                    const u32x2 k0 = widen4<TYPE>(kr[0]), k1 = widen4<TYPE>(kr[1]);
-                    const u32x2 v0 = widen4<TYPE>(vr[0]), v1 = widen4<TYPE>(vr[1]);
-                    kv = u32x4{k0[0], k0[1], k1[0], k1[1]};
-                    vv = u32x4{v0[0], v0[1], v1[0], v1[1]};
-                    ks = a.pages.k_scale[pr];
-                    vs = a.pages.v_scale[pr];
-                } else {
-                    kv = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.pages.k) + e);
-                    vv = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.pages.v) + e);
-                }
-            }
-            *reinterpret_cast<u32x4*>(kt + staged<D>(row, ch)) = kv;
-            *reinterpret_cast<u32x4*>(vt + staged<D>(row, ch)) = vv;
-            if (SCALED && ch == 0) ksc[row] = ks * a.scale, vsc[row] = vs;
-        }
-        __syncthreads();
+        if (tile + 1 < tile1) load(tile + 1);
 
         // value e of s[u] is key key0 + 32 u + 8 (e / 4) + 4 half + e % 4
         floatx16 s[2];
@@ -136,25 +170,43 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
 #pragma unroll
             for (int kc = 0; kc < KC; ++kc) {
                 const bf16x8 k = load_bf16x8(reinterpret_cast<const uint16_t*>(
-                    kt + staged<D>(32 * u + (lane & 31), 2 * kc + half)));
+                    kt[buf] + staged<D>(32 * u + (lane & 31), 2 * kc + half)));
                 s[u] = mfma32(k, qf[kc], s[u]);
             }
         }
-        float mx = kNone;
+        if constexpr (kScaled) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[u][e] *= ksc[buf][32 * u + 8 * (e >> 2) + 4 * half + (e & 3)];
+        }
+        if (key0 + kKeys > all_see) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    s[u][e] = key0 + 32 * u + 8 * (e >> 2) + 4 * half + (e & 3) <= last ? s[u][e] : -INFINITY;
+        }
+        const float scale = kScaled ? 1.f : a.scale;
+        float mx = s[0][0];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int row = 32 * u + 8 * (e >> 2) + 4 * half + (e & 3);
-                float x = s[u][e] * (SCALED ? ksc[row] : a.scale);
-                x = key0 + row <= last ? x : -INFINITY;
-                s[u][e] = x;
-                mx = fmaxf(mx, x);
-            }
-        mx = fmaxf(half_max(mx), m);
-        const float f = fast_exp2(m - mx);
-        m = mx;
-        l *= f;
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e]);
+        mx = half_max(mx) * scale;
+        // The reference m moves only where it is left behind by more than 2^8: the
+        // sums hold as well relative to any m near the maximum, and the output is
+        // rescaled in few tiles.
+        if (__any(mx > m + 8.f)) {
+            mx = fmaxf(mx, m);
+            const float f = fast_exp2(m - mx);
+            m = mx;
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[t][j] *= f;
+        }
         bf16x8 p[4];                       // p[2 u + w]: values 8 w .. 8 w + 7 of s[u]
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -166,19 +218,17 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
                     float x[2];
 #pragma unroll
                     for (int z = 0; z < 2; ++z) {
-                        const int e = 8 * w + 2 * j + z, row = 32 * u + 8 * (e >> 2) + 4 * half + (e & 3);
-                        x[z] = fast_exp2(s[u][e] - m);
+                        const int e = 8 * w + 2 * j + z;
+                        x[z] = fast_exp2(kScaled ? s[u][e] - m : fmaf(s[u][e], scale, -m));
                         l += x[z];
-                        if (SCALED) x[z] *= vsc[row];
+                        if (kScaled) x[z] *= vsc[buf][32 * u + 8 * (e >> 2) + 4 * half + (e & 3)];
                     }
                     y[j] = pack_bf16(x[0], x[1]);
                 }
                 p[2 * u + w] = __builtin_bit_cast(bf16x8, y);
             }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[t][j] *= f;
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 // V^T: dims 32 t + lane % 32, keys 16 u + 4 half + {0..3, 8..11}
@@ -189,17 +239,19 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
                     const int row = 16 * u + 8 * w + 4 * half + ((lane & 15) >> 2);
                     const int dim = 32 * t + (lane & 16) + 4 * (lane & 3);
                     const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds4)(vt + staged<D>(row, dim >> 3) + 2 * (dim & 7)));
+                        (lds4)(vt[buf] + staged<D>(row, dim >> 3) + 2 * (dim & 7)));
                     const u32x2 y = __builtin_bit_cast(u32x2, x);
                     v[2 * w] = y[0];
                     v[2 * w + 1] = y[1];
                 }
                 o[t] = mfma32(__builtin_bit_cast(bf16x8, v), p[u], o[t]);
             }
-        }
+        if (tile + 1 < tile1) store(tile + 1, buf ^ 1);
+        __syncthreads();
     }
     l = half_sum(l);
     if (r >= a.rows) return;
+    if (!there) l = 0.f;                   // (took part where nothing is masked)
     // value 4 w + j of o[t] is dim 32 t + 8 w + 4 half + j
     if (a.splits > 1) {
         const int64_t pr = (static_cast<int64_t>(split) * gridDim.x + bc) * a.rows + r;
@@ -307,15 +359,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
         int id[T::kGroups];
     };
     auto pages_of = [&](int tile) {
-        typedef const int __attribute__((address_space(4))) * ctable;
-        const ctable row = (ctable)(a.pages.table) + static_cast<int64_t>(b) * a.pages.max_pages;
         Ids ids;
 #pragma unroll
-        for (int g = 0; g < T::kGroups; ++g) {
-            const int j = (tile * T::kKeys + 16 * g) >> a.pages.shift;
-            const int id = row[min(j, a.pages.max_pages - 1)];
-            ids.id[g] = j < a.pages.max_pages && static_cast<uint32_t>(id) < static_cast<uint32_t>(a.pages.n_pages) ? id : -1;
-        }
+        for (int g = 0; g < T::kGroups; ++g) ids.id[g] = uniform_page(a.pages, b, tile * T::kKeys + 16 * g);
         return ids;
     };
     auto load_stage = [&](int tile, int stage, const Ids& ids) {

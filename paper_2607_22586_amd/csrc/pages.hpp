@@ -111,6 +111,16 @@ __device__ __forceinline__ void read_transposed8(const uint32_t (&at)[8], u32x2 
                  : "memory");
 }
 
+// Page of row t of sequence b for a whole wave, by a scalar load (its wait is not
+// that of the vector loads); -1 as page_of.
+__device__ __forceinline__ int uniform_page(const Pages& p, int b, int t) {
+    typedef const int __attribute__((address_space(4))) * ctable;
+    const ctable row = (ctable)(p.table) + static_cast<int64_t>(b) * p.max_pages;
+    const int j = t >> p.shift;
+    const int id = row[min(j, p.max_pages - 1)];
+    return j < p.max_pages && static_cast<uint32_t>(id) < static_cast<uint32_t>(p.n_pages) ? id : -1;
+}
+
 // Row number, in the pool seen as [n_pages * Hkv * page, d], of row t of head c
 // on page id (in 64 bits: a pool may hold more than 2^31 rows).
 __device__ __forceinline__ int64_t pool_row(const Pages& p, int Hkv, int c, int id, int t) {
@@ -129,12 +139,12 @@ __device__ __forceinline__ void unpack4(uint32_t w, float (&x)[4]) {
     }
 }
 
-// The same four as bf16 (both types fit it exactly).
+// The same four as bf16 (both types fit it exactly); e4m3: times a power of two.
 template <int TYPE>
-__device__ __forceinline__ u32x2 widen4(uint32_t w) {
+__device__ __forceinline__ u32x2 widen4(uint32_t w, float scale = 1.f) {
     if constexpr (TYPE == kCacheE4m3) {
-        return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true))};
+        return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
     } else {
         float x[4];
         unpack4<TYPE>(w, x);

@@ -23,7 +23,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kRows = 32 * kWaves;         // query rows of a workgroup
 constexpr int kKeys = 64;                  // keys of a tile
 constexpr float kNone = -3e38f;            // running maximum before the first visible key
 
@@ -41,6 +40,9 @@ __device__ __forceinline__ float half_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Waves of a workgroup of many rows, 32 rows each.
+constexpr int tile_waves(int d) { return d == 64 ? 4 : 4; }
+
 // Bytes from the start of a staged tile to 16-byte chunk ch of row r.  Rows
 // without padding; the chunks of a row are permuted by its index, so that 16
 // consecutive rows of one chunk (the reads of K) and four rows of 64 bytes (the
@@ -51,13 +53,16 @@ __device__ __forceinline__ int staged(int r, int ch) {
     return r * (2 * D) + 16 * (ch ^ swz);
 }
 
-template <int D, int TYPE>
-__global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
+template <int D, int TYPE, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 8 / WAVES) chunk_kernel(ChunkArgs a) {
+    constexpr int kRows = 32 * WAVES;      // query rows of the workgroup
     constexpr int KC = D / 16;             // 16-dim steps of S
     constexpr int NT = D / 32;             // 32-dim tiles of O
     constexpr int kRow = D * kCacheBytes<TYPE>;      // bytes of a cached row
     constexpr int kCh = kRow / 16;                   // its 16-byte chunks
-    constexpr int kLoads = kRow / 64;                // 16-byte loads of a lane for its wave's 16 rows of K (and of V)
+    constexpr int kWaveRows = kKeys / WAVES;         // rows of a tile that a wave stages
+    constexpr int kLoads = kWaveRows * kRow / 1024;  // its 16-byte loads of a lane of K (and of V)
+    static_assert(kLoads >= 1, "whole load instructions");
     constexpr bool kScaled = TYPE == kCacheI8;       // scales applied to the logits and to p
     __shared__ __align__(16) char kt[2][kKeys * 2 * D];
     __shared__ __align__(16) char vt[2][kKeys * 2 * D];
@@ -77,35 +82,38 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     const int i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
     const bool there = r < a.rows && i < nq;
     const int last = !there ? -1 : (a.causal ? len - nq + i : len - 1);
-    // keys that all rows of the wave see (those that are not there aside)
-    const int all_see = a.causal ? len - nq + (r0 + 32 * wave) / a.Gh + 1 : len;
+    // keys that all rows of the workgroup see (those that are not there aside)
+    const int all_see = a.causal ? len - nq + r0 / a.Gh + 1 : len;
     // keys that the workgroup's rows see together, and this split's part of them
     const int i_end = min((min(r0 + kRows, a.rows) - 1) / a.Gh, nq - 1);
     const int end = i_end < r0 / a.Gh ? 0 : max(a.causal ? len - nq + i_end + 1 : len, 0);
     const int tiles = (end + kKeys - 1) / kKeys, per = (tiles + a.splits - 1) / a.splits;
     const int tile0 = split * per, tile1 = min(tile0 + per, tiles);
 
-    // A wave stages rows 16 wave .. + 15 of a tile, which are on one page: 16
-    // rows of kRow consecutive bytes of K and of V, by way of registers, so that
-    // the next tile's are on their way while this one is worked on.
+    // A wave stages rows kWaveRows * wave .. of a tile, which are on one page:
+    // consecutive bytes of K and of V, by way of registers, so that the next
+    // tile's are on their way while this one is worked on.
     u32x4 kr[kLoads], vr[kLoads];
     float ksr[kLoads], vsr[kLoads];
     auto load = [&](int tile) {
-        const int t = tile * kKeys + 16 * wave;
+        const int t = tile * kKeys + kWaveRows * wave;
         const int id = uniform_page(a.pages, b, t);
         const int64_t pr = pool_row(a.pages, a.Hkv, c, id, t);
-        const char* none = reinterpret_cast<const char*>(kNoRows);
-        const char* ks = id >= 0 ? static_cast<const char*>(a.pages.k) + pr * kRow : none;
-        const char* vs = id >= 0 ? static_cast<const char*>(a.pages.v) + pr * kRow : none;
+        typedef const char __attribute__((address_space(1))) * gchar;
+        typedef const u32x4 __attribute__((address_space(1))) * gvec;
+        typedef const float __attribute__((address_space(1))) * gfloat;
+        const gchar none = (gchar)(kNoRows);
+        const gchar ks = id >= 0 ? (gchar)(a.pages.k) + pr * kRow : none;
+        const gchar vs = id >= 0 ? (gchar)(a.pages.v) + pr * kRow : none;
         const int step = id >= 0 ? 1024 : 0;         // (1 KB stands for a page that is not there)
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            kr[j] = *reinterpret_cast<const u32x4*>(ks + j * step + 16 * lane);
-            vr[j] = *reinterpret_cast<const u32x4*>(vs + j * step + 16 * lane);
+            kr[j] = *(gvec)(ks + j * step + 16 * lane);
+            vr[j] = *(gvec)(vs + j * step + 16 * lane);
         }
         if constexpr (TYPE != kCacheBf16) {
-            const float* kss = id >= 0 ? a.pages.k_scale + pr : reinterpret_cast<const float*>(none);
-            const float* vss = id >= 0 ? a.pages.v_scale + pr : reinterpret_cast<const float*>(none);
+            const gfloat kss = id >= 0 ? (gfloat)(a.pages.k_scale) + pr : (gfloat)(none);
+            const gfloat vss = id >= 0 ? (gfloat)(a.pages.v_scale) + pr : (gfloat)(none);
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 ksr[j] = kss[j * (64 / kCh) + lane / kCh];
@@ -116,8 +124,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     auto store = [&](int tile, int buf) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int row = 16 * wave + j * (64 / kCh) + lane / kCh, ch = lane % kCh;
-            if (tile * kKeys + row >= end) {         // may hold anything
+            const int row = kWaveRows * wave + j * (64 / kCh) + lane / kCh, ch = lane % kCh;
+            if ((tile + 1) * kKeys > end && tile * kKeys + row >= end) {     // may hold anything
                 kr[j] = u32x4{0u, 0u, 0u, 0u};
                 vr[j] = kr[j];
                 if (TYPE != kCacheBf16) ksr[j] = vsr[j] = TYPE == kCacheE4m3 ? 1.f : 0.f;
@@ -151,65 +159,41 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         for (int j = 0; j < 16; ++j) o[t][j] = 0.f;
     float m = kNone, l = 0.f;
 
-    if (tile0 < tile1) {
-        load(tile0);
-        store(tile0, 0);
-    }
-    __syncthreads();
-    int buf = 0;
-    for (int tile = tile0; tile < tile1; ++tile, buf ^= 1) {
-        const int key0 = tile * kKeys;
-        if (tile + 1 < tile1) load(tile + 1);
-
-        // value e of s[u] is key key0 + 32 u + 8 (e / 4) + 4 half + e % 4
+    // value e of s[u] is key key0 + 32 u + 8 (e / 4) + 4 half + e % 4
+    const float scale = kScaled ? 1.f : a.scale;
+    // One tile, in two 32-key halves u.  MASKED: some row does not see all of it.
+    auto attend = [&](int key0, int buf, auto masked) {
+        constexpr bool MASKED = decltype(masked)::value != 0;
+        // staged() of this lane's rows of K (chunk 2 kc + half: a permuted chunk is
+        // one exclusive or away) and of V; opaque, so that they are formed where
+        // they are used instead of being kept in 24 registers
+        int ka = staged<D>(lane & 31, half), va = staged<D>(4 * half + ((lane & 15) >> 2), (lane & 16) / 8 + ((lane & 3) >> 1));
+        va += 8 * (lane & 1);
+        asm volatile("" : "+v"(ka), "+v"(va));
+        const int rel = last - key0 - 4 * half;
         floatx16 s[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        auto logits = [&](int u) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
 #pragma unroll
             for (int kc = 0; kc < KC; ++kc) {
-                const bf16x8 k = load_bf16x8(reinterpret_cast<const uint16_t*>(
-                    kt[buf] + staged<D>(32 * u + (lane & 31), 2 * kc + half)));
+                const bf16x8 k = load_bf16x8(reinterpret_cast<const uint16_t*>(kt[buf] + u * 32 * 2 * D + (ka ^ (32 * kc))));
                 s[u] = mfma32(k, qf[kc], s[u]);
             }
-        }
-        if constexpr (kScaled) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[u][e] *= ksc[buf][32 * u + 8 * (e >> 2) + 4 * half + (e & 3)];
-        }
-        if (key0 + kKeys > all_see) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
+        };
+        auto row_scale = [&](int u, int e) { return ksc[buf][32 * u + 8 * (e >> 2) + 4 * half + (e & 3)]; };
+        // what is left to multiply s[u][e] by (a masked -inf meets no scale of 0)
+        auto logit_scale = [&](int u, int e) { return !kScaled ? scale : MASKED ? 1.f : row_scale(u, e); };
+        auto mask = [&](int u) {
+            if constexpr (MASKED) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    s[u][e] = key0 + 32 * u + 8 * (e >> 2) + 4 * half + (e & 3) <= last ? s[u][e] : -INFINITY;
-        }
-        const float scale = kScaled ? 1.f : a.scale;
-        float mx = s[0][0];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e]);
-        mx = half_max(mx) * scale;
-        // The reference m moves only where it is left behind by more than 2^8: the
-        // sums hold as well relative to any m near the maximum, and the output is
-        // rescaled in few tiles.
-        if (__any(mx > m + 8.f)) {
-            mx = fmaxf(mx, m);
-            const float f = fast_exp2(m - mx);
-            m = mx;
-            l *= f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[t][j] *= f;
-        }
-        bf16x8 p[4];                       // p[2 u + w]: values 8 w .. 8 w + 7 of s[u]
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
+                    s[u][e] = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? (kScaled ? s[u][e] * row_scale(u, e) : s[u][e]) : -INFINITY;
+            }
+        };
+        // p[w]: values 8 w .. 8 w + 7 of s[u], relative to m; their sum
+        auto weights = [&](int u, bf16x8 (&p)[2]) {
+            float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 u32x4 y;
@@ -218,37 +202,86 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
                     float x[2];
 #pragma unroll
                     for (int z = 0; z < 2; ++z) {
-                        const int e = 8 * w + 2 * j + z;
-                        x[z] = fast_exp2(kScaled ? s[u][e] - m : fmaf(s[u][e], scale, -m));
-                        l += x[z];
-                        if (kScaled) x[z] *= vsc[buf][32 * u + 8 * (e >> 2) + 4 * half + (e & 3)];
+                        const int e = 8 * w + 2 * j + z, row = 32 * u + 8 * (e >> 2) + 4 * half + (e & 3);
+                        x[z] = fast_exp2(fmaf(s[u][e], logit_scale(u, e), -m));
+                        sum += x[z];
+                        if (kScaled) x[z] *= vsc[buf][row];
                     }
                     y[j] = pack_bf16(x[0], x[1]);
                 }
-                p[2 * u + w] = __builtin_bit_cast(bf16x8, y);
+                p[w] = __builtin_bit_cast(bf16x8, y);
             }
+            return sum;
+        };
+        // The reference m moves only where a lane's sum says that it is left far
+        // behind: the sums hold as well relative to any m near the maximum, so that
+        // no maximum is formed in most tiles and the output seldom rescaled.
+        auto settle = [&](bf16x8 (&p0)[2], bf16x8 (&p1)[2], float sum) {
+            if (__any(!(sum < 0x1p16f))) {
+                float mx = kNone;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                // V^T: dims 32 t + lane % 32, keys 16 u + 4 half + {0..3, 8..11}
-                typedef s16x4 __attribute__((address_space(3))) * lds4;
-                u32x4 v;
+                    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e] * logit_scale(u, e));
+                mx = fmaxf(half_max(mx), m);
+                const float f = fast_exp2(m - mx);
+                m = mx;
+                l *= f;
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const int row = 16 * u + 8 * w + 4 * half + ((lane & 15) >> 2);
-                    const int dim = 32 * t + (lane & 16) + 4 * (lane & 3);
-                    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds4)(vt[buf] + staged<D>(row, dim >> 3) + 2 * (dim & 7)));
-                    const u32x2 y = __builtin_bit_cast(u32x2, x);
-                    v[2 * w] = y[0];
-                    v[2 * w + 1] = y[1];
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[t][j] *= f;
+                sum = weights(0, p0) + weights(1, p1);
+            }
+            l += sum;
+        };
+        auto output = [&](int u, const bf16x8 (&p)[2]) {
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    // V^T: dims 32 t + lane % 32, keys 32 u + 16 w + 4 half + {0..3, 8..11}
+                    typedef s16x4 __attribute__((address_space(3))) * lds4;
+                    u32x4 v;
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        // eight rows further the permutation differs by two chunks (d = 128 and 64)
+                        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (lds4)(vt[buf] + (32 * u + 16 * w + 8 * z) * 2 * D + (va ^ (64 * t + 32 * z))));
+                        const u32x2 y = __builtin_bit_cast(u32x2, x);
+                        v[2 * z] = y[0];
+                        v[2 * z + 1] = y[1];
+                    }
+                    o[t] = mfma32(__builtin_bit_cast(bf16x8, v), p[w], o[t]);
                 }
-                o[t] = mfma32(__builtin_bit_cast(bf16x8, v), p[u], o[t]);
-            }
+        };
+        bf16x8 p0[2], p1[2];
+        logits(0);
+        mask(0);
+        logits(1);
+        mask(1);
+        const float sum0 = weights(0, p0), sum1 = weights(1, p1);
+        settle(p0, p1, sum0 + sum1);
+        output(0, p0);
+        output(1, p1);
+    };
+
+    if (tile0 < tile1) {
+        load(tile0);
+        store(tile0, 0);
+    }
+    __syncthreads();
+    int buf = 0, tile = tile0;
+    auto step = [&](auto masked) {
+        if (tile + 1 < tile1) load(tile + 1);
+        attend(tile * kKeys, buf, masked);
         if (tile + 1 < tile1) store(tile + 1, buf ^ 1);
         __syncthreads();
-    }
+        ++tile, buf ^= 1;
+    };
+    const int whole = min(max(all_see, 0) / kKeys, tile1);
+    while (tile < whole) step(CacheType<0>{});
+    while (tile < tile1) step(CacheType<1>{});
     l = half_sum(l);
     if (r >= a.rows) return;
     if (!there) l = 0.f;                   // (took part where nothing is masked)
@@ -717,15 +750,16 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
     *reinterpret_cast<u32x4*>(a.out + b * a.osb + h * a.osh + i * a.ost + 8 * lane) = v;
 }
 
-constexpr int64_t kTarget = 2 * kPlanCus;  // workgroups that fill the chip
+constexpr int64_t kTileRowsMost = 256 * 2 * kPlanCus;  // rows of the workgroups that fill the chip
 constexpr int kMaxSplits = 128;
 
 template <int D, int TYPE>
 void attend(const ChunkArgs& a, hipStream_t s) {
     const unsigned heads = static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hkv);
     if (a.rows > kFewRows) {
-        const int tiles = (a.rows + kRows - 1) / kRows;
-        hipLaunchKernelGGL((chunk_kernel<D, TYPE>), dim3(heads, tiles, a.splits), dim3(kThreads), 0, s, a);
+        constexpr int W = tile_waves(D);
+        const int tiles = (a.rows + 32 * W - 1) / (32 * W);
+        hipLaunchKernelGGL((chunk_kernel<D, TYPE, W>), dim3(heads, tiles, a.splits), dim3(64 * W), 0, s, a);
         return;
     }
     const dim3 grid(heads, a.splits);
@@ -784,9 +818,10 @@ int few_splits(int64_t heads, int T, int keys) {
 
 int chunk_splits(int64_t heads, int rows, int T, int d, int dtype) {
     if (rows <= kFewRows) return few_splits(heads, T, d == 128 && dtype == kCacheBf16 ? 32 : 64);
-    const int64_t base = heads * ((rows + kRows - 1) / kRows);
-    const int64_t want = (kTarget + base - 1) / base, most = (T + 255) / 256;
-    const int64_t s = want < most ? want : most;
+    const int wg_rows = 32 * tile_waves(d);
+    const int64_t base = heads * ((rows + wg_rows - 1) / wg_rows);
+    const int64_t want = 2 * kPlanCus / base, most = (T + 255) / 256;
+    const int64_t s = want < 1 ? 1 : want < most ? want : most;
     return static_cast<int>(s < kMaxSplits ? s : kMaxSplits);
 }
 
@@ -796,11 +831,11 @@ size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d) {
     const int64_t few_s = T / 128 + 1 < kFewSplits ? T / 128 + 1 : kFewSplits;
     const int64_t few_b = heads > kFewBlocks / few_s ? kFewBlocks : heads * few_s;
     int64_t part = few_b * (rows < kFewRows ? rows : kFewRows);
-    // ... more rows: fewer than 2 kTarget workgroups have splits
+    // ... more rows: where there are splits, they fill the chip once
     if (rows > kFewRows) {
         const int64_t most = T / 256 + 1 < kMaxSplits ? T / 256 + 1 : kMaxSplits;
         int64_t tile = heads * rows;
-        tile = tile > (2 * kTarget * kRows) / most ? 2 * kTarget * kRows : tile * most;
+        tile = tile > kTileRowsMost / most ? kTileRowsMost : tile * most;
         if (tile > part) part = tile;
     }
     return static_cast<size_t>(part) * (d * sizeof(float) + sizeof(float2)) + 256;

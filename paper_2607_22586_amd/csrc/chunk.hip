@@ -18,6 +18,7 @@
 namespace mmskv {
 namespace {
 
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -121,28 +122,34 @@ __global__ void __launch_bounds__(64 * WAVES, 8 / WAVES) chunk_kernel(ChunkArgs 
             }
         }
     };
-    auto store = [&](int tile, int buf) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int row = kWaveRows * wave + j * (64 / kCh) + lane / kCh, ch = lane % kCh;
-            if ((tile + 1) * kKeys > end && tile * kKeys + row >= end) {     // may hold anything
-                kr[j] = u32x4{0u, 0u, 0u, 0u};
-                vr[j] = kr[j];
-                if (TYPE != kCacheBf16) ksr[j] = vsr[j] = TYPE == kCacheE4m3 ? 1.f : 0.f;
-            }
-            if constexpr (TYPE == kCacheBf16) {
-                *reinterpret_cast<u32x4*>(kt[buf] + staged<D>(row, ch)) = kr[j];
-                *reinterpret_cast<u32x4*>(vt[buf] + staged<D>(row, ch)) = vr[j];
-            } else {
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const u32x2 k0 = widen4<TYPE>(kr[j][2 * w], ksr[j]), k1 = widen4<TYPE>(kr[j][2 * w + 1], ksr[j]);
-                    const u32x2 v0 = widen4<TYPE>(vr[j][2 * w], vsr[j]), v1 = widen4<TYPE>(vr[j][2 * w + 1], vsr[j]);
-                    *reinterpret_cast<u32x4*>(kt[buf] + staged<D>(row, 2 * ch + w)) = u32x4{k0[0], k0[1], k1[0], k1[1]};
-                    *reinterpret_cast<u32x4*>(vt[buf] + staged<D>(row, 2 * ch + w)) = u32x4{v0[0], v0[1], v1[0], v1[1]};
-                }
-                if (kScaled && ch == 0) ksc[buf][row] = ksr[j] * a.scale, vsc[buf][row] = vsr[j];
-            }
+    // Piece z (of kPieces) of what a lane stages: 16 bytes of a staged row of K (z
+    // even) or V.
+    constexpr int kPieces = 2 * kLoads * (TYPE == kCacheBf16 ? 1 : 2);
+    auto store_piece = [&](int buf, int z) {
+        const int j = TYPE == kCacheBf16 ? z / 2 : z / 4, w = z / 2 % 2;
+        const int row = kWaveRows * wave + j * (64 / kCh) + lane / kCh, ch = lane % kCh;
+        const bool v = z % 2 != 0;
+        char* const to = (v ? vt : kt)[buf];
+        const u32x4 x = v ? vr[j] : kr[j];
+        if constexpr (TYPE == kCacheBf16) {
+            *reinterpret_cast<u32x4*>(to + staged<D>(row, ch)) = x;
+        } else {
+            const float by = v ? vsr[j] : ksr[j];
+            const u32x2 y0 = widen4<TYPE>(w ? x[2] : x[0], by), y1 = widen4<TYPE>(w ? x[3] : x[1], by);
+            *reinterpret_cast<u32x4*>(to + (staged<D>(row, 2 * ch) ^ (16 * w))) = u32x4{y0[0], y0[1], y1[0], y1[1]};
+            if (kScaled && w == 0 && ch == 0) (v ? vsc : ksc)[buf][row] = v ? by : by * a.scale;
+        }
+    };
+    // Rows of V behind the last key may hold anything: zeros, for p = 0 to meet
+    // (their logits are masked).  By the wave that staged them.
+    auto clear_tail = [&](int tile, int buf) {
+        if ((tile + 1) * kKeys <= end) return;
+        constexpr int kOut = 2 * D / 16;
+        for (int x = lane; x < kWaveRows * kOut; x += kWave) {
+            const int row = kWaveRows * wave + x / kOut;
+            if (tile * kKeys + row < end) continue;
+            *reinterpret_cast<u32x4*>(vt[buf] + row * 2 * D + 16 * (x % kOut)) = u32x4{0u, 0u, 0u, 0u};
+            if (kScaled) vsc[buf][row] = 0.f;
         }
     };
 
@@ -161,9 +168,18 @@ __global__ void __launch_bounds__(64 * WAVES, 8 / WAVES) chunk_kernel(ChunkArgs 
 
     // value e of s[u] is key key0 + 32 u + 8 (e / 4) + 4 half + e % 4
     const float scale = kScaled ? 1.f : a.scale;
-    // One tile, in two 32-key halves u.  MASKED: some row does not see all of it.
-    auto attend = [&](int key0, int buf, auto masked) {
+    // One tile, in two 32-key halves u, as a sequence of steps of one matrix
+    // instruction with vector instructions to run beside it: the exponentials of
+    // half 0 with the second half's S, those of half 1 with the first half's part
+    // of O, the staging of the next tile with the second's.  (Left to itself the
+    // compiler puts all matrix instructions of a phase first, and a SIMD's two
+    // waves do not fill the gaps: 960 TFLOP/s.)  MASKED: some row does not see all.
+    auto attend = [&](int key0, int buf, auto masked, auto staging) {
         constexpr bool MASKED = decltype(masked)::value != 0;
+        constexpr int N = KC;              // steps of a phase: KC = 2 NT
+        constexpr int PAIRS = 8 / N;       // pairs of exponentials of a step
+        constexpr int AHEAD = 4;           // steps from a read of LDS to its use
+        static_assert(N == 2 * NT, "as many steps in S as in O");
         // staged() of this lane's rows of K (chunk 2 kc + half: a permuted chunk is
         // one exclusive or away) and of V; opaque, so that they are formed where
         // they are used instead of being kept in 24 registers
@@ -172,57 +188,61 @@ __global__ void __launch_bounds__(64 * WAVES, 8 / WAVES) chunk_kernel(ChunkArgs 
         asm volatile("" : "+v"(ka), "+v"(va));
         const int rel = last - key0 - 4 * half;
         floatx16 s[2];
-        auto logits = [&](int u) {
+        floatx4 kw[4], vw[4];              // scales of a half's keys
+        auto scales = [&](int u) {
+            if constexpr (kScaled) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
-#pragma unroll
-            for (int kc = 0; kc < KC; ++kc) {
-                const bf16x8 k = load_bf16x8(reinterpret_cast<const uint16_t*>(kt[buf] + u * 32 * 2 * D + (ka ^ (32 * kc))));
-                s[u] = mfma32(k, qf[kc], s[u]);
-            }
-        };
-        auto row_scale = [&](int u, int e) { return ksc[buf][32 * u + 8 * (e >> 2) + 4 * half + (e & 3)]; };
-        // what is left to multiply s[u][e] by (a masked -inf meets no scale of 0)
-        auto logit_scale = [&](int u, int e) { return !kScaled ? scale : MASKED ? 1.f : row_scale(u, e); };
-        auto mask = [&](int u) {
-            if constexpr (MASKED) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    s[u][e] = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? (kScaled ? s[u][e] * row_scale(u, e) : s[u][e]) : -INFINITY;
-            }
-        };
-        // p[w]: values 8 w .. 8 w + 7 of s[u], relative to m; their sum
-        auto weights = [&](int u, bf16x8 (&p)[2]) {
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                u32x4 y;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float x[2];
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const int e = 8 * w + 2 * j + z, row = 32 * u + 8 * (e >> 2) + 4 * half + (e & 3);
-                        x[z] = fast_exp2(fmaf(s[u][e], logit_scale(u, e), -m));
-                        sum += x[z];
-                        if (kScaled) x[z] *= vsc[buf][row];
-                    }
-                    y[j] = pack_bf16(x[0], x[1]);
+                for (int g = 0; g < 4; ++g) {
+                    kw[g] = *reinterpret_cast<const floatx4*>(ksc[buf] + 32 * u + 8 * g + 4 * half);
+                    vw[g] = *reinterpret_cast<const floatx4*>(vsc[buf] + 32 * u + 8 * g + 4 * half);
                 }
-                p[w] = __builtin_bit_cast(bf16x8, y);
             }
-            return sum;
+        };
+        auto k_frag = [&](int j) {         // step j % N of half j / N
+            return load_bf16x8(reinterpret_cast<const uint16_t*>(kt[buf] + j / N * 32 * 2 * D + (ka ^ (32 * (j % N)))));
+        };
+        auto v_frag = [&](int j) {         // half j / N, step j % N: keys 16 w .., dims 32 t ..
+            typedef s16x4 __attribute__((address_space(3))) * lds4;
+            const int u = j / N, w = j % N / NT, t = j % NT;
+            u32x4 v;
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                // V^T: dims 32 t + lane % 32, keys 32 u + 16 w + 4 half + {0..3, 8..11}; eight
+                // rows further the permutation differs by two chunks (d = 128 and 64)
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds4)(vt[buf] + (32 * u + 16 * w + 8 * z) * 2 * D + (va ^ (64 * t + 32 * z))));
+                const u32x2 y = __builtin_bit_cast(u32x2, x);
+                v[2 * z] = y[0];
+                v[2 * z + 1] = y[1];
+            }
+            return __builtin_bit_cast(bf16x8, v);
+        };
+        // logit e of half u, scaled; a masked one is -inf whatever its row's scale
+        auto logit = [&](int u, int e, float less) {
+            float x = fmaf(s[u][e], kScaled ? kw[e >> 2][e & 3] : scale, -less);
+            if (MASKED) x = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? x : -INFINITY;
+            return x;
+        };
+        // p of values 2 j, 2 j + 1 of half u relative to m, as bf16; their sum
+        auto pair = [&](int u, int j, float& sum) {
+            float x[2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                const int e = 2 * j + z;
+                x[z] = fast_exp2(logit(u, e, m));
+                sum += x[z];
+                if (kScaled) x[z] *= vw[e >> 2][e & 3];
+            }
+            return pack_bf16(x[0], x[1]);
         };
         // The reference m moves only where a lane's sum says that it is left far
         // behind: the sums hold as well relative to any m near the maximum, so that
         // no maximum is formed in most tiles and the output seldom rescaled.
-        auto settle = [&](bf16x8 (&p0)[2], bf16x8 (&p1)[2], float sum) {
+        auto settle = [&](int u, uint32_t (&p)[8], float sum) {
             if (__any(!(sum < 0x1p16f))) {
                 float mx = kNone;
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e] * logit_scale(u, e));
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, logit(u, e, 0.f));
                 mx = fmaxf(half_max(mx), m);
                 const float f = fast_exp2(m - mx);
                 m = mx;
@@ -231,51 +251,79 @@ __global__ void __launch_bounds__(64 * WAVES, 8 / WAVES) chunk_kernel(ChunkArgs 
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) o[t][j] *= f;
-                sum = weights(0, p0) + weights(1, p1);
+                sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j] = pair(u, j, sum);
             }
             l += sum;
         };
-        auto output = [&](int u, const bf16x8 (&p)[2]) {
-#pragma unroll
-            for (int w = 0; w < 2; ++w)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    // V^T: dims 32 t + lane % 32, keys 32 u + 16 w + 4 half + {0..3, 8..11}
-                    typedef s16x4 __attribute__((address_space(3))) * lds4;
-                    u32x4 v;
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        // eight rows further the permutation differs by two chunks (d = 128 and 64)
-                        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (lds4)(vt[buf] + (32 * u + 16 * w + 8 * z) * 2 * D + (va ^ (64 * t + 32 * z))));
-                        const u32x2 y = __builtin_bit_cast(u32x2, x);
-                        v[2 * z] = y[0];
-                        v[2 * z + 1] = y[1];
-                    }
-                    o[t] = mfma32(__builtin_bit_cast(bf16x8, v), p[w], o[t]);
-                }
+        auto p_frag = [](const uint32_t (&p)[8], int w) {
+            return __builtin_bit_cast(bf16x8, (u32x4{p[4 * w], p[4 * w + 1], p[4 * w + 2], p[4 * w + 3]}));
         };
-        bf16x8 p0[2], p1[2];
-        logits(0);
-        mask(0);
-        logits(1);
-        mask(1);
-        const float sum0 = weights(0, p0), sum1 = weights(1, p1);
-        settle(p0, p1, sum0 + sum1);
-        output(0, p0);
-        output(1, p1);
+        const auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+
+        bf16x8 f[2 * N];
+        uint32_t p0[8], p1[8];
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) f[j] = k_frag(j);
+        scales(0);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j) {
+            fence();
+            if (j + AHEAD < 2 * N) f[j + AHEAD] = k_frag(j + AHEAD);
+            s[j / N] = mfma32(f[j], qf[j % N], s[j / N]);
+            if (j >= N) {
+#pragma unroll
+                for (int z = 0; z < PAIRS; ++z) p0[(j - N) * PAIRS + z] = pair(0, (j - N) * PAIRS + z, sum);
+            }
+        }
+        fence();
+        settle(0, p0, sum);
+        sum = 0.f;
+        scales(1);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) f[j] = v_frag(j);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            fence();
+            f[j + AHEAD] = v_frag(j + AHEAD);
+            o[j % NT] = mfma32(f[j], p_frag(p0, j / NT), o[j % NT]);
+#pragma unroll
+            for (int z = 0; z < PAIRS; ++z) p1[j * PAIRS + z] = pair(1, j * PAIRS + z, sum);
+        }
+        fence();
+        settle(1, p1, sum);
+#pragma unroll
+        for (int j = N; j < 2 * N; ++j) {
+            fence();
+            if (j + AHEAD < 2 * N) f[j + AHEAD] = v_frag(j + AHEAD);
+            o[j % NT] = mfma32(f[j], p_frag(p1, (j - N) / NT), o[j % NT]);
+            staging(j - N);
+        }
+        fence();
     };
 
     if (tile0 < tile1) {
         load(tile0);
-        store(tile0, 0);
+#pragma unroll
+        for (int z = 0; z < kPieces; ++z) store_piece(0, z);
+        clear_tail(tile0, 0);
     }
     __syncthreads();
     int buf = 0, tile = tile0;
     auto step = [&](auto masked) {
         if (tile + 1 < tile1) load(tile + 1);
-        attend(tile * kKeys, buf, masked);
-        if (tile + 1 < tile1) store(tile + 1, buf ^ 1);
+        // (behind the last tile the registers' old values, which nobody reads)
+        attend(tile * kKeys, buf, masked, [&](int j) {
+#pragma unroll
+            for (int z = j * kPieces / KC; z < (j + 1) * kPieces / KC; ++z) store_piece(buf ^ 1, z);
+        });
+        if (tile + 1 < tile1) clear_tail(tile + 1, buf ^ 1);
         __syncthreads();
         ++tile, buf ^= 1;
     };
@@ -323,7 +371,6 @@ __global__ void __launch_bounds__(64 * WAVES, 8 / WAVES) chunk_kernel(ChunkArgs 
 // their 32: with that order a lane's eight p are those of eight consecutive
 // keys, the ones that its transposing reads of V fetch.
 constexpr int kFewRows = 64;
-typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ floatx4 mfma16(bf16x8 a, bf16x8 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

@@ -24,6 +24,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
+constexpr int kRows = 32 * kWaves;         // query rows of a workgroup
 constexpr int kKeys = 64;                  // keys of a tile
 constexpr float kNone = -3e38f;            // running maximum before the first visible key
 
@@ -41,9 +42,6 @@ __device__ __forceinline__ float half_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Waves of a workgroup of many rows, 32 rows each.
-constexpr int tile_waves(int d) { return d == 64 ? 4 : 4; }
-
 // Bytes from the start of a staged tile to 16-byte chunk ch of row r.  Rows
 // without padding; the chunks of a row are permuted by its index, so that 16
 // consecutive rows of one chunk (the reads of K) and four rows of 64 bytes (the
@@ -54,14 +52,13 @@ __device__ __forceinline__ int staged(int r, int ch) {
     return r * (2 * D) + 16 * (ch ^ swz);
 }
 
-template <int D, int TYPE, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 8 / WAVES) chunk_kernel(ChunkArgs a) {
-    constexpr int kRows = 32 * WAVES;      // query rows of the workgroup
+template <int D, int TYPE>
+__global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     constexpr int KC = D / 16;             // 16-dim steps of S
     constexpr int NT = D / 32;             // 32-dim tiles of O
     constexpr int kRow = D * kCacheBytes<TYPE>;      // bytes of a cached row
     constexpr int kCh = kRow / 16;                   // its 16-byte chunks
-    constexpr int kWaveRows = kKeys / WAVES;         // rows of a tile that a wave stages
+    constexpr int kWaveRows = kKeys / kWaves;         // rows of a tile that a wave stages
     constexpr int kLoads = kWaveRows * kRow / 1024;  // its 16-byte loads of a lane of K (and of V)
     static_assert(kLoads >= 1, "whole load instructions");
     constexpr bool kScaled = TYPE == kCacheI8;       // scales applied to the logits and to p
@@ -797,16 +794,15 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
     *reinterpret_cast<u32x4*>(a.out + b * a.osb + h * a.osh + i * a.ost + 8 * lane) = v;
 }
 
-constexpr int64_t kTileRowsMost = 256 * 2 * kPlanCus;  // rows of the workgroups that fill the chip
-constexpr int kMaxSplits = 128;
+constexpr int kMaxSplits = 64;             // splits of a head's rows
+constexpr int64_t kTileBlocks = 4 * kPlanCus;   // workgroups of many rows, where there are splits
 
 template <int D, int TYPE>
 void attend(const ChunkArgs& a, hipStream_t s) {
     const unsigned heads = static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hkv);
     if (a.rows > kFewRows) {
-        constexpr int W = tile_waves(D);
-        const int tiles = (a.rows + 32 * W - 1) / (32 * W);
-        hipLaunchKernelGGL((chunk_kernel<D, TYPE, W>), dim3(heads, tiles, a.splits), dim3(64 * W), 0, s, a);
+        const int tiles = (a.rows + kRows - 1) / kRows;
+        hipLaunchKernelGGL((chunk_kernel<D, TYPE>), dim3(heads, tiles, a.splits), dim3(kThreads), 0, s, a);
         return;
     }
     const dim3 grid(heads, a.splits);
@@ -839,8 +835,7 @@ hipError_t launch(const ChunkArgs& a, hipStream_t s) {
 
 namespace {
 
-constexpr int kFewSplits = 64;             // splits of a head, few rows
-constexpr int kFewBlocks = 4 * kPlanCus;   // their workgroups, where there are splits
+constexpr int kFewBlocks = 4 * kPlanCus;   // workgroups of few rows, where there are splits
 
 // Splits for few rows.  A workgroup has a CU for itself, so that the launch
 // takes as many turns as there are workgroups per CU, each of its split's rounds
@@ -853,9 +848,31 @@ int few_splits(int64_t heads, int T, int keys) {
     const int64_t rounds = (T + 4 * keys - 1) / (4 * keys);
     int64_t best = 0;
     int best_s = 1;
-    for (int s = 1; s <= kFewSplits && s <= rounds && (s == 1 || s * heads <= kFewBlocks); ++s) {
+    for (int s = 1; s <= kMaxSplits && s <= rounds && (s == 1 || s * heads <= kFewBlocks); ++s) {
         const int64_t turns = (heads * s + kPlanCus - 1) / kPlanCus;
         const int64_t cost = turns * ((rounds + s - 1) / s + 2) + (s > 1 ? 3 : 0);
+        if (s == 1 || cost < best) best = cost, best_s = s;
+    }
+    return best_s;
+}
+
+// Splits for more rows.  In ns, as measured at d = 128 (64): a tile takes a
+// workgroup 1500 (950) with a CU to itself, 2000 (1250) beside another, which is
+// how they run from one per CU up to two; it begins within two tiles' time.  A
+// join reads and writes what the splits left (4 TB/s) beside 3000 for its launch.
+// (1024 queries of 28 heads on 4 over 8191 rows, 224 row tiles: 197 us with 1 split,
+// 142 with 2, 154 with 3; 512 of 32 on 8 over 4096, 128: 98 / 67 / 60 / 56 / 60 us
+// with 1 / 2 / 3 / 4 / 6; 1024 of 32 on 8 over 1024, 256: 31 with 1, 40 with 2.)
+int tile_splits(int64_t heads, int rows, int T, int d) {
+    const int64_t alone = d == 64 ? 950 : 1500, paired = d == 64 ? 1250 : 2000;
+    const int64_t base = heads * ((rows + kRows - 1) / kRows), tiles = (T + kKeys - 1) / kKeys;
+    int64_t best = 0;
+    int best_s = 1;
+    for (int s = 1; s <= kMaxSplits && s <= tiles && (s == 1 || base * s <= kTileBlocks); ++s) {
+        const int64_t n = base * s, rest = n % (2 * kPlanCus);
+        const int64_t turns = n / (2 * kPlanCus) * paired + (rest == 0 ? 0 : rest <= kPlanCus ? alone : paired);
+        const int64_t join = s > 1 ? 3000 + heads * rows * s * d * 3 / 1000 : 0;
+        const int64_t cost = turns * ((tiles + s - 1) / s + 2) + join;
         if (s == 1 || cost < best) best = cost, best_s = s;
     }
     return best_s;
@@ -865,24 +882,20 @@ int few_splits(int64_t heads, int T, int keys) {
 
 int chunk_splits(int64_t heads, int rows, int T, int d, int dtype) {
     if (rows <= kFewRows) return few_splits(heads, T, d == 128 && dtype == kCacheBf16 ? 32 : 64);
-    const int wg_rows = 32 * tile_waves(d);
-    const int64_t base = heads * ((rows + wg_rows - 1) / wg_rows);
-    const int64_t want = 2 * kPlanCus / base, most = (T + 255) / 256;
-    const int64_t s = want < 1 ? 1 : want < most ? want : most;
-    return static_cast<int>(s < kMaxSplits ? s : kMaxSplits);
+    return tile_splits(heads, rows, T, d);
 }
 
 size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d) {
     // rows of partial sums: splits * heads * rows.  Few rows: kFewBlocks
     // workgroups at most, a split for every 128 keys at most ...
-    const int64_t few_s = T / 128 + 1 < kFewSplits ? T / 128 + 1 : kFewSplits;
+    const int64_t few_s = T / 128 + 1 < kMaxSplits ? T / 128 + 1 : kMaxSplits;
     const int64_t few_b = heads > kFewBlocks / few_s ? kFewBlocks : heads * few_s;
     int64_t part = few_b * (rows < kFewRows ? rows : kFewRows);
-    // ... more rows: where there are splits, they fill the chip once
+    // ... more rows: kTileBlocks workgroups of kRows at most
     if (rows > kFewRows) {
-        const int64_t most = T / 256 + 1 < kMaxSplits ? T / 256 + 1 : kMaxSplits;
+        const int64_t most = T / kKeys + 1 < kMaxSplits ? T / kKeys + 1 : kMaxSplits;
         int64_t tile = heads * rows;
-        tile = tile > kTileRowsMost / most ? kTileRowsMost : tile * most;
+        tile = tile > kTileBlocks * kRows / most ? kTileBlocks * kRows : tile * most;
         if (tile > part) part = tile;
     }
     return static_cast<size_t>(part) * (d * sizeof(float) + sizeof(float2)) + 256;

@@ -174,9 +174,10 @@ def _dev(t: torch.Tensor) -> torch.device:
 
 
 def _strides4(t: torch.Tensor) -> Strides:
-    if t.dim() != 4 or t.stride(3) != 1:
+    st = t.stride()
+    if len(st) != 4 or st[3] != 1:
         raise ValueError("expected a [batch, head, token, d] tensor with contiguous d")
-    return Strides(t.stride(0), t.stride(1), t.stride(2))
+    return Strides(st[0], st[1], st[2])
 
 
 def _public_stream(index: int) -> int:
@@ -636,37 +637,40 @@ class PagedCache:
         return cls(k, v, ks, vs, torch.arange(B * per, dtype=torch.int32, device=device).view(B, per))
 
     def c_pages(self) -> Pages:
-        k, v, table = self.k, self.v, self.table
-        if k.dtype not in _CACHE_DTYPES:
-            raise TypeError("expected bfloat16, float8_e4m3fn or int8 pages, got %s" % k.dtype)
-        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or not k.is_contiguous() \
-                or not v.is_contiguous():
+        k, v, ks, vs, table = self.k, self.v, self.k_scale, self.v_scale, self.table
+        dtype, shape = k.dtype, k.shape
+        code = _CACHE_DTYPES.get(dtype)
+        if code is None:
+            raise TypeError("expected bfloat16, float8_e4m3fn or int8 pages, got %s" % dtype)
+        if len(shape) != 4 or v.shape != shape or v.dtype != dtype or not (k.is_contiguous() and v.is_contiguous()):
             raise ValueError("k and v pages must be contiguous [n_pages, Hkv, page, d] of one dtype")
         if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
             raise ValueError("the table must be a contiguous int32 [B, max_pages] tensor")
-        if k.dtype != torch.bfloat16:
-            for s in (self.k_scale, self.v_scale):
-                if s is None or s.dtype != torch.float32 or s.shape != k.shape[:3] or not s.is_contiguous():
-                    raise ValueError("8-bit pages need contiguous fp32 scales [n_pages, Hkv, page]")
-                _same_device(k, s)
         _same_device(k, v, table)
-        return Pages(_p(k), _p(v), _p(self.k_scale), _p(self.v_scale), _p(table), k.shape[0], k.shape[2],
-                     table.shape[1], _CACHE_DTYPES[k.dtype])
+        if code == MMSKV_BF16:
+            ks = vs = None
+        else:
+            rows = shape[:3]
+            for s in (ks, vs):
+                if s is None or s.dtype != torch.float32 or s.shape != rows or not s.is_contiguous():
+                    raise ValueError("8-bit pages need contiguous fp32 scales [n_pages, Hkv, page]")
+            _same_device(k, ks, vs)
+        return Pages(k.data_ptr(), v.data_ptr(), _p(ks), _p(vs), table.data_ptr(), shape[0], shape[2],
+                     table.shape[1], code)
 
 
 def _same_device(t, *others):
-    dev = _dev(t)
+    i = t.get_device()                 # (-1: host)
     for o in others:
-        if o is not None and o.device != dev:
-            raise ValueError("tensors on different devices (%s, %s)" % (dev, o.device))
-    return dev
+        if o is not None and o.get_device() != i:
+            raise ValueError("tensors on different devices (%s, %s)" % (t.device, o.device))
+    return _dev(t)
 
 
 def _int32(t, shape, what):
-    """A list of row numbers as the library takes it: contiguous int32 of that shape."""
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
+    """Row numbers as the library takes them: contiguous int32 of that shape, or None."""
+    if t is not None and (t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous()):
         raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (what, shape))
-    return t
 
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor | None = None,

@@ -395,12 +395,48 @@ struct FewTile {
     static constexpr int kGroups = kKeys / 16;                  // 16-row groups, each on one page
     static constexpr int kAll = 2 * kLoads + (kScaled ? 2 : 0);
     static constexpr int kStage = 2 * kTile + (kScaled ? 2 * kKeys * 4 : 0);
-    // byte of 16-byte chunk ch of row r (chunks permuted against bank conflicts)
+    // Byte of 16-byte chunk ch of row r.  The chunks of a row are permuted by those
+    // bits of r that differ between the lanes of a read (0, 1, 3 and 4), so that the
+    // reads spread over all banks and rows 4 or 32 apart are a constant apart.
     static __device__ __forceinline__ int swz(int r) {
-        return kCh == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : kCh == 8 ? ((r >> 1) ^ (r >> 3)) & 7 : ((r >> 2) ^ (r >> 4)) & 3;
+        return kCh == 16 ? ((r & 3) << 2) | ((r >> 3) & 3)
+                         : kCh == 8 ? ((r >> 1) & 1) | (((r >> 3) & 3) << 1) : (r >> 3) & 3;
     }
     static __device__ __forceinline__ int at(int r, int ch) { return r * kRow + 16 * (ch ^ swz(r)); }
 };
+
+// Offsets of eight reads of a stage's K, V and scales.
+template <class T, int STAGE, int U0, int KC>
+struct KOffsets {                          // 16-key tiles U0 + z / KC
+    static constexpr int at(int z) {
+        const int u = U0 + z / KC;
+        return STAGE * T::kStage + (32 * (u >> 1) + 4 * (u & 1)) * T::kRow;
+    }
+};
+template <class T, int STAGE>
+struct ScaleOffsets {                      // four of K, four of V: keys 32 (z / 2 % 2) + 4 (z % 2)
+    static constexpr int at(int z) {
+        return STAGE * T::kStage + 2 * T::kTile + z / 4 * T::kKeys * 4 + 4 * (32 * (z / 2 % 2) + 4 * (z % 2));
+    }
+};
+template <class T, int STAGE, int U0>
+struct VOffsets {                          // 8-bit: 32-key steps z % (NS / 2); bf16: step U0, keys 4 (z % 2) ..
+    static constexpr int at(int z) {
+        const int row = T::kScaled ? 32 * (z % (T::kKeys / 32)) : 32 * U0 + 4 * (z & 1);
+        return STAGE * T::kStage + T::kTile + row * T::kRow;
+    }
+};
+
+// The load instructions J .. LOADS - 1 of a 16-row group from src (its first row;
+// 1 KB of zeros where `any` is not set) to dst; row0: its first row in the tile.
+template <class T, int J, int LOADS>
+__device__ __forceinline__ void load_group(const char* src, char* dst, int row0, int ld_row, int lane, bool any) {
+    const int r = row0 + J * T::kPer + ld_row;
+    const int off = ld_row * T::kRow + 16 * ((lane % T::kCh) ^ T::swz(r));
+    // (the offset of an instruction is added to both of its addresses)
+    load16_to_lds<1024 * J>(src + off - (any ? 0 : 1024 * J), dst);
+    if constexpr (J + 1 < LOADS) load_group<T, J + 1, LOADS>(src, dst, row0, ld_row, lane, any);
+}
 
 // Workgroup: 4 waves; (b, c) and a split of its keys.
 template <int D, int TYPE, int NR>
@@ -428,10 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
     const int tiles = (end + T::kKeys - 1) / T::kKeys, per = (tiles + a.splits - 1) / a.splits;
     const int tile0 = split * per + wave, tile1 = min(split * per + per, tiles);
 
-    // lane's part of a load: row lane / kCh of kPer, chunk lane % kCh of the staged order
-    const int ld_row = lane / T::kCh;
-    // pages of the 16-row groups of a tile (-1: none), by scalar loads, whose
-    // waits are not those of the loads to LDS
+    // pages of the 16-row groups of a tile (-1: none)
     struct Ids {
         int id[T::kGroups];
     };
@@ -441,27 +474,28 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
         for (int g = 0; g < T::kGroups; ++g) ids.id[g] = uniform_page(a.pages, b, tile * T::kKeys + 16 * g);
         return ids;
     };
+    // A load instruction fetches 1 KB, kPer rows of a group; a lane's bytes of it are
+    // those of the chunk that its place in the staged order stands for.
+    constexpr int kGroupLoads = 16 / T::kPer;
+    const int ld_row = lane / T::kCh;
     auto load_stage = [&](int tile, int stage, const Ids& ids) {
         char* dst = base + stage * T::kStage;
         const int t0 = tile * T::kKeys;
+        const char* none = reinterpret_cast<const char*>(kNoRows);
 #pragma unroll
-        for (int j = 0; j < T::kLoads; ++j) {
-            const int r = j * T::kPer;     // uniform; its kPer rows are on one page
-            const int id = ids.id[r / 16];
-            const int rr = r + ld_row;
-            const int off = ld_row * T::kRow + 16 * ((lane % T::kCh) ^ T::swz(rr));
-            const int64_t e = pool_row(a.pages, a.Hkv, c, id, t0 + r) * T::kRow;
-            const char* ks = id >= 0 ? static_cast<const char*>(a.pages.k) + e : reinterpret_cast<const char*>(kNoRows);
-            const char* vs = id >= 0 ? static_cast<const char*>(a.pages.v) + e : reinterpret_cast<const char*>(kNoRows);
-            load16_to_lds(ks + off, dst + j * 1024);
-            load16_to_lds(vs + off, dst + T::kTile + j * 1024);
+        for (int g = 0; g < T::kGroups; ++g) {
+            const bool any = ids.id[g] >= 0;
+            const int64_t e = pool_row(a.pages, a.Hkv, c, ids.id[g], t0 + 16 * g) * T::kRow;
+            const char* ks = any ? static_cast<const char*>(a.pages.k) + e : none;
+            const char* vs = any ? static_cast<const char*>(a.pages.v) + e : none;
+            load_group<T, 0, kGroupLoads>(ks, dst + g * 16 * T::kRow, 16 * g, ld_row, lane, any);
+            load_group<T, 0, kGroupLoads>(vs, dst + T::kTile + g * 16 * T::kRow, 16 * g, ld_row, lane, any);
         }
         if constexpr (T::kScaled) {        // kKeys is 64: a lane has the scales of one row
             const int g = lane / 16;
             const int id = g == 0 ? ids.id[0] : g == 1 ? ids.id[T::kGroups > 1 ? 1 : 0] : g == 2 ? ids.id[T::kGroups > 2 ? 2 : 0]
                                                                                             : ids.id[T::kGroups - 1];
             const int64_t pr = pool_row(a.pages, a.Hkv, c, id, t0 + lane);
-            const char* none = reinterpret_cast<const char*>(kNoRows);
             load4_to_lds(id >= 0 ? reinterpret_cast<const char*>(a.pages.k_scale + pr) : none, dst + 2 * T::kTile);
             load4_to_lds(id >= 0 ? reinterpret_cast<const char*>(a.pages.v_scale + pr) : none, dst + 2 * T::kTile + 256);
         }
@@ -521,22 +555,36 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
         for (int kc = 0; kc < KC; ++kc) qf[x][kc] = __builtin_bit_cast(bf16x8, w[kc]);
     }
 
-    int stage = 0;
-    for (int tile = tile0; tile < tile1; tile += kWaves, stage ^= 1) {
+    // a lane's places in a stage: of K, one for each 32-dim step; of V, for each
+    // 16-dim tile; of the scales
+    uint32_t k_at[KC], v_at[NT];
+    const uint32_t s_at = lds_address(base) + 32 * quarter;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+        const int row = 8 * ((lane & 15) >> 2) + (lane & 3);
+        k_at[kc] = lds_address(base) + (T::kScaled ? T::at(row, 2 * kc + (quarter >> 1)) + 8 * (quarter & 1)
+                                                   : T::at(row, 4 * kc + quarter));
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+        v_at[t] = lds_address(base) + 8 * (lane & 1) +
+                  (T::kScaled ? T::at(8 * quarter + ((lane & 15) >> 1), t)
+                              : T::at(8 * quarter + ((lane & 15) >> 2), 2 * t + ((lane >> 1) & 1)));
+
+    auto step = [&](int tile, auto which, bool first) {
+        constexpr int STAGE = decltype(which)::value;
         if (tile + kWaves < tile1) wait_vm<T::kAll>();     // all but the next stage
         else wait_vm<0>();
         __builtin_amdgcn_sched_barrier(0);
         ids = pages_of(tile + 2 * kWaves);
-        char* const kt = base + stage * T::kStage;
-        char* const vt = kt + T::kTile;
-        float* const ksc = reinterpret_cast<float*>(vt + T::kTile);
-        float* const vsc = ksc + T::kKeys;
         const int key0 = tile * T::kKeys;
         if (key0 + T::kKeys > end) {
             // rows behind the last key may hold anything: zeros, with zero scales
+            char* const vt = base + STAGE * T::kStage + T::kTile;
+            float* const sc = reinterpret_cast<float*>(vt + T::kTile);
             for (int i = lane; i < T::kKeys * T::kCh; i += kWave)
                 if (key0 + i / T::kCh >= end) *reinterpret_cast<u32x4*>(vt + i * 16) = u32x4{0u, 0u, 0u, 0u};
-            if (T::kScaled && key0 + lane >= end) ksc[lane] = 0.f, vsc[lane] = 0.f;
+            if (T::kScaled && key0 + lane >= end) sc[lane] = 0.f, sc[T::kKeys + lane] = 0.f;
         }
         // value e of s[x][u] is key key0 + 32 (u / 2) + 8 quarter + 4 (u % 2) + e
         floatx4 s[NR][NS];
@@ -545,20 +593,15 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
 #pragma unroll
             for (int x = 0; x < NR; ++x) s[x][u] = floatx4{0.f, 0.f, 0.f, 0.f};
         constexpr int UB = 8 / KC;         // 16-key tiles of eight reads
-#pragma unroll
-        for (int u0 = 0; u0 < NS; u0 += UB) {
+        auto logits = [&](auto first_tile) {
+            constexpr int U0 = decltype(first_tile)::value;
             uint32_t at[8];
             bf16x8 k[8];
 #pragma unroll
-            for (int z = 0; z < 8; ++z) {
-                const int u = u0 + z / KC, kc = z % KC;
-                const int row = 32 * (u >> 1) + 8 * ((lane & 15) >> 2) + 4 * (u & 1) + (lane & 3);
-                at[z] = lds_address(kt) + (T::kScaled ? T::at(row, 2 * kc + (quarter >> 1)) + 8 * (quarter & 1)
-                                                      : T::at(row, 4 * kc + quarter));
-            }
+            for (int z = 0; z < 8; ++z) at[z] = k_at[z % KC];
             if constexpr (T::kScaled) {
                 u32x2 w[8];
-                read64(at, w);
+                read64<KOffsets<T, STAGE, U0, KC>>(at, w);
 #pragma unroll
                 for (int z = 0; z < 8; ++z) {
                     const u32x2 y0 = widen4<TYPE>(w[z][0]), y1 = widen4<TYPE>(w[z][1]);
@@ -566,106 +609,138 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
                 }
             } else {
                 u32x4 w[8];
-                read128(at, w);
+                read128<KOffsets<T, STAGE, U0, KC>>(at, w);
 #pragma unroll
                 for (int z = 0; z < 8; ++z) k[z] = __builtin_bit_cast(bf16x8, w[z]);
             }
 #pragma unroll
             for (int z = 0; z < 8; ++z)
 #pragma unroll
-                for (int x = 0; x < NR; ++x) s[x][u0 + z / KC] = mfma16(k[z], qf[x][z % KC], s[x][u0 + z / KC]);
-        }
-        floatx4 kw[NS], vw[NS];
+                for (int x = 0; x < NR; ++x) s[x][U0 + z / KC] = mfma16(k[z], qf[x][z % KC], s[x][U0 + z / KC]);
+        };
+        logits(CacheType<0>{});
+        if constexpr (UB < NS) logits(CacheType<UB < NS ? UB : 0>{});
+        static_assert(2 * UB >= NS, "two blocks of reads");
+        floatx4 vw[NS];                    // scales of the keys' V
         if constexpr (T::kScaled) {
             static_assert(!T::kScaled || NS == 4, "eight reads of four scales");
             uint32_t at[8];
             u32x4 w[8];
 #pragma unroll
-            for (int z = 0; z < 8; ++z)
-                at[z] = lds_address(z < 4 ? ksc : vsc) + 4 * (32 * ((z & 3) >> 1) + 8 * quarter + 4 * (z & 1));
-            read128(at, w);
+            for (int z = 0; z < 8; ++z) at[z] = s_at;
+            read128<ScaleOffsets<T, STAGE>>(at, w);
 #pragma unroll
             for (int u = 0; u < NS; ++u) {
-                kw[u] = __builtin_bit_cast(floatx4, w[u]) * a.scale;
                 vw[u] = __builtin_bit_cast(floatx4, w[4 + u]);
+#pragma unroll
+                for (int x = 0; x < NR; ++x) s[x][u] *= __builtin_bit_cast(floatx4, w[u]);
             }
         }
-        const bool whole = key0 + T::kKeys <= all_see;
+        if (key0 + T::kKeys > all_see) {
+            asm volatile("");              // (a branch: few tiles come here)
+#pragma unroll
+            for (int x = 0; x < NR; ++x) {
+                const int rel = last[x] - key0 - 8 * quarter;
+#pragma unroll
+                for (int u = 0; u < NS; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s[x][u][e] = 32 * (u >> 1) + 4 * (u & 1) + e <= rel ? s[x][u][e] : -INFINITY;
+            }
+        }
         bf16x8 p[NR][NS / 2];
+        float sum[NR];
+        auto weights = [&]() {
 #pragma unroll
-        for (int x = 0; x < NR; ++x) {
-            float mx = kNone;
+            for (int x = 0; x < NR; ++x) {
+                sum[x] = 0.f;
 #pragma unroll
-            for (int u = 0; u < NS; ++u)
+                for (int u = 0; u < NS; u += 2) {
+                    u32x4 y;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float y = s[x][u][e] * (T::kScaled ? kw[u][e] : a.scale);
-                    if (!whole) y = key0 + 32 * (u >> 1) + 8 * quarter + 4 * (u & 1) + e <= last[x] ? y : -INFINITY;
-                    s[x][u][e] = y;
-                    mx = fmaxf(mx, y);
+                    for (int j = 0; j < 4; ++j) {
+                        const int z = u + (j >> 1), e = 2 * (j & 1);
+                        float p0 = fast_exp2(fmaf(s[x][z][e], a.scale, -m[x]));
+                        float p1 = fast_exp2(fmaf(s[x][z][e + 1], a.scale, -m[x]));
+                        sum[x] += p0 + p1;
+                        if (T::kScaled) p0 *= vw[z][e], p1 *= vw[z][e + 1];
+                        y[j] = pack_bf16(p0, p1);
+                    }
+                    p[x][u / 2] = __builtin_bit_cast(bf16x8, y);
                 }
-            mx = fmaxf(quarter_max(mx), m[x]);
-            const float f = fast_exp2(m[x] - mx);
-            m[x] = mx;
-            float sum = 0.f;
-#pragma unroll
-            for (int u = 0; u < NS; u += 2) {
-                u32x4 y;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int z = u + (j >> 1), e = 2 * (j & 1);
-                    float p0 = fast_exp2(s[x][z][e] - mx), p1 = fast_exp2(s[x][z][e + 1] - mx);
-                    sum += p0 + p1;
-                    if (T::kScaled) p0 *= vw[z][e], p1 *= vw[z][e + 1];
-                    y[j] = pack_bf16(p0, p1);
-                }
-                p[x][u / 2] = __builtin_bit_cast(bf16x8, y);
             }
-            l[x] = fmaf(l[x], f, sum);
+        };
+        // the reference m moves only where it is left far behind, as above
+        bool behind = first;
+        if (!first) {
+            weights();
+            float most = sum[0];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) o[x][t] *= f;
+            for (int x = 1; x < NR; ++x) most = sum[x] < 0x1p16f ? most : sum[x];
+            behind = __any(!(most < 0x1p16f));
         }
-        // V^T: dims 16 t + lane % 16, keys 32 u + 8 quarter + 0 .. 7
-        // eight reads: four tiles t of one 32-key step (bf16: two reads each), or of both
+        if (behind) {
+#pragma unroll
+            for (int x = 0; x < NR; ++x) {
+                float mx = s[x][0][0];
+#pragma unroll
+                for (int u = 0; u < NS; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][u][e]);
+                mx = fmaxf(quarter_max(mx) * a.scale, m[x]);
+                const float f = fast_exp2(m[x] - mx);
+                m[x] = mx;
+                l[x] *= f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) o[x][t] *= f;
+            }
+            weights();
+        }
+#pragma unroll
+        for (int x = 0; x < NR; ++x) l[x] += sum[x];
+        // V^T: dims 16 t + lane % 16, keys 32 u + 8 quarter + 0 .. 7; eight reads: four
+        // tiles t of one 32-key step (bf16: two reads each), or of both
         constexpr int TB = T::kScaled ? 8 / (NS / 2) : 4;
-        constexpr int UV = T::kScaled ? NS / 2 : 1;
+        auto output = [&](auto first_tile, auto key_step) {
+            constexpr int T0 = decltype(first_tile)::value, U0 = decltype(key_step)::value;
+            uint32_t at[8];
+            u32x2 w[8];
 #pragma unroll
-        for (int t0 = 0; t0 < NT; t0 += TB)
-#pragma unroll
-            for (int u0 = 0; u0 < NS / 2; u0 += UV) {
-                uint32_t at[8];
-                u32x2 w[8];
+            for (int z = 0; z < 8; ++z) at[z] = v_at[T0 + z * TB / 8];
+            if constexpr (T::kScaled) {
+                read_transposed8<VOffsets<T, STAGE, U0>>(at, w);
 #pragma unroll
                 for (int z = 0; z < 8; ++z) {
-                    const int t = t0 + z / 2, u = u0 + (T::kScaled ? z & 1 : 0);
-                    at[z] = lds_address(vt) + 8 * (lane & 1) +
-                            (T::kScaled ? T::at(32 * u + 8 * quarter + ((lane & 15) >> 1), t)
-                                        : T::at(32 * u + 8 * quarter + 4 * (z & 1) + ((lane & 15) >> 2),
-                                                2 * t + ((lane >> 1) & 1)));
+                    const u32x2 y0 = widen4<TYPE>(w[z][0]), y1 = widen4<TYPE>(w[z][1]);
+                    const bf16x8 v = __builtin_bit_cast(bf16x8, (u32x4{y0[0], y0[1], y1[0], y1[1]}));
+                    const int t = T0 + z * TB / 8, u = z % (NS / 2);
+#pragma unroll
+                    for (int x = 0; x < NR; ++x) o[x][t] = mfma16(v, p[x][u], o[x][t]);
                 }
-                if constexpr (T::kScaled) {
-                    read_transposed8(at, w);
+            } else {
+                read_transposed16<VOffsets<T, STAGE, U0>>(at, w);
 #pragma unroll
-                    for (int z = 0; z < 8; ++z) {
-                        const u32x2 y0 = widen4<TYPE>(w[z][0]), y1 = widen4<TYPE>(w[z][1]);
-                        const bf16x8 v = __builtin_bit_cast(bf16x8, (u32x4{y0[0], y0[1], y1[0], y1[1]}));
+                for (int z = 0; z < 4; ++z) {
+                    const bf16x8 v = __builtin_bit_cast(bf16x8, (u32x4{w[2 * z][0], w[2 * z][1], w[2 * z + 1][0],
+                                                                      w[2 * z + 1][1]}));
 #pragma unroll
-                        for (int x = 0; x < NR; ++x) o[x][t0 + z / 2] = mfma16(v, p[x][z & 1], o[x][t0 + z / 2]);
-                    }
-                } else {
-                    read_transposed16(at, w);
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) {
-                        const bf16x8 v = __builtin_bit_cast(bf16x8, (u32x4{w[2 * z][0], w[2 * z][1], w[2 * z + 1][0],
-                                                                          w[2 * z + 1][1]}));
-#pragma unroll
-                        for (int x = 0; x < NR; ++x) o[x][t0 + z] = mfma16(v, p[x][u0], o[x][t0 + z]);
-                    }
+                    for (int x = 0; x < NR; ++x) o[x][T0 + z] = mfma16(v, p[x][U0], o[x][T0 + z]);
                 }
             }
+        };
+        constexpr int US = T::kScaled ? 1 : NS / 2;        // blocks of reads per TB tiles
+        static_assert(NT <= 2 * TB && US <= 2, "two by two blocks of reads");
+        output(CacheType<0>{}, CacheType<0>{});
+        if constexpr (US > 1) output(CacheType<0>{}, CacheType<1>{});
+        if constexpr (NT > TB) output(CacheType<NT - TB>{}, CacheType<0>{});
+        if constexpr (NT > TB && US > 1) output(CacheType<NT - TB>{}, CacheType<1>{});
         __builtin_amdgcn_sched_barrier(0);
         // this stage has been read: the one after the next into its place
-        if (tile + 2 * kWaves < tile1) load_stage(tile + 2 * kWaves, stage, ids);
+        if (tile + 2 * kWaves < tile1) load_stage(tile + 2 * kWaves, STAGE, ids);
+    };
+    for (int tile = tile0; tile < tile1; tile += 2 * kWaves) {
+        step(tile, CacheType<0>{}, tile == tile0);
+        if (tile + kWaves < tile1) step(tile + kWaves, CacheType<1>{}, false);
     }
 
     // join the waves: value e of o[x][t] is dim 16 t + 4 quarter + e of row 16 x + lane % 16

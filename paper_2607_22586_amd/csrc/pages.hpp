@@ -33,9 +33,11 @@ __device__ __forceinline__ int page_of(const Pages& p, int b, int t) {
 // load instruction of a wave fetches.
 __device__ __attribute__((aligned(16))) const unsigned char kNoRows[1024] = {};
 
-// 16 / 4 bytes per lane from memory to LDS (dst + 16 / 4 * lane)
+// 16 / 4 bytes per lane from memory to LDS (dst + 16 / 4 * lane); OFF is added
+// to both addresses.
+template <int OFF = 0>
 __device__ __forceinline__ void load16_to_lds(const char* src, char* dst) {
-    __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, OFF, 0);
 }
 __device__ __forceinline__ void load4_to_lds(const char* src, char* dst) {
     __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
@@ -53,10 +55,39 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
 }
 
-// LDS reads of a wave's staged tiles, several at a time with their wait.  As
-// plain reads or builtins they would wait for every load to LDS that is under
-// way, the later stages' among them: the compiler does not see which bytes those
-// write.  What they read has been waited for (wait_vm) before.
+// LDS reads of a wave's staged tiles, several at a time with their wait, from
+// LDS address at[i] + OFF::at(i).  As plain reads or builtins they would wait for every
+// load to LDS that is under way, the later stages' among them: the compiler does
+// not see which bytes those write.  What they read has been waited for before.
+template <class OFF>
+__device__ __forceinline__ void read128(const uint32_t (&at)[8], u32x4 (&x)[8]) {
+    asm volatile("ds_read_b128 %0, %8 offset:%16\n\tds_read_b128 %1, %9 offset:%17\n\t"
+                 "ds_read_b128 %2, %10 offset:%18\n\tds_read_b128 %3, %11 offset:%19\n\t"
+                 "ds_read_b128 %4, %12 offset:%20\n\tds_read_b128 %5, %13 offset:%21\n\t"
+                 "ds_read_b128 %6, %14 offset:%22\n\tds_read_b128 %7, %15 offset:%23\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
+                   "=&v"(x[7])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]),
+                   "v"(at[7]), "n"(OFF::at(0)), "n"(OFF::at(1)), "n"(OFF::at(2)), "n"(OFF::at(3)), "n"(OFF::at(4)),
+                   "n"(OFF::at(5)), "n"(OFF::at(6)), "n"(OFF::at(7))
+                 : "memory");
+}
+template <class OFF>
+__device__ __forceinline__ void read64(const uint32_t (&at)[8], u32x2 (&x)[8]) {
+    asm volatile("ds_read_b64 %0, %8 offset:%16\n\tds_read_b64 %1, %9 offset:%17\n\t"
+                 "ds_read_b64 %2, %10 offset:%18\n\tds_read_b64 %3, %11 offset:%19\n\t"
+                 "ds_read_b64 %4, %12 offset:%20\n\tds_read_b64 %5, %13 offset:%21\n\t"
+                 "ds_read_b64 %6, %14 offset:%22\n\tds_read_b64 %7, %15 offset:%23\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
+                   "=&v"(x[7])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]),
+                   "v"(at[7]), "n"(OFF::at(0)), "n"(OFF::at(1)), "n"(OFF::at(2)), "n"(OFF::at(3)), "n"(OFF::at(4)),
+                   "n"(OFF::at(5)), "n"(OFF::at(6)), "n"(OFF::at(7))
+                 : "memory");
+}
+// (two or four, at offset 0)
 __device__ __forceinline__ void read128(const uint32_t (&at)[2], u32x4 (&x)[2]) {
     asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)"
                  : "=&v"(x[0]), "=&v"(x[1])
@@ -70,44 +101,35 @@ __device__ __forceinline__ void read128(const uint32_t (&at)[4], u32x4 (&x)[4]) 
                  : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
                  : "memory");
 }
-__device__ __forceinline__ void read128(const uint32_t (&at)[8], u32x4 (&x)[8]) {
-    asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\t"
-                 "ds_read_b128 %3, %11\n\tds_read_b128 %4, %12\n\tds_read_b128 %5, %13\n\t"
-                 "ds_read_b128 %6, %14\n\tds_read_b128 %7, %15\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
-               "=&v"(x[7])
-                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
-                 : "memory");
-}
-__device__ __forceinline__ void read64(const uint32_t (&at)[8], u32x2 (&x)[8]) {
-    asm volatile("ds_read_b64 %0, %8\n\tds_read_b64 %1, %9\n\tds_read_b64 %2, %10\n\t"
-                 "ds_read_b64 %3, %11\n\tds_read_b64 %4, %12\n\tds_read_b64 %5, %13\n\t"
-                 "ds_read_b64 %6, %14\n\tds_read_b64 %7, %15\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
-               "=&v"(x[7])
-                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
-                 : "memory");
-}
 // Transposing reads.  16-bit: the 16 lanes of a group name four rows of 16
 // columns (lane: row lane / 4, columns 4 (lane % 4) ..) and get column lane % 16
 // of them; 8-bit: eight rows of 16 columns (row lane / 2, columns 8 (lane % 2) ..).
+template <class OFF>
 __device__ __forceinline__ void read_transposed16(const uint32_t (&at)[8], u32x2 (&x)[8]) {
-    asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\tds_read_b64_tr_b16 %2, %10\n\t"
-                 "ds_read_b64_tr_b16 %3, %11\n\tds_read_b64_tr_b16 %4, %12\n\t"
-                 "ds_read_b64_tr_b16 %5, %13\n\tds_read_b64_tr_b16 %6, %14\n\t"
-                 "ds_read_b64_tr_b16 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %2, %10 offset:%18\n\tds_read_b64_tr_b16 %3, %11 offset:%19\n\t"
+                 "ds_read_b64_tr_b16 %4, %12 offset:%20\n\tds_read_b64_tr_b16 %5, %13 offset:%21\n\t"
+                 "ds_read_b64_tr_b16 %6, %14 offset:%22\n\tds_read_b64_tr_b16 %7, %15 offset:%23\n\t"
+                 "s_waitcnt lgkmcnt(0)"
                  : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
-               "=&v"(x[7])
-                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
+                   "=&v"(x[7])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]),
+                   "v"(at[7]), "n"(OFF::at(0)), "n"(OFF::at(1)), "n"(OFF::at(2)), "n"(OFF::at(3)), "n"(OFF::at(4)),
+                   "n"(OFF::at(5)), "n"(OFF::at(6)), "n"(OFF::at(7))
                  : "memory");
 }
+template <class OFF>
 __device__ __forceinline__ void read_transposed8(const uint32_t (&at)[8], u32x2 (&x)[8]) {
-    asm volatile("ds_read_b64_tr_b8 %0, %8\n\tds_read_b64_tr_b8 %1, %9\n\tds_read_b64_tr_b8 %2, %10\n\t"
-                 "ds_read_b64_tr_b8 %3, %11\n\tds_read_b64_tr_b8 %4, %12\n\tds_read_b64_tr_b8 %5, %13\n\t"
-                 "ds_read_b64_tr_b8 %6, %14\n\tds_read_b64_tr_b8 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+    asm volatile("ds_read_b64_tr_b8 %0, %8 offset:%16\n\tds_read_b64_tr_b8 %1, %9 offset:%17\n\t"
+                 "ds_read_b64_tr_b8 %2, %10 offset:%18\n\tds_read_b64_tr_b8 %3, %11 offset:%19\n\t"
+                 "ds_read_b64_tr_b8 %4, %12 offset:%20\n\tds_read_b64_tr_b8 %5, %13 offset:%21\n\t"
+                 "ds_read_b64_tr_b8 %6, %14 offset:%22\n\tds_read_b64_tr_b8 %7, %15 offset:%23\n\t"
+                 "s_waitcnt lgkmcnt(0)"
                  : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]),
-               "=&v"(x[7])
-                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
+                   "=&v"(x[7])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]),
+                   "v"(at[7]), "n"(OFF::at(0)), "n"(OFF::at(1)), "n"(OFF::at(2)), "n"(OFF::at(3)), "n"(OFF::at(4)),
+                   "n"(OFF::at(5)), "n"(OFF::at(6)), "n"(OFF::at(7))
                  : "memory");
 }
 

@@ -912,20 +912,27 @@ namespace {
 
 constexpr int kFewBlocks = 4 * kPlanCus;   // workgroups of few rows, where there are splits
 
-// Splits for few rows.  A workgroup has a CU for itself, so that the launch
-// takes as many turns as there are workgroups per CU, each of its split's rounds
-// (a tile for each of the four waves) and about two rounds' time to begin; a join
-// costs about three.  (28 heads on 4, d = 128, bf16: of 1 / 6 / 12 / 64 splits one
-// is best at 384 rows, 7.2 us, six at 700, 8.2 against 10.5, twelve at 1100, 8.7
-// against 13.6, 64 at 16384, 14.7 against 138; for 16 sequences of 16384 rows
-// four, 98.4 against 105 with 6 and 167 with 1.)
-int few_splits(int64_t heads, int T, int keys) {
+// Splits for few rows.  A workgroup has a CU for itself, so that the launch takes
+// as many turns as there are workgroups per CU, each of them 2 us and the rounds
+// of its split (a tile for each of the four waves); a join reads and writes what
+// the splits left beside 3 us for its launch.  (What memory takes for the keys is
+// the same for any number.)  A round takes one workgroup, at d = 128 and 16 rows, 0.75 us for 128
+// bf16 rows, 1.6 for 256 e4m3 and 2.0 for 256 int8 ones, and more with more tiles
+// of 16 rows.  (28 heads on 4, d = 128, bf16, 1 / 6 / 12 / 64 splits: one is best at
+// 384 rows, six at 700, twelve at 1100, 64 at 16384, 14.7 us against 138; for 16
+// sequences of 16384 rows four, 98 against 105 with 6 and 167 with 1.)
+int few_splits(int64_t heads, int rows, int T, int d, int dtype) {
+    const int keys = d == 128 && dtype == kCacheBf16 ? 32 : 64;
+    const int nr = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const int64_t round = d == 128 ? (dtype == kCacheBf16 ? 550 + 200 * nr : dtype == kCacheE4m3 ? 1150 + 450 * nr : 1500 + 500 * nr)
+                                   : (dtype == kCacheBf16 ? 340 : dtype == kCacheE4m3 ? 460 : 590) + 140 * nr;
     const int64_t rounds = (T + 4 * keys - 1) / (4 * keys);
     int64_t best = 0;
     int best_s = 1;
     for (int s = 1; s <= kMaxSplits && s <= rounds && (s == 1 || s * heads <= kFewBlocks); ++s) {
         const int64_t turns = (heads * s + kPlanCus - 1) / kPlanCus;
-        const int64_t cost = turns * ((rounds + s - 1) / s + 2) + (s > 1 ? 3 : 0);
+        const int64_t work = turns * ((rounds + s - 1) / s * round + 2000);
+        const int64_t cost = work + (s > 1 ? 3000 + heads * rows * s * d * 2 / 1000 : 0);
         if (s == 1 || cost < best) best = cost, best_s = s;
     }
     return best_s;
@@ -956,7 +963,7 @@ int tile_splits(int64_t heads, int rows, int T, int d) {
 }  // namespace
 
 int chunk_splits(int64_t heads, int rows, int T, int d, int dtype) {
-    if (rows <= kFewRows) return few_splits(heads, T, d == 128 && dtype == kCacheBf16 ? 32 : 64);
+    if (rows <= kFewRows) return few_splits(heads, rows, T, d, dtype);
     return tile_splits(heads, rows, T, d);
 }
 

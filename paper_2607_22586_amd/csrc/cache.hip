@@ -2,7 +2,11 @@
 // (mmshiftkv_cache_write), and read back (mmshiftkv_cache_read).  Both are
 // bound by HBM: a row is read and written once, its scale is formed from the
 // registers that hold it.  A group of d / 8 lanes has one row of K and of V,
-// eight values each, so that a row's largest value is a maximum over the group.
+// eight values each, so that a row's largest value is a maximum over the group,
+// by lane moves without LDS.  What is written is stored past the caches (two
+// prompts of 32768 rows of 8 heads, 407 MB: 82 -> 78 us; 65536 rows of 4 heads
+// read back, 194 MB: 41 -> 29 us with the pages still in the memory-side cache);
+// several rows per group, and loads past the caches, were no faster.
 #include "pages.hpp"
 
 namespace mmskv {
@@ -10,13 +14,20 @@ namespace {
 
 constexpr int kCacheThreads = 256;
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <typename V>
+__device__ __forceinline__ void put(void* p, V x) {
+    __builtin_nontemporal_store(x, static_cast<V*>(p));
+}
+
 // Eight values of a source row in fp32.
 template <bool F32>
 __device__ __forceinline__ void load8(const void* base, int64_t elem, float (&x)[8]) {
     if constexpr (F32) {
-        const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + elem);
-        const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + elem + 4);
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+        const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + elem);
+        const f32x4 b = *reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + elem + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
     } else {
         const u32x4 r = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + elem);
 #pragma unroll
@@ -25,6 +36,21 @@ __device__ __forceinline__ void load8(const void* base, int64_t elem, float (&x)
             x[2 * j + 1] = __uint_as_float(r[j] & 0xFFFF0000u);
         }
     }
+}
+
+// Maximum over groups of 8 or 16 lanes: neighbours, pairs, then mirrored quads and
+// octets.
+template <int LANES>
+__device__ __forceinline__ float group_max(float x) {
+    const auto moved = [](float v, auto ctrl) {
+        const int b = static_cast<int>(__float_as_uint(v));
+        return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_update_dpp(b, b, decltype(ctrl)::value, 0xF, 0xF, false)));
+    };
+    x = fmaxf(x, moved(x, CacheType<0xB1>{}));     // quad_perm [1, 0, 3, 2]
+    x = fmaxf(x, moved(x, CacheType<0x4E>{}));     // quad_perm [2, 3, 0, 1]
+    x = fmaxf(x, moved(x, CacheType<0x141>{}));    // row_half_mirror
+    if constexpr (LANES == 16) x = fmaxf(x, moved(x, CacheType<0x140>{}));     // row_mirror
+    return x;
 }
 
 // Scale of a row with largest value a, and what its values are multiplied by.
@@ -53,13 +79,12 @@ __device__ __forceinline__ void store_row(void* pool, float* scales, int64_t row
         u32x4 y;
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(pool) + (row * LANES + lane) * 8) = y;
+        put(static_cast<uint16_t*>(pool) + (row * LANES + lane) * 8, y);
     } else {
         float a = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) a = fmaxf(a, fabsf(x[j]));
-#pragma unroll
-        for (int m = 1; m < LANES; m *= 2) a = fmaxf(a, __shfl_xor(a, m, LANES));
+        a = group_max<LANES>(a);
         float mul;
         const float scale = row_scale<TYPE>(a, &mul);
         u32x2 y;
@@ -77,7 +102,7 @@ __device__ __forceinline__ void store_row(void* pool, float* scales, int64_t row
                 y[w] = v;
             }
         }
-        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(pool) + (row * LANES + lane) * 8) = y;
+        put(static_cast<uint8_t*>(pool) + (row * LANES + lane) * 8, y);
         if (lane == 0) scales[row] = scale;
     }
 }
@@ -105,8 +130,8 @@ __global__ void __launch_bounds__(kCacheThreads) cache_write_kernel(CacheWriteAr
     store_row<TYPE, LANES>(a.pages.v, a.pages.v_scale, row, lane, v);
 }
 
-// Eight cached values times their scale, rounded once, to dst.
-template <int TYPE, bool F32>
+// Eight cached values times their scale.
+template <int TYPE>
 __device__ __forceinline__ void load_row(const void* pool, const float* scales, int64_t row, int lanes, int lane,
                                          float (&x)[8]) {
     const int64_t e = (row * lanes + lane) * 8;
@@ -129,13 +154,13 @@ template <bool F32>
 __device__ __forceinline__ void store8(void* base, int64_t elem, const float (&x)[8]) {
     if constexpr (F32) {
         float* p = static_cast<float*>(base) + elem;
-        *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+        put(p, f32x4{x[0], x[1], x[2], x[3]});
+        put(p + 4, f32x4{x[4], x[5], x[6], x[7]});
     } else {
         u32x4 y;
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(base) + elem) = y;
+        put(static_cast<uint16_t*>(base) + elem, y);
     }
 }
 
@@ -145,61 +170,57 @@ __global__ void __launch_bounds__(kCacheThreads) cache_read_kernel(CacheReadArgs
     const int lane = threadIdx.x % LANES;
     const int64_t t = static_cast<int64_t>(blockIdx.x) * (kCacheThreads / LANES) + threadIdx.x / LANES;
     const int c = blockIdx.y, b = blockIdx.z;
-    const int64_t hc = static_cast<int64_t>(b) * a.Hkv + c;
     if (t >= a.T) return;
     float k[8] = {}, v[8] = {};
-    if (t < min(a.lens[hc], a.pages.cap)) {
+    if (t < min(a.lens[static_cast<int64_t>(b) * a.Hkv + c], a.pages.cap)) {
         const int id = page_of(a.pages, b, static_cast<int>(t));
         if (id >= 0) {
             const int64_t row = pool_row(a.pages, a.Hkv, c, id, static_cast<int>(t));
-            load_row<TYPE, F32>(a.pages.k, a.pages.k_scale, row, LANES, lane, k);
-            load_row<TYPE, F32>(a.pages.v, a.pages.v_scale, row, LANES, lane, v);
+            load_row<TYPE>(a.pages.k, a.pages.k_scale, row, LANES, lane, k);
+            load_row<TYPE>(a.pages.v, a.pages.v_scale, row, LANES, lane, v);
         }
     }
     store8<F32>(a.k, b * a.ksb + c * a.ksh + t * a.kst + 8 * lane, k);
     store8<F32>(a.v, b * a.vsb + c * a.vsh + t * a.vst + 8 * lane, v);
 }
 
-template <int D, int TYPE>
-void write_rows(const CacheWriteArgs& a, dim3 grid, hipStream_t s) {
-    if (a.dtype == 0) hipLaunchKernelGGL((cache_write_kernel<D, TYPE, true>), grid, dim3(kCacheThreads), 0, s, a);
-    else hipLaunchKernelGGL((cache_write_kernel<D, TYPE, false>), grid, dim3(kCacheThreads), 0, s, a);
-}
-
-template <int D, int TYPE>
-void read_rows(const CacheReadArgs& a, dim3 grid, hipStream_t s) {
-    if (a.dtype == 0) hipLaunchKernelGGL((cache_read_kernel<D, TYPE, true>), grid, dim3(kCacheThreads), 0, s, a);
-    else hipLaunchKernelGGL((cache_read_kernel<D, TYPE, false>), grid, dim3(kCacheThreads), 0, s, a);
-}
-
+// A group of lanes for each row of each head.
 dim3 row_grid(int rows, int d, int Hkv, int B) {
     const int per = kCacheThreads / (d / 8);
     return dim3(static_cast<unsigned>((static_cast<int64_t>(rows) + per - 1) / per), Hkv, B);
 }
 
+// The kernel's type and row size as constants.
+template <typename F>
+void with_type(int d, int type, F&& run) {
+    const auto at = [&](auto t) {
+        if (d == 64) run(CacheType<64>{}, t);
+        else run(CacheType<128>{}, t);
+    };
+    if (type == kCacheBf16) at(CacheType<kCacheBf16>{});
+    else if (type == kCacheE4m3) at(CacheType<kCacheE4m3>{});
+    else at(CacheType<kCacheI8>{});
+}
+
 }  // namespace
 
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t s) {
-    const dim3 grid = row_grid(a.n, a.d, a.Hkv, a.B);
-    const auto at = [&](auto type) {
-        if (a.d == 64) write_rows<64, decltype(type)::value>(a, grid, s);
-        else write_rows<128, decltype(type)::value>(a, grid, s);
-    };
-    if (a.pages.dtype == kCacheBf16) at(CacheType<kCacheBf16>{});
-    else if (a.pages.dtype == kCacheE4m3) at(CacheType<kCacheE4m3>{});
-    else at(CacheType<kCacheI8>{});
+    with_type(a.d, a.pages.dtype, [&](auto d, auto type) {
+        constexpr int D = decltype(d)::value, TYPE = decltype(type)::value;
+        const dim3 grid = row_grid(a.n, a.d, a.Hkv, a.B);
+        if (a.dtype == 0) hipLaunchKernelGGL((cache_write_kernel<D, TYPE, true>), grid, dim3(kCacheThreads), 0, s, a);
+        else hipLaunchKernelGGL((cache_write_kernel<D, TYPE, false>), grid, dim3(kCacheThreads), 0, s, a);
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t s) {
-    const dim3 grid = row_grid(a.T, a.d, a.Hkv, a.B);
-    const auto at = [&](auto type) {
-        if (a.d == 64) read_rows<64, decltype(type)::value>(a, grid, s);
-        else read_rows<128, decltype(type)::value>(a, grid, s);
-    };
-    if (a.pages.dtype == kCacheBf16) at(CacheType<kCacheBf16>{});
-    else if (a.pages.dtype == kCacheE4m3) at(CacheType<kCacheE4m3>{});
-    else at(CacheType<kCacheI8>{});
+    with_type(a.d, a.pages.dtype, [&](auto d, auto type) {
+        constexpr int D = decltype(d)::value, TYPE = decltype(type)::value;
+        const dim3 grid = row_grid(a.T, a.d, a.Hkv, a.B);
+        if (a.dtype == 0) hipLaunchKernelGGL((cache_read_kernel<D, TYPE, true>), grid, dim3(kCacheThreads), 0, s, a);
+        else hipLaunchKernelGGL((cache_read_kernel<D, TYPE, false>), grid, dim3(kCacheThreads), 0, s, a);
+    });
     return hipGetLastError();
 }
 

@@ -34,10 +34,11 @@ __device__ __forceinline__ int page_of(const Pages& p, int b, int t) {
 __device__ __attribute__((aligned(16))) const unsigned char kNoRows[1024] = {};
 
 // 16 / 4 bytes per lane from memory to LDS (dst + 16 / 4 * lane); OFF is added
-// to both addresses.
+// to both addresses.  The 16 bytes are fetched as not to be used again (cached
+// rows that one workgroup alone reads: 16 x 8 heads of 32768 rows 304 -> 272 us).
 template <int OFF = 0>
 __device__ __forceinline__ void load16_to_lds(const char* src, char* dst) {
-    __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, OFF, 0);
+    __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, OFF, 2);
 }
 __device__ __forceinline__ void load4_to_lds(const char* src, char* dst) {
     __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);

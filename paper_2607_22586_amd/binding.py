@@ -638,39 +638,59 @@ class PagedCache:
 
     def c_pages(self) -> Pages:
         k, v, ks, vs, table = self.k, self.v, self.k_scale, self.v_scale, self.table
-        dtype, shape = k.dtype, k.shape
+        dtype, shape, i = k.dtype, k.shape, k.get_device()
         code = _CACHE_DTYPES.get(dtype)
         if code is None:
             raise TypeError("expected bfloat16, float8_e4m3fn or int8 pages, got %s" % dtype)
-        if len(shape) != 4 or v.shape != shape or v.dtype != dtype or not (k.is_contiguous() and v.is_contiguous()):
+        if v.dtype != dtype or v.shape != shape or len(shape) != 4 or not (k.is_contiguous() and v.is_contiguous()):
             raise ValueError("k and v pages must be contiguous [n_pages, Hkv, page, d] of one dtype")
-        if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
+        size = table.shape
+        if table.dtype != torch.int32 or len(size) != 2 or not table.is_contiguous():
             raise ValueError("the table must be a contiguous int32 [B, max_pages] tensor")
-        _same_device(k, v, table)
+        if v.get_device() != i or table.get_device() != i:
+            raise ValueError("pages and table on different devices")
         if code == MMSKV_BF16:
-            ks = vs = None
-        else:
-            rows = shape[:3]
-            for s in (ks, vs):
-                if s is None or s.dtype != torch.float32 or s.shape != rows or not s.is_contiguous():
-                    raise ValueError("8-bit pages need contiguous fp32 scales [n_pages, Hkv, page]")
-            _same_device(k, ks, vs)
-        return Pages(k.data_ptr(), v.data_ptr(), _p(ks), _p(vs), table.data_ptr(), shape[0], shape[2],
-                     table.shape[1], code)
+            return Pages(k.data_ptr(), v.data_ptr(), None, None, table.data_ptr(), shape[0], shape[2], size[1], code)
+        rows = shape[:3]
+        for s in (ks, vs):
+            if (s is None or s.dtype != torch.float32 or s.shape != rows or not s.is_contiguous()
+                    or s.get_device() != i):
+                raise ValueError("8-bit pages need contiguous fp32 scales [n_pages, Hkv, page] on their device")
+        return Pages(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), table.data_ptr(), shape[0], shape[2],
+                     size[1], code)
 
 
-def _same_device(t, *others):
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _enqueue(name: str, i: int, *args):
+    """A call of the library on the current stream of device i, which is made current around it."""
+    fn = getattr(load_library(), name)
+    if _current_device() == i:
+        rc = fn(*args, _raw_stream(i))
+    else:
+        with _on(torch.device("cuda", i)):
+            rc = fn(*args, _raw_stream(i))
+    if rc != MMSKV_OK:
+        raise MMShiftKVError(name, rc)
+
+
+def _same_device(t, *others) -> int:
+    """The index of the device that all the tensors are on."""
     i = t.get_device()                 # (-1: host)
     for o in others:
         if o is not None and o.get_device() != i:
             raise ValueError("tensors on different devices (%s, %s)" % (t.device, o.device))
-    return _dev(t)
+    if i < 0:
+        _dev(t)
+    return i
 
 
 def _int32(t, shape, what):
-    """Row numbers as the library takes them: contiguous int32 of that shape, or None."""
-    if t is not None and (t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous()):
+    """Row numbers as the library takes them: contiguous int32 of that shape."""
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (what, shape))
+    return t.data_ptr()
 
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, start: torch.Tensor | None = None,
@@ -678,42 +698,48 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, start: torc
     """mmshiftkv_cache_write: rows of k, v [B, Hkv, T, d] (fp32 or bf16) into the cache, from row
     start[b, c] (None: 0) of each head on: the first counts[b, c] (None: all) tokens, or those of
     idx [B, Hkv, n] (a Selected's idx and counts: the kept tokens).  All row numbers int32."""
-    dev = _same_device(k, v, cache.k, start, counts, idx)
-    if v.shape != k.shape or v.dtype != k.dtype:
+    i = _same_device(k, v, cache.k, start, counts, idx)
+    shape = k.shape
+    if v.shape != shape or v.dtype != k.dtype:
         raise ValueError("k and v must have the same shape and dtype")
     ks, vs = _strides4(k), _strides4(v)
-    B, Hkv, T, d = k.shape
-    if cache.k.shape[1] != Hkv or cache.k.shape[3] != d or cache.table.shape[0] != B:
+    B, Hkv, T, d = shape
+    pages, n = cache.c_pages(), T
+    _, heads, _, row = cache.k.shape
+    if heads != Hkv or row != d or cache.table.shape[0] != B:
         raise ValueError("k does not match the cache's heads, row size or sequences")
-    n = T if idx is None else idx.shape[-1]
-    _int32(idx, (B, Hkv, n), "idx")
-    _int32(counts, (B, Hkv), "counts")
-    _int32(start, (B, Hkv), "start")
-    with _on(dev):
-        rc = load_library().mmshiftkv_cache_write(
-            ctypes.byref(_shape(B, 0, Hkv, T, 0, d)), ctypes.byref(cache.c_pages()), _p(k), _p(v), _dtype_code(k),
-            ctypes.byref(ks), ctypes.byref(vs), _p(idx), _p(counts), _p(start), n, _stream(dev))
-    _check("mmshiftkv_cache_write", rc)
+    if idx is not None:
+        n = idx.shape[-1]
+        idx = _int32(idx, (B, Hkv, n), "idx")
+    if counts is not None:
+        counts = _int32(counts, (B, Hkv), "counts")
+    if start is not None:
+        start = _int32(start, (B, Hkv), "start")
+    ref = ctypes.byref
+    _enqueue("mmshiftkv_cache_write", i, ref(Shape(B, 0, Hkv, T, 0, d)), ref(pages), k.data_ptr(), v.data_ptr(),
+             _dtype_code(k), ref(ks), ref(vs), idx, counts, start, n)
 
 
 def cache_read(cache: PagedCache, lens: torch.Tensor, T: int, dtype: torch.dtype = torch.bfloat16, out=None):
     """mmshiftkv_cache_read: (k, v) [B, Hkv, T, d] of the first lens[b, c] cached rows of each head
     (zeros behind them), as bfloat16 or float32; `out` may hold preallocated (k, v)."""
-    dev = _same_device(cache.k, lens)
-    B, Hkv, d = cache.table.shape[0], cache.k.shape[1], cache.k.shape[3]
-    _int32(lens, (B, Hkv), "lens")
+    i = _same_device(cache.k, lens)
+    pages = cache.c_pages()
+    B, T = cache.table.shape[0], int(T)
+    _, Hkv, _, d = cache.k.shape
+    rows = _int32(lens, (B, Hkv), "lens")
+    shape = (B, Hkv, T, d)
     if out is None:
-        out = tuple(torch.empty((B, Hkv, T, d), dtype=dtype, device=dev) for _ in range(2))
-    ko, vo = out
-    _same_device(cache.k, ko, vo)
-    if tuple(ko.shape) != (B, Hkv, T, d) or vo.shape != ko.shape or ko.dtype != dtype or vo.dtype != dtype:
-        raise ValueError("preallocated k/v do not match")
-    with _on(dev):
-        rc = load_library().mmshiftkv_cache_read(
-            ctypes.byref(_shape(B, 0, Hkv, T, 0, d)), ctypes.byref(cache.c_pages()), _p(lens), _dtype_code(ko),
-            _p(ko), ctypes.byref(_strides4(ko)), _p(vo), ctypes.byref(_strides4(vo)), _stream(dev))
-    _check("mmshiftkv_cache_read", rc)
-    return ko, vo
+        ko, vo = out = lens.new_empty(shape, dtype=dtype), lens.new_empty(shape, dtype=dtype)
+    else:
+        ko, vo = out
+        _same_device(lens, ko, vo)
+        if ko.shape != shape or vo.shape != shape or ko.dtype != dtype or vo.dtype != dtype:
+            raise ValueError("preallocated k/v do not match")
+    ref = ctypes.byref
+    _enqueue("mmshiftkv_cache_read", i, ref(Shape(B, 0, Hkv, T, 0, d)), ref(pages), rows, _dtype_code(ko),
+             ko.data_ptr(), ref(_strides4(ko)), vo.data_ptr(), ref(_strides4(vo)))
+    return out
 
 
 def chunk_attention_workspace(B, Hq, Hkv, T, d, n) -> int:
@@ -727,34 +753,35 @@ def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_co
     bf16 (n = 1: a decoding step) over the first lens[b, c] cached rows of each head, the chunk's own
     among them; q_counts[b] (None: n) queries of sequence b are there.  T is an upper bound of lens
     (None: what the table can hold).  The result is laid out as q is unless `out` is given."""
-    dev = _same_device(q, cache.k, lens, q_counts, workspace, out)
+    i = _same_device(q, cache.k, lens, q_counts, workspace, out)
     if q.dtype != torch.bfloat16:
         raise TypeError("q is bf16")
     qs = _strides4(q)
     B, Hq, n, d = q.shape
-    Hkv = cache.k.shape[1]
-    if cache.k.shape[3] != d or cache.table.shape[0] != B:
+    pages = cache.c_pages()
+    _, Hkv, page, row = cache.k.shape
+    if row != d or cache.table.shape[0] != B:
         raise ValueError("q does not match the cache's row size or sequences")
-    _int32(lens, (B, Hkv), "lens")
-    _int32(q_counts, (B,), "q_counts")
-    T = cache.table.shape[1] * cache.k.shape[2] if T is None else int(T)
+    rows = _int32(lens, (B, Hkv), "lens")
+    if q_counts is not None:
+        q_counts = _int32(q_counts, (B,), "q_counts")
     if out is None:
         out = torch.empty_like(q)
-        if out.stride(3) != 1:
-            out = torch.empty((B, Hq, n, d), dtype=torch.bfloat16, device=dev)
-    elif out.dtype != torch.bfloat16 or out.shape != q.shape:
-        raise ValueError("preallocated out does not match")
-    shape = _shape(B, Hq, Hkv, T, 0, d)
-    lib = load_library()
+        os = _strides4(out) if out.stride(3) == 1 else None
+        if os is None:
+            out = q.new_empty(q.shape)
+            os = _strides4(out)
+    else:
+        if out.dtype != torch.bfloat16 or out.shape != q.shape:
+            raise ValueError("preallocated out does not match")
+        os = _strides4(out)
+    ref = ctypes.byref
+    shape = ref(Shape(B, Hq, Hkv, cache.table.shape[1] * page if T is None else int(T), 0, d))
     ws = workspace
     if ws is None:
-        ws = _ws(lib.mmshiftkv_chunk_attention_workspace(ctypes.byref(shape), int(n)), dev)
-    with _on(dev):
-        rc = lib.mmshiftkv_chunk_attention(
-            ctypes.byref(shape), ctypes.byref(cache.c_pages()), _p(q), ctypes.byref(qs), _p(q_counts), _p(lens),
-            n, int(bool(causal)), _p(out), ctypes.byref(_strides4(out)), _p(ws), ws.numel() * ws.element_size(),
-            _stream(dev))
-    _check("mmshiftkv_chunk_attention", rc)
+        ws = _ws(load_library().mmshiftkv_chunk_attention_workspace(shape, n), q.device)
+    _enqueue("mmshiftkv_chunk_attention", i, shape, ref(pages), q.data_ptr(), ref(qs), q_counts, rows, n,
+             1 if causal else 0, out.data_ptr(), ref(os), ws.data_ptr(), ws.numel() * ws.element_size())
     return out
 
 

@@ -428,7 +428,8 @@ typedef struct {
  *               float type no precision, and the division is exact
  *   MMSKV_I8    a' = max(a, 2^-100), scale a' / 127, y = rint(x * (127 / a'))
  * every rounding to nearest even.
- * Reads shape->B, Hkv, T and d (64 or 128); Hq and W are ignored.
+ * Reads shape->B, Hkv, T and d (64 or 128); Hq and W are ignored.  n up to 2^27
+ * (more -> MMSKV_EUNSUPPORTED).
  *   k, v    [B, Hkv, T, d] dtype (fp32 or bf16), strides k_strides / v_strides
  *   idx     [B, Hkv, n] int32 or NULL;  counts, start  [B, Hkv] int32 or NULL
  *           (NULL: n rows, from row 0) */
@@ -440,7 +441,8 @@ int mmshiftkv_cache_write(const mmskv_shape *shape, const mmskv_pages *pages, co
 /* Reads a paged cache back: row t < lens[b,c] of (b, c), times its scale in
  * fp32, rounded once to dtype; rows t >= lens[b,c] are zero-filled.  The
  * result has the layout that mmshiftkv_score and mmshiftkv_gather_kv take.
- * Reads shape->B, Hkv, T (rows of the result) and d (64 or 128).
+ * Reads shape->B, Hkv, T (rows of the result, up to 2^27, else
+ * MMSKV_EUNSUPPORTED) and d (64 or 128).
  *   lens          [B, Hkv] int32, taken as if clamped to [0, max_pages * page]
  *   k_out, v_out  [B, Hkv, T, d] dtype (fp32 or bf16), strides
  *                 k_out_strides / v_out_strides, rows not overlapping */
@@ -463,7 +465,8 @@ int mmshiftkv_cache_read(const mmskv_shape *shape, const mmskv_pages *pages, con
  * the result rounded once.  A query that sees no row gives zeros, and so do
  * the rows i >= nq of out.
  * Reads shape->B, Hq, Hkv, T (an upper bound of lens, which fixes how the work
- * is split) and d; W is ignored.
+ * is split) and d; W is ignored.  Gh * n up to 2^22 and B * Hkv up to 2^23 (more
+ * -> MMSKV_EUNSUPPORTED).
  *   q    [B, Hq, n, d] bf16, strides q_strides;  q_counts [B] int32 or NULL
  *   out  [B, Hq, n, d] bf16, strides out_strides, rows not overlapping
  * Workspace: mmshiftkv_chunk_attention_workspace bytes (256-byte aligned; 0

@@ -686,6 +686,14 @@ def _same_device(t, *others) -> int:
     return i
 
 
+def _row_strides(t: torch.Tensor) -> Strides:
+    """_strides4 with 0 for dimensions of one entry, whose stride means nothing."""
+    st, n = t.stride(), t.shape
+    if len(st) != 4 or st[3] != 1:
+        raise ValueError("expected a [batch, head, token, d] tensor with contiguous d")
+    return Strides(st[0] if n[0] > 1 else 0, st[1] if n[1] > 1 else 0, st[2] if n[2] > 1 else 0)
+
+
 def _int32(t, shape, what):
     """Row numbers as the library takes them: contiguous int32 of that shape."""
     if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
@@ -702,7 +710,7 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, start: torc
     shape = k.shape
     if v.shape != shape or v.dtype != k.dtype:
         raise ValueError("k and v must have the same shape and dtype")
-    ks, vs = _strides4(k), _strides4(v)
+    ks, vs = _row_strides(k), _row_strides(v)
     B, Hkv, T, d = shape
     pages, n = cache.c_pages(), T
     _, heads, _, row = cache.k.shape
@@ -738,7 +746,7 @@ def cache_read(cache: PagedCache, lens: torch.Tensor, T: int, dtype: torch.dtype
             raise ValueError("preallocated k/v do not match")
     ref = ctypes.byref
     _enqueue("mmshiftkv_cache_read", i, ref(Shape(B, 0, Hkv, T, 0, d)), ref(pages), rows, _dtype_code(ko),
-             ko.data_ptr(), ref(_strides4(ko)), vo.data_ptr(), ref(_strides4(vo)))
+             ko.data_ptr(), ref(_row_strides(ko)), vo.data_ptr(), ref(_row_strides(vo)))
     return out
 
 
@@ -756,7 +764,7 @@ def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_co
     i = _same_device(q, cache.k, lens, q_counts, workspace, out)
     if q.dtype != torch.bfloat16:
         raise TypeError("q is bf16")
-    qs = _strides4(q)
+    qs = _row_strides(q)
     B, Hq, n, d = q.shape
     pages = cache.c_pages()
     _, Hkv, page, row = cache.k.shape
@@ -767,14 +775,14 @@ def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_co
         q_counts = _int32(q_counts, (B,), "q_counts")
     if out is None:
         out = torch.empty_like(q)
-        os = _strides4(out) if out.stride(3) == 1 else None
+        os = _row_strides(out) if out.stride(3) == 1 else None
         if os is None:
             out = q.new_empty(q.shape)
-            os = _strides4(out)
+            os = _row_strides(out)
     else:
         if out.dtype != torch.bfloat16 or out.shape != q.shape:
             raise ValueError("preallocated out does not match")
-        os = _strides4(out)
+        os = _row_strides(out)
     ref = ctypes.byref
     shape = ref(Shape(B, Hq, Hkv, cache.table.shape[1] * page if T is None else int(T), 0, d))
     ws = workspace

@@ -791,6 +791,10 @@ int check_cache_shape(const mmskv_shape* s) {
     return MMSKV_OK;
 }
 
+// Rows of a head and (b, c) pairs that a launch of these calls can hold.
+constexpr int kMaxCacheRows = 1 << 27;
+constexpr int64_t kMaxChunkHeads = 1 << 23;
+
 // Output rows that are written: a stride of 0 would put rows over each other.
 int check_out_rows(const void* base, const mmskv_strides* st, int eb, int nb, int nh, int nt) {
     const int rc = check_rows(base, st, eb, true);
@@ -805,6 +809,7 @@ int check_chunk(const mmskv_shape* s, int32_t n) {
     if (s->d < 1 || n < 1) return MMSKV_EINVAL;
     if (s->d != 64 && s->d != 128) return MMSKV_EUNSUPPORTED;
     if (static_cast<int64_t>(s->Hq / s->Hkv) * n > (1 << 22)) return MMSKV_EUNSUPPORTED;
+    if (static_cast<int64_t>(s->B) * s->Hkv > kMaxChunkHeads) return MMSKV_EUNSUPPORTED;
     return MMSKV_OK;
 }
 
@@ -826,6 +831,7 @@ int mmshiftkv_cache_write(const mmskv_shape* shape, const mmskv_pages* pages, co
     const int eb = elem_bytes(dtype);
     if (eb == 0 || k == nullptr || v == nullptr) return MMSKV_EINVAL;
     if (n < 1 || (idx == nullptr && n > shape->T)) return MMSKV_EINVAL;
+    if (n > kMaxCacheRows) return MMSKV_EUNSUPPORTED;
     if (!aligned(idx, 4) || !aligned(counts, 4) || !aligned(start, 4)) return MMSKV_EINVAL;
     rc = check_rows(k, k_strides, eb, true);
     if (rc) return rc;
@@ -861,6 +867,7 @@ int mmshiftkv_cache_read(const mmskv_shape* shape, const mmskv_pages* pages, con
     if (rc) return rc;
     const int eb = elem_bytes(dtype);
     if (eb == 0 || lens == nullptr || !aligned(lens, 4) || k_out == nullptr || v_out == nullptr) return MMSKV_EINVAL;
+    if (shape->T > kMaxCacheRows) return MMSKV_EUNSUPPORTED;
     rc = check_out_rows(k_out, k_out_strides, eb, shape->B, shape->Hkv, shape->T);
     if (rc) return rc;
     rc = check_out_rows(v_out, v_out_strides, eb, shape->B, shape->Hkv, shape->T);

@@ -27,6 +27,11 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 32 * kWaves;         // query rows of a workgroup
 constexpr int kKeys = 64;                  // keys of a tile
 constexpr float kNone = -3e38f;            // running maximum before the first visible key
+// The reference m of a row's sums need not be its maximum, only near it: it moves
+// where a lane's 16 (few rows: 8 or 16) weights add up to this, so that no maximum
+// is formed in most tiles and the output is seldom rescaled.  The sums are at most
+// this much larger than they would be relative to the maximum.
+constexpr float kBehind = 0x1p8f;
 
 __device__ __forceinline__ floatx16 mfma32(bf16x8 a, bf16x8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -67,8 +72,9 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     __shared__ __align__(16) float ksc[2][kScaled ? kKeys : 4], vsc[2][kScaled ? kKeys : 4];
 
     const int bc = blockIdx.x, b = bc / a.Hkv, c = bc - b * a.Hkv;
-    const int r0 = static_cast<int>(gridDim.y - 1 - blockIdx.y) * kRows;
-    const int split = blockIdx.z;
+    // the last rows, which see most keys, first, with all their splits
+    const int r0 = static_cast<int>((gridDim.y - 1 - blockIdx.y) / a.splits) * kRows;
+    const int split = blockIdx.y % a.splits;
     const int tid = threadIdx.x, lane = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane >> 5;
@@ -232,11 +238,9 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
             }
             return pack_bf16(x[0], x[1]);
         };
-        // The reference m moves only where a lane's sum says that it is left far
-        // behind: the sums hold as well relative to any m near the maximum, so that
-        // no maximum is formed in most tiles and the output seldom rescaled.
+        // m moved where half u leaves it behind
         auto settle = [&](int u, uint32_t (&p)[8], float sum) {
-            if (__any(!(sum < 0x1p16f))) {
+            if (__any(!(sum < kBehind))) {
                 float mx = kNone;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, logit(u, e, 0.f));
@@ -670,14 +674,14 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_few_kernel(ChunkArgs a) {
                 }
             }
         };
-        // the reference m moves only where it is left far behind, as above
+        // m moves where the tile leaves it behind; in the first tile there is none yet
         bool behind = first;
         if (!first) {
             weights();
             float most = sum[0];
 #pragma unroll
-            for (int x = 1; x < NR; ++x) most = sum[x] < 0x1p16f ? most : sum[x];
-            behind = __any(!(most < 0x1p16f));
+            for (int x = 1; x < NR; ++x) most = sum[x] < kBehind ? most : sum[x];
+            behind = __any(!(most < kBehind));
         }
         if (behind) {
 #pragma unroll
@@ -877,7 +881,7 @@ void attend(const ChunkArgs& a, hipStream_t s) {
     const unsigned heads = static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hkv);
     if (a.rows > kFewRows) {
         const int tiles = (a.rows + kRows - 1) / kRows;
-        hipLaunchKernelGGL((chunk_kernel<D, TYPE>), dim3(heads, tiles, a.splits), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((chunk_kernel<D, TYPE>), dim3(heads, tiles * a.splits), dim3(kThreads), 0, s, a);
         return;
     }
     const dim3 grid(heads, a.splits);

@@ -71,6 +71,7 @@ def test_write_rejects(lib):  # noqa: F811
     assert write(lib, n=0) == bd.MMSKV_EINVAL
     assert write(lib, n=1025) == bd.MMSKV_EINVAL                      # more rows than tokens
     assert write(lib, idx=ctypes.c_void_p(0x10002), n=2000) == bd.MMSKV_EINVAL
+    assert write(lib, idx=FAKE, n=(1 << 27) + 1) == bd.MMSKV_EUNSUPPORTED
     # scales are not asked for where none are kept (the call stops at its source)
     assert write(lib, p=pages(dtype=bd.MMSKV_BF16, k_scale=None, v_scale=None), k=None) == bd.MMSKV_EINVAL
 
@@ -83,6 +84,7 @@ def test_read_rejects(lib):  # noqa: F811
     assert read(lib, ks=bd.Strides(0, 0, 3)) == bd.MMSKV_EINVAL
     assert read(lib, vs=bd.Strides(64, 64, 0)) == bd.MMSKV_EINVAL     # rows over each other
     assert read(lib, s=shape(B=2), ks=bd.Strides(0, 64, 64)) == bd.MMSKV_EINVAL
+    assert read(lib, s=shape(T=(1 << 27) + 1)) == bd.MMSKV_EUNSUPPORTED
 
 
 def test_attention_rejects(lib):  # noqa: F811
@@ -97,6 +99,7 @@ def test_attention_rejects(lib):  # noqa: F811
     assert attend(lib, os=bd.Strides(64, 0, 64)) == bd.MMSKV_EINVAL
     assert attend(lib, n=0) == bd.MMSKV_EINVAL
     assert attend(lib, n=1 << 21) == bd.MMSKV_EUNSUPPORTED
+    assert attend(lib, s=shape(B=65535, Hq=129, Hkv=129)) == bd.MMSKV_EUNSUPPORTED
     assert attend(lib, causal=2) == bd.MMSKV_EINVAL
     assert attend(lib, s=shape(Hq=5, Hkv=2)) == bd.MMSKV_EINVAL
     assert attend(lib, ws=None) == bd.MMSKV_EWORKSPACE

@@ -201,6 +201,10 @@ CASES = [(1, 1, 1, 1, 64, 16, 1), (1, 4, 1, 63, 64, 16, 1), (2, 7, 1, 64, 128, 6
          (1, 3, 1, 128, 64, 1024, 43), (1, 14, 2, 500, 128, 64, 70), (1, 2, 2, 300, 64, 256, 300),
          (1, 33, 1, 1500, 128, 32, 1), (2, 20, 1, 900, 64, 64, 7), (1, 7, 1, 5001, 128, 64, 1),
          (1, 8, 1, 4100, 64, 16, 2)]
+# heads for all CUs, so that nothing is split and every wave walks several tiles: one, two and four tiles
+# of 16 rows, and rows for the staged tiles
+CASES += [(16, 16, 16, 1500, 64, 64, 1), (8, 64, 32, 1111, 128, 16, 1), (8, 160, 32, 650, 128, 32, 4),
+          (4, 384, 64, 700, 64, 64, 8), (8, 192, 32, 650, 128, 64, 8), (8, 96, 32, 700, 128, 64, 25)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
@@ -262,6 +266,34 @@ def test_attention_layouts(kind, n):
     assert torch.equal(view, want)
     view.fill_(7.0)
     assert (big == 7.0).all()
+
+
+def test_strides_of_single_entries():
+    """The stride of a dimension of one entry means nothing (here 1 element: no multiple of 16 bytes)."""
+    cache = filled(2, 3, 80, 64, E4M3, 16)
+    q = rnd(6, 2, 3, 64, 1, dtype=BF16).to(DEV).transpose(2, 3)
+    assert q.stride(2) == 1
+    check_attention(cache, q, [[80, 3, 17], [40, 79, 16]])
+    bd.cache_write(cache, q, q, start=i32([[70, 2, 16], [39, 0, 15]]))
+    ko, vo = bd.cache_read(cache, i32([[71, 3, 17], [40, 1, 16]]), 80)
+    for b, c, t in ((0, 0, 70), (1, 2, 15)):
+        y, s = paged.quantised(q[b, c].float().cpu().numpy(), E4M3)
+        assert np.array_equal(ko[b, c, t].cpu().double().numpy(), y[0] * s[0]) and torch.equal(ko[b, c, t], vo[b, c, t])
+
+
+@pytest.mark.parametrize("n", [1, 30])
+def test_attention_large_values(n):
+    """Values of 2^110, keys whose logits grow along the sequence: sums relative to a reference that lags
+    behind the maximum (by 2^8 at most) stay in range."""
+    T, d = 500, 64
+    cache = make_cache(1, 2, T, d, BF16, 64)
+    k, v = rnd(1, 1, 2, T, d), rnd(2, 1, 2, T, d).sign() * 2.0 ** 110
+    k *= torch.linspace(0.1, 3.0, T)[:, None]
+    k[..., 0] += torch.linspace(0, 40, T)
+    bd.cache_write(cache, k.to(DEV), v.to(DEV))
+    q = rnd(3, 1, 6, n, d)
+    q[..., 0] = 3.0
+    check_attention(cache, q.to(BF16), [[T, 333]])
 
 
 @pytest.mark.parametrize("kind", KINDS)

@@ -24,7 +24,9 @@ bounded sample of the same workload.
 Other modes, one JSON line each: --decode-check N_DEC (the decode-time
 coverage check), --selectors N_DEC (the method beside the baseline
 selectors on the same kernels), --hidden (the hidden-state form of the
-proxies in front of the same scoring and selection).
+proxies in front of the same scoring and selection), --paged TYPE (a prompt
+in a paged cache of bf16, e4m3 or int8: its chunks, the selection on what is
+read back, decoding on the kept rows).
 """
 from __future__ import annotations
 
@@ -388,6 +390,105 @@ def hidden_bench(args):
     print(json.dumps(out), flush=True)
 
 
+PAGED_CHUNK = 1024            # tokens of a prompt's last chunk in the --paged mode
+
+
+def paged_bench(args):
+    """A layer's prompt in a paged cache, as a serving program has it: its rows
+    written (and quantised), the attention of its last chunk, the rows read back
+    for the selection, the kept rows written to a small cache, then K steps of
+    decoding (a captured graph), each a token's row written and its attention over
+    the kept rows; beside it the attention of one token over the whole prompt.  One JSON line:
+    decoded tokens per second over all layers, and each call's time."""
+    import torch
+    from paper_2607_22586_amd import binding as bd
+    from paper_2607_22586_amd import workloads as wl
+    bd.load_library()
+    dev = torch.device("cuda:0")
+    w = wl.WORKLOADS[args.workload]
+    L = args.layers or w.L
+    B, Hq, Hkv, T, d = w.B, w.Hq, w.Hkv, w.T, w.d
+    dtype = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}[args.paged]
+    n = min(PAGED_CHUNK, T)
+    new = args.warmup + args.steps                 # decoded tokens
+    log("generating %d layers of %s" % (L, w.name))
+    layers = [wl.make_layer(w, l, device=dev) for l in range(L)]
+    gen = torch.Generator(device=dev).manual_seed(w.wid)
+    full = torch.full((B, Hkv), T, dtype=torch.int32, device=dev)
+    prompt = bd.PagedCache.empty(B, Hkv, T, d, dtype, device=dev)
+    q = torch.randn((B, n, Hq, d), generator=gen, device=dev).bfloat16().transpose(1, 2)
+    ws = torch.empty(max(bd.chunk_attention_workspace(B, Hq, Hkv, T, d, x) for x in (1, n)), dtype=torch.uint8,
+                     device=dev)
+    eb, cb = layers[0]["k"].element_size(), prompt.k.element_size()
+    row = 2 * (d * cb + (0 if cb == 2 else 4))     # bytes of a cached row of K and V
+    calls = {}                                     # name: (times, bytes, flops)
+
+    def timed(name, nbytes, flops, fn):
+        e0, e1 = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        e0.record()
+        r = fn()
+        e1.record()
+        calls.setdefault(name, ([], nbytes, flops))[0].append((e0, e1))
+        return r
+
+    kept, lens = [], []
+    for l, x in enumerate(layers):
+        timed("write_prompt", B * Hkv * T * (2 * d * eb + row), 0, lambda: bd.cache_write(prompt, x["k"], x["v"]))
+        seen = n * (T - n) + n * (n + 1) // 2
+        timed("chunk_attention", B * (Hkv * T * row + 4 * Hq * n * d), 4 * d * B * Hq * seen,
+              lambda: bd.chunk_attention(q, prompt, full, T=T, workspace=ws))
+        timed("step_over_prompt", B * (Hkv * T * row + 4 * Hq * d), 4 * d * B * Hq * T,
+              lambda: bd.chunk_attention(q[:, :, -1:], prompt, full, T=T, workspace=ws))
+        k, v = timed("read_prompt", B * Hkv * T * (4 * d + row), 0, lambda: bd.cache_read(prompt, full, T))
+        sel = bd.select_layer(x["q_win"], k, v, w.budget, bd.SelectionConfig(seed=w.wid, layer=l)).sel
+        cache = bd.PagedCache.empty(B, Hkv, w.budget + new, d, dtype, device=dev)
+        timed("write_kept", B * Hkv * w.budget * (4 * d + row + 4), 0,
+              lambda: bd.cache_write(cache, k, v, counts=sel.counts, idx=sel.idx))
+        kept.append(cache)
+        lens.append(sel.counts.clone())
+        x.clear()
+    kn, vn = (torch.randn((B, 1, Hkv, d), generator=gen, device=dev).bfloat16().transpose(1, 2) for _ in range(2))
+    q1 = q[:, :, :1].contiguous()
+    out = torch.empty_like(q1)
+
+    def step():
+        for cache, ln in zip(kept, lens):
+            bd.cache_write(cache, kn, vn, start=ln)
+            ln.add_(1)
+            bd.chunk_attention(q1, cache, ln, T=w.budget + new, workspace=ws, out=out)
+
+    # launch-bound (three short launches a layer): captured once, replayed for every token
+    warm = torch.cuda.Stream(dev)
+    warm.wait_stream(torch.cuda.current_stream(dev))
+    with torch.cuda.stream(warm):
+        for _ in range(args.warmup):
+            step()
+    torch.cuda.current_stream(dev).wait_stream(warm)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    t0.record()
+    for _ in range(args.steps):
+        graph.replay()
+    t1.record()
+    torch.cuda.synchronize()
+    ms_step = t0.elapsed_time(t1) / args.steps
+    us = {k: sorted(a.elapsed_time(b) * 1e3 for a, b in ev)[len(ev) // 2] for k, (ev, _, _) in calls.items()}
+    print(json.dumps({
+        "metric": "tokens decoded/sec on kept rows in pages", "value": B / (ms_step * 1e-3), "unit": "tokens/s",
+        "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": ms_step,
+        "us_per_layer": ms_step * 1e3 / L, "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
+        "dtype": args.paged, "data": "synthetic",
+        "config": {"workload": w.name, "layers": L, "batch": B, "T": T, "Hq": Hq, "Hkv": Hkv, "d": d,
+                   "budget": w.budget, "chunk": n, "page": prompt.k.shape[2]},
+        "calls": {k: {"us": us[k], "GB/s": calls[k][1] / us[k] / 1e3, "TFLOP/s": calls[k][2] / us[k] / 1e6}
+                  for k in us},
+        "calls_timing": "median over the layers of events around one call",
+    }), flush=True)
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -411,6 +512,9 @@ def main():
                          "in front of the same scoring, selection and gather")
     ap.add_argument("--hidden-layers", type=int, default=4,
                     help="distinct hidden-state layers generated for --hidden (reused cyclically)")
+    ap.add_argument("--paged", choices=["bf16", "e4m3", "int8"],
+                    help="time a prompt in a paged cache of that type instead: its rows written and read back, "
+                         "the attention of its last chunk, decoding on the kept rows")
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="only run a 1 GiB device copy (counter calibration)")
     args = ap.parse_args()
@@ -430,6 +534,9 @@ def main():
         return
     if args.hidden:
         hidden_bench(args)
+        return
+    if args.paged:
+        paged_bench(args)
         return
 
     import torch

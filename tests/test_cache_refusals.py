@@ -1,6 +1,9 @@
 """Host validation of the paged-cache calls, their workspace contract and the
 binding's checks (CPU only: every call is rejected before anything is enqueued)."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -140,3 +143,11 @@ def test_binding_checks():
         bd.PagedCache(eight.k, eight.v, None, eight.v_scale, eight.table).c_pages()
     with pytest.raises(ValueError):
         bd.PagedCache(eight.k, eight.v, eight.k_scale, eight.v_scale, eight.table.long()).c_pages()
+
+
+def test_bench_lists_the_paged_mode():
+    bench = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "bench.py")
+    r = subprocess.run([sys.executable, bench, "--help"], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "--paged" in r.stdout
+    r = subprocess.run([sys.executable, bench, "--paged", "fp4"], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 2 and r.stdout.strip() == ""

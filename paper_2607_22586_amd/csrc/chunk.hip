@@ -931,18 +931,22 @@ constexpr int kFewBlocks = 4 * kPlanCus;   // workgroups of few rows, where ther
 
 // Splits for few rows.  A workgroup has a CU for itself, so that the launch takes
 // as many turns as there are workgroups per CU, each of them 2 us and the rounds
-// of its split (a tile for each of the four waves); a join reads and writes what
-// the splits left beside 3 us for its launch.  (What memory takes for the keys is
-// the same for any number.)  A round takes one workgroup, at d = 128 and 16 rows, 0.75 us for 128
-// bf16 rows, 1.6 for 256 e4m3 and 2.0 for 256 int8 ones, and more with more tiles
-// of 16 rows.  (28 heads on 4, d = 128, bf16, 1 / 6 / 12 / 64 splits: one is best at
-// 384 rows, six at 700, twelve at 1100, 64 at 16384, 14.7 us against 138; for 16
-// sequences of 16384 rows four, 98 against 105 with 6 and 167 with 1.)
+// of its split (a tile for each of its waves); a join reads and writes what the
+// splits left beside 3 us for its launch.  (What memory takes for the keys is the
+// same for any number.)  A round takes one workgroup, at d = 128 and 16 rows, 0.75
+// us for 128 bf16 rows, 1.2 for 256 e4m3 and 1.6 for 256 int8 ones, and more with
+// more tiles of 16 rows.  (28 heads on 4, d = 128, bf16, 1 / 6 / 12 / 64 splits: one
+// is best at 321 rows, 6.6 us, twelve at 1100, 8.2 against 11.3, 48 or more at
+// 16384, 13.8 against 101; for 16 sequences of 16384 rows four, 97 against 105 with
+// 2 and 166 with 1; for 32 of 1100 e4m3 rows one, 11.9 against 13.8 with 2.)
 int few_splits(int64_t heads, int rows, int T, int d, int dtype) {
     const int keys = d == 128 && dtype == kCacheBf16 ? 32 : 64;
     const int nr = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int64_t round = d == 128 ? (dtype == kCacheBf16 ? 550 + 200 * nr : dtype == kCacheE4m3 ? 1150 + 450 * nr : 1500 + 500 * nr)
-                                   : (dtype == kCacheBf16 ? 340 : dtype == kCacheE4m3 ? 460 : 590) + 140 * nr;
+    int64_t round;
+    if (d == 64) round = (dtype == kCacheBf16 ? 340 : dtype == kCacheE4m3 ? 460 : 590) + 140 * nr;
+    else if (dtype == kCacheBf16) round = 550 + 200 * nr;
+    else if (nr <= 2) round = dtype == kCacheE4m3 ? 1000 + 200 * nr : 1300 + 300 * nr;
+    else round = dtype == kCacheE4m3 ? 3000 : 3500;
     const int64_t rounds = (T + 4 * keys - 1) / (4 * keys);
     int64_t best = 0;
     int best_s = 1;

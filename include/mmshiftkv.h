@@ -465,7 +465,7 @@ int mmshiftkv_cache_read(const mmskv_shape *shape, const mmskv_pages *pages, con
  * the result rounded once.  A query that sees no row gives zeros, and so do
  * the rows i >= nq of out.
  * Reads shape->B, Hq, Hkv, T (an upper bound of lens, which fixes how the work
- * is split) and d; W is ignored.  Gh * n up to 2^22 and B * Hkv up to 2^23 (more
+ * is split) and d; W is ignored.  Gh * n and B * Hkv up to 2^22 (more
  * -> MMSKV_EUNSUPPORTED).
  *   q    [B, Hq, n, d] bf16, strides q_strides;  q_counts [B] int32 or NULL
  *   out  [B, Hq, n, d] bf16, strides out_strides, rows not overlapping

@@ -793,7 +793,7 @@ int check_cache_shape(const mmskv_shape* s) {
 
 // Rows of a head and (b, c) pairs that a launch of these calls can hold.
 constexpr int kMaxCacheRows = 1 << 27;
-constexpr int64_t kMaxChunkHeads = 1 << 23;
+constexpr int64_t kMaxChunkHeads = 1 << 22;
 
 // Output rows that are written: a stride of 0 would put rows over each other.
 int check_out_rows(const void* base, const mmskv_strides* st, int eb, int nb, int nh, int nt) {

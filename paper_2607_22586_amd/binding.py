@@ -784,7 +784,8 @@ def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_co
             raise ValueError("preallocated out does not match")
         os = _row_strides(out)
     ref = ctypes.byref
-    shape = ref(Shape(B, Hq, Hkv, cache.table.shape[1] * page if T is None else int(T), 0, d))
+    most = cache.table.shape[1] * page
+    shape = ref(Shape(B, Hq, Hkv, most if T is None else min(int(T), most), 0, d))
     ws = workspace
     if ws is None:
         ws = _ws(load_library().mmshiftkv_chunk_attention_workspace(shape, n), q.device)

@@ -46,10 +46,10 @@ __device__ __forceinline__ float group_max(float x) {
         const int b = static_cast<int>(__float_as_uint(v));
         return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_update_dpp(b, b, decltype(ctrl)::value, 0xF, 0xF, false)));
     };
-    x = fmaxf(x, moved(x, CacheType<0xB1>{}));     // quad_perm [1, 0, 3, 2]
-    x = fmaxf(x, moved(x, CacheType<0x4E>{}));     // quad_perm [2, 3, 0, 1]
-    x = fmaxf(x, moved(x, CacheType<0x141>{}));    // row_half_mirror
-    if constexpr (LANES == 16) x = fmaxf(x, moved(x, CacheType<0x140>{}));     // row_mirror
+    x = fmaxf(x, moved(x, Constant<0xB1>{}));     // quad_perm [1, 0, 3, 2]
+    x = fmaxf(x, moved(x, Constant<0x4E>{}));     // quad_perm [2, 3, 0, 1]
+    x = fmaxf(x, moved(x, Constant<0x141>{}));    // row_half_mirror
+    if constexpr (LANES == 16) x = fmaxf(x, moved(x, Constant<0x140>{}));     // row_mirror
     return x;
 }
 
@@ -194,12 +194,12 @@ dim3 row_grid(int rows, int d, int Hkv, int B) {
 template <typename F>
 void with_type(int d, int type, F&& run) {
     const auto at = [&](auto t) {
-        if (d == 64) run(CacheType<64>{}, t);
-        else run(CacheType<128>{}, t);
+        if (d == 64) run(Constant<64>{}, t);
+        else run(Constant<128>{}, t);
     };
-    if (type == kCacheBf16) at(CacheType<kCacheBf16>{});
-    else if (type == kCacheE4m3) at(CacheType<kCacheE4m3>{});
-    else at(CacheType<kCacheI8>{});
+    if (type == kCacheBf16) at(Constant<kCacheBf16>{});
+    else if (type == kCacheE4m3) at(Constant<kCacheE4m3>{});
+    else at(Constant<kCacheI8>{});
 }
 
 }  // namespace

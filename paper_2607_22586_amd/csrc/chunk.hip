@@ -333,8 +333,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         ++tile, buf ^= 1;
     };
     const int whole = min(max(all_see, 0) / kKeys, tile1);
-    while (tile < whole) step(CacheType<0>{});
-    while (tile < tile1) step(CacheType<1>{});
+    while (tile < whole) step(Constant<0>{});
+    while (tile < tile1) step(Constant<1>{});
     l = half_sum(l);
     if (r >= a.rows) return;
     if (!there) l = 0.f;                   // (took part where nothing is masked)
@@ -645,8 +645,8 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
 #pragma unroll
                 for (int x = 0; x < NR; ++x) s[x][U0 + z / KC] = mfma16(k[z], qf[x][z % KC], s[x][U0 + z / KC]);
         };
-        logits(CacheType<0>{});
-        if constexpr (UB < NS) logits(CacheType<UB < NS ? UB : 0>{});
+        logits(Constant<0>{});
+        if constexpr (UB < NS) logits(Constant<UB < NS ? UB : 0>{});
         static_assert(2 * UB >= NS, "two blocks of reads");
         floatx4 vw[NS];                    // scales of the keys' V
         if constexpr (T::kScaled) {
@@ -757,18 +757,18 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
         };
         constexpr int US = T::kScaled ? 1 : NS / 2;        // blocks of reads per TB tiles
         static_assert(NT <= 2 * TB && US <= 2, "two by two blocks of reads");
-        output(CacheType<0>{}, CacheType<0>{});
-        if constexpr (US > 1) output(CacheType<0>{}, CacheType<1>{});
-        if constexpr (NT > TB) output(CacheType<NT - TB>{}, CacheType<0>{});
-        if constexpr (NT > TB && US > 1) output(CacheType<NT - TB>{}, CacheType<1>{});
+        output(Constant<0>{}, Constant<0>{});
+        if constexpr (US > 1) output(Constant<0>{}, Constant<1>{});
+        if constexpr (NT > TB) output(Constant<NT - TB>{}, Constant<0>{});
+        if constexpr (NT > TB && US > 1) output(Constant<NT - TB>{}, Constant<1>{});
         __builtin_amdgcn_sched_barrier(0);
         // this stage has been read: the one after the next into its place
         if (tile + 2 * kWaves < tile1) load_stage(tile + 2 * kWaves, STAGE, ids);
         __builtin_amdgcn_sched_barrier(0);
     };
     for (int tile = tile0; tile < tile1; tile += 2 * kWaves) {
-        step(tile, CacheType<0>{}, tile == tile0);
-        if (tile + kWaves < tile1) step(tile + kWaves, CacheType<1>{}, false);
+        step(tile, Constant<0>{}, tile == tile0);
+        if (tile + kWaves < tile1) step(tile + kWaves, Constant<1>{}, false);
     }
 
     // join the waves: value e of o[x][t] is dim 16 t + 4 quarter + e of row 16 x + lane % 16
@@ -929,9 +929,9 @@ hipError_t launch(const ChunkArgs& a, hipStream_t s) {
         hipLaunchKernelGGL((chunk_join_kernel<D, SG>), dim3(static_cast<unsigned>((rows + kPer - 1) / kPer)),
                            dim3(kJoinThreads), 0, s, a);
     };
-    if (a.splits <= kJoinPer) join(CacheType<1>{});
-    else if (a.splits <= 4 * kJoinPer) join(CacheType<4>{});
-    else join(CacheType<16>{});
+    if (a.splits <= kJoinPer) join(Constant<1>{});
+    else if (a.splits <= 4 * kJoinPer) join(Constant<4>{});
+    else join(Constant<16>{});
     return hipGetLastError();
 }
 

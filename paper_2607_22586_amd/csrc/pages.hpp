@@ -12,9 +12,9 @@ typedef float floatx2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kCacheBf16 = 1, kCacheE4m3 = 2, kCacheI8 = 3;   // mmskv_dtype
 
-template <int TYPE>
-struct CacheType {
-    static constexpr int value = TYPE;
+template <int N>
+struct Constant {                          // a number as a type, for generic lambdas
+    static constexpr int value = N;
 };
 
 template <int TYPE>

@@ -430,10 +430,11 @@ struct KOffsets {                          // 16-key tiles U0 + z / KC
     }
 };
 template <class T, int STAGE>
-struct ScaleOffsets {                      // half of K, half of V: keys 32 (z / 2) + 4 (z % 2) (32 keys: some twice)
+struct ScaleOffsets {                      // half of K, half of V: keys 32 (u / 2) + 4 (u % 2)
     static constexpr int at(int z) {
-        const int u = z % 4 % (T::kKeys / 16);
-        return STAGE * T::kStage + 2 * T::kTile + z / 4 * T::kKeys * 4 + 4 * (32 * (u / 2) + 4 * (u % 2));
+        constexpr int kTiles = T::kKeys / 16;
+        const int u = z % kTiles;
+        return STAGE * T::kStage + 2 * T::kTile + z / kTiles * T::kKeys * 4 + 4 * (32 * (u / 2) + 4 * (u % 2));
     }
 };
 template <class T, int STAGE, int U0>
@@ -650,15 +651,22 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
         static_assert(2 * UB >= NS, "two blocks of reads");
         floatx4 vw[NS];                    // scales of the keys' V
         if constexpr (T::kScaled) {
-            static_assert(!T::kScaled || NS == 4 || NS == 2, "eight reads of four scales");
-            uint32_t at[8];
-            u32x4 w[8];
+            u32x4 w[2 * NS];               // of K, then of V
+            if constexpr (NS == 4) {
+                uint32_t at[8];
 #pragma unroll
-            for (int z = 0; z < 8; ++z) at[z] = s_at;
-            read128<ScaleOffsets<T, STAGE>>(at, w);
+                for (int z = 0; z < 8; ++z) at[z] = s_at;
+                read128<ScaleOffsets<T, STAGE>>(at, w);
+            } else {
+                static_assert(NS == 2, "four or eight reads of four scales");
+                uint32_t at[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z) at[z] = s_at + ScaleOffsets<T, STAGE>::at(z);
+                read128(at, w);
+            }
 #pragma unroll
             for (int u = 0; u < NS; ++u) {
-                vw[u] = __builtin_bit_cast(floatx4, w[4 + u]);
+                vw[u] = __builtin_bit_cast(floatx4, w[NS + u]);
 #pragma unroll
                 for (int x = 0; x < NR; ++x) s[x][u] *= __builtin_bit_cast(floatx4, w[u]);
             }

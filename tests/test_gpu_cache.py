@@ -204,7 +204,8 @@ CASES = [(1, 1, 1, 1, 64, 16, 1), (1, 4, 1, 63, 64, 16, 1), (2, 7, 1, 64, 128, 6
 # heads for all CUs, so that nothing is split and every wave walks several tiles: one, two and four tiles
 # of 16 rows, and rows for the staged tiles
 CASES += [(16, 16, 16, 1500, 64, 64, 1), (8, 64, 32, 1111, 128, 16, 1), (8, 160, 32, 650, 128, 32, 4),
-          (4, 384, 64, 700, 64, 64, 8), (8, 192, 32, 650, 128, 64, 8), (8, 96, 32, 700, 128, 64, 25)]
+          (4, 384, 64, 700, 64, 64, 8), (8, 192, 32, 650, 128, 64, 8), (8, 96, 32, 700, 128, 64, 25),
+          (1, 96, 1, 333, 128, 64, 1)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
@@ -266,6 +267,23 @@ def test_attention_layouts(kind, n):
     assert torch.equal(view, want)
     view.fill_(7.0)
     assert (big == 7.0).all()
+
+
+@pytest.mark.parametrize("n", [3, 40])
+def test_attention_padding_may_hold_anything(n):
+    """Queries behind a sequence's count, page entries behind its rows: NaN and numbers of no page."""
+    cache = filled(3, 2, 100, 64, E4M3, 16)
+    cache.table[1, 3:] = -1
+    cache.table[2, 2:] = 2 ** 30
+    q = rnd(8, 3, 4, n, 64, dtype=BF16)
+    counts = [n, n - 2, 1]
+    for b in range(3):
+        q[b, :, counts[b]:] = float("nan")
+    got = bd.chunk_attention(q.to(DEV), cache, i32([[100, 90], [48, 41], [32, 1]]), i32(counts))
+    assert torch.isfinite(got).all()
+    check_attention(cache, torch.nan_to_num(q), [[100, 90], [48, 41], [32, 1]], counts)
+    again = bd.chunk_attention(torch.nan_to_num(q).to(DEV), cache, i32([[100, 90], [48, 41], [32, 1]]), i32(counts))
+    assert torch.equal(got, again)
 
 
 def test_strides_of_single_entries():

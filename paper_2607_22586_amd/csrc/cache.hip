@@ -130,15 +130,43 @@ __global__ void __launch_bounds__(kCacheThreads) cache_write_kernel(CacheWriteAr
     store_row<TYPE, LANES>(a.pages.v, a.pages.v_scale, row, lane, v);
 }
 
+// The two groups of four values that a lane reads back start kApart values apart:
+// next to each other for bf16, which stores them as 16 bytes, half a row for fp32,
+// so that the lanes' 16 bytes of each store lie side by side (32 adjacent bytes a
+// lane leave every store with gaps: 4 x 8 heads of 16384 keys of 128, e4m3, 145 us
+// against 124, 5.4 TB/s; 8 x 8 heads of 8192 keys of 64, 106 us against 51).
+template <int D, bool F32>
+constexpr int kApart = F32 ? D / 2 : 4;
+
 // Eight cached values times their scale.
-template <int TYPE>
-__device__ __forceinline__ void load_row(const void* pool, const float* scales, int64_t row, int lanes, int lane,
-                                         float (&x)[8]) {
-    const int64_t e = (row * lanes + lane) * 8;
+template <int D, int TYPE, bool F32>
+__device__ __forceinline__ void load_row(const void* pool, const float* scales, int64_t row, int lane, float (&x)[8]) {
+    const int64_t e = row * D + (F32 ? 4 : 8) * lane;
     if constexpr (TYPE == kCacheBf16) {
-        load8<false>(pool, e, x);
+        if constexpr (F32) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint16_t* p = static_cast<const uint16_t*>(pool) + e + h * kApart<D, F32>;
+                const u32x2 r = *reinterpret_cast<const u32x2*>(p);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    x[4 * h + 2 * j] = __uint_as_float(r[j] << 16);
+                    x[4 * h + 2 * j + 1] = __uint_as_float(r[j] & 0xFFFF0000u);
+                }
+            }
+        } else {
+            load8<false>(pool, e, x);
+        }
     } else {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(pool) + e);
+        uint32_t w[2];
+        const uint8_t* p = static_cast<const uint8_t*>(pool) + e;
+        if constexpr (F32) {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+            w[1] = *reinterpret_cast<const uint32_t*>(p + kApart<D, F32>);
+        } else {
+            const u32x2 r = *reinterpret_cast<const u32x2*>(p);
+            w[0] = r[0], w[1] = r[1];
+        }
         const float s = scales[row];
         float y[4];
 #pragma unroll
@@ -150,17 +178,17 @@ __device__ __forceinline__ void load_row(const void* pool, const float* scales, 
     }
 }
 
-template <bool F32>
-__device__ __forceinline__ void store8(void* base, int64_t elem, const float (&x)[8]) {
+template <int D, bool F32>
+__device__ __forceinline__ void store8(void* base, int64_t row, int lane, const float (&x)[8]) {
     if constexpr (F32) {
-        float* p = static_cast<float*>(base) + elem;
+        float* p = static_cast<float*>(base) + row + 4 * lane;
         put(p, f32x4{x[0], x[1], x[2], x[3]});
-        put(p + 4, f32x4{x[4], x[5], x[6], x[7]});
+        put(p + kApart<D, F32>, f32x4{x[4], x[5], x[6], x[7]});
     } else {
         u32x4 y;
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
-        put(static_cast<uint16_t*>(base) + elem, y);
+        put(static_cast<uint16_t*>(base) + row + 8 * lane, y);
     }
 }
 
@@ -176,12 +204,12 @@ __global__ void __launch_bounds__(kCacheThreads) cache_read_kernel(CacheReadArgs
         const int id = page_of(a.pages, b, static_cast<int>(t));
         if (id >= 0) {
             const int64_t row = pool_row(a.pages, a.Hkv, c, id, static_cast<int>(t));
-            load_row<TYPE>(a.pages.k, a.pages.k_scale, row, LANES, lane, k);
-            load_row<TYPE>(a.pages.v, a.pages.v_scale, row, LANES, lane, v);
+            load_row<D, TYPE, F32>(a.pages.k, a.pages.k_scale, row, lane, k);
+            load_row<D, TYPE, F32>(a.pages.v, a.pages.v_scale, row, lane, v);
         }
     }
-    store8<F32>(a.k, b * a.ksb + c * a.ksh + t * a.kst + 8 * lane, k);
-    store8<F32>(a.v, b * a.vsb + c * a.vsh + t * a.vst + 8 * lane, v);
+    store8<D, F32>(a.k, b * a.ksb + c * a.ksh + t * a.kst, lane, k);
+    store8<D, F32>(a.v, b * a.vsb + c * a.vsh + t * a.vst, lane, v);
 }
 
 // A group of lanes for each row of each head.

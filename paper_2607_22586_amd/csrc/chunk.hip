@@ -351,15 +351,18 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         if (half == 0) a.part_ml[pr] = make_float2(m, l);
         return;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    // (by selects: the sums of a row without weight may hold NaN, of 0 or 1 times an infinite V of its tiles)
+    const bool none = l == 0.f;
+    const float inv = 1.f / l;
     uint16_t* out = a.out + b * a.osb + h * a.osh + i * a.ost + 4 * half;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-            *reinterpret_cast<u32x2*>(out + 32 * t + 8 * w) =
-                u32x2{pack_bf16(o[t][4 * w] * inv, o[t][4 * w + 1] * inv),
-                      pack_bf16(o[t][4 * w + 2] * inv, o[t][4 * w + 3] * inv)};
+        for (int w = 0; w < 4; ++w) {
+            const u32x2 y{pack_bf16(o[t][4 * w] * inv, o[t][4 * w + 1] * inv),
+                          pack_bf16(o[t][4 * w + 2] * inv, o[t][4 * w + 3] * inv)};
+            *reinterpret_cast<u32x2*>(out + 32 * t + 8 * w) = none ? u32x2{0u, 0u} : y;
+        }
 }
 
 // ---- few rows -----------------------------------------------------------
@@ -814,11 +817,12 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
             *reinterpret_cast<float4*>(po + 4) = make_float4(x[4], x[5], x[6], x[7]);
             if (d0 == 0) a.part_ml[pr] = make_float2(M, L);
         } else {
-            const float inv = L > 0.f ? 1.f / L : 0.f;
+            const float inv = 1.f / L;
             const int h = c * a.Gh + (r - i * a.Gh);
             u32x4 v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = pack_bf16(x[2 * j] * inv, x[2 * j + 1] * inv);
+            if (L == 0.f) v = u32x4{0u, 0u, 0u, 0u};       // (x may hold NaN, as in chunk_kernel)
             *reinterpret_cast<u32x4*>(a.out + b * a.osb + h * a.osh + i * a.ost + d0) = v;
         }
     }

@@ -1,0 +1,53 @@
+"""Values at the ends of their range in the attention over a paged cache: infinities and NaN, sums near the
+largest number, scales of every kind, against plain 64-bit forms (tests/paged.py)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged
+from paper_2607_22586_amd import binding as bd
+from test_gpu_cache import BF16, DEV, E4M3, F32, I8, KINDS, _gpu, check_attention, i32, make_cache, rnd  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# (Hq, Hkv, T, n): rows of a head on the few-row kernel and on the staged one, over keys of one split and of
+# many (they are more than the rows of a workgroup can walk before a join pays)
+SPLITS = [(4, 2, 200, 2), (4, 2, 5000, 2), (8, 2, 200, 40), (8, 2, 5000, 40)]
+
+
+def attend(cache, q, lens, q_counts=None, causal=True, T=None):
+    print("attend", tuple(q.shape), cache.k.dtype, tuple(cache.k.shape), flush=True)
+    return bd.chunk_attention(q.to(DEV), cache, i32(lens), None if q_counts is None else i32(q_counts), T=T,
+                              causal=causal).cpu().float()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,T,n", SPLITS)
+def test_rows_that_are_not_there_beside_infinite_values(Hq, Hkv, T, n, causal):
+    """Zeros for queries behind a sequence's count, whatever the rows of V that others see hold."""
+    cache = make_cache(2, Hkv, T, 64, BF16, 64)
+    k, v = (rnd(s, 2, Hkv, T, 64) for s in (1, 2))
+    v[:, :, 3, 5], v[:, :, 70, 6], v[:, :, 71, 7] = math.inf, -math.inf, math.nan
+    bd.cache_write(cache, k.to(DEV), v.to(DEV))
+    counts = [n - 1, 0]
+    got = attend(cache, rnd(3, 2, Hq, n, 64, dtype=BF16), [[T] * Hkv] * 2, counts, causal, T)
+    assert (got[0, :, n - 1:] == 0).all() and (got[1] == 0).all()
+    there = got[0, :, :n - 1]
+    assert (there[..., 5] == math.inf).all() and (there[..., 6] == -math.inf).all()
+    assert torch.isnan(there[..., 7]).all()
+    assert torch.isfinite(there[..., :5]).all() and torch.isfinite(there[..., 8:]).all()
+
+
+@pytest.mark.parametrize("Hq,n", [(2, 10), (2, 70)])
+def test_queries_that_see_nothing_beside_infinite_values(Hq, n):
+    """Fewer rows than queries: the first queries see none, also where the rows of the others hold infinities."""
+    cache = make_cache(1, 1, 64, 64, BF16, 64)
+    k, v = (rnd(s, 1, 1, 3, 64) for s in (1, 2))
+    v[..., 0, 5], v[..., 0, 6] = math.inf, math.nan
+    bd.cache_write(cache, k.to(DEV), v.to(DEV))
+    got = attend(cache, rnd(3, 1, Hq, n, 64, dtype=BF16), [[3]])
+    assert (got[:, :, :n - 3] == 0).all()
+    assert (got[:, :, n - 3:, 5] == math.inf).all() and torch.isnan(got[:, :, n - 3:, 6]).all()
+    assert torch.isfinite(got[:, :, n - 3:, 7:]).all()

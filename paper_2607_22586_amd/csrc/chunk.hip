@@ -870,7 +870,7 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
         for (int e = 0; e < 8; ++e) o[e] *= f0;
 #pragma unroll
         for (int j = 0; j < kJoinPer; ++j) {
-            const bool any = v[j].y > 0.f;             // a split that saw no key leaves m only
+            const bool any = v[j].y != 0.f;            // a split that saw no key leaves m only (a NaN sum is kept)
             const float f = any ? fast_exp2(v[j].x - m) : 0.f;
             const float z[8] = {x[j].x, x[j].y, x[j].z, x[j].w, y[j].x, y[j].y, y[j].z, y[j].w};
             l = fmaf(v[j].y, f, l);
@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
         }
     }
     if (row >= rows) return;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l != 0.f ? 1.f / l : 0.f;        // (no split saw a key: o is 0 too)
     const int bc = static_cast<int>(row / a.rows), r = static_cast<int>(row - static_cast<int64_t>(bc) * a.rows);
     const int b = bc / a.Hkv, c = bc - b * a.Hkv, i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
     u32x4 v;

@@ -51,3 +51,18 @@ def test_queries_that_see_nothing_beside_infinite_values(Hq, n):
     assert (got[:, :, :n - 3] == 0).all()
     assert (got[:, :, n - 3:, 5] == math.inf).all() and torch.isnan(got[:, :, n - 3:, 6]).all()
     assert torch.isfinite(got[:, :, n - 3:, 7:]).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,T,n", SPLITS)
+def test_a_nan_key_is_seen_through_splits(Hq, Hkv, T, n):
+    """NaN in a key that the queries see, or in a query, makes their results NaN, however the keys are split,
+    and leaves the other heads' as they are."""
+    cache = make_cache(1, Hkv, T, 64, BF16, 64)
+    k, v = (rnd(s, 1, Hkv, T, 64) for s in (1, 2))
+    k[0, 1, 17, 9] = math.nan
+    bd.cache_write(cache, k.to(DEV), v.to(DEV))
+    q = rnd(3, 1, Hq, n, 64, dtype=BF16)
+    q[0, 0, n - 1, 3] = math.nan
+    got = attend(cache, q, [[T] * Hkv], causal=False, T=T)
+    assert torch.isnan(got[:, Hq // 2:]).all() and torch.isnan(got[:, 0, n - 1]).all()
+    assert torch.isfinite(got[:, 1:Hq // 2]).all() and torch.isfinite(got[:, 0, :n - 1]).all()

@@ -66,3 +66,50 @@ def test_a_nan_key_is_seen_through_splits(Hq, Hkv, T, n):
     got = attend(cache, q, [[T] * Hkv], causal=False, T=T)
     assert torch.isnan(got[:, Hq // 2:]).all() and torch.isnan(got[:, 0, n - 1]).all()
     assert torch.isfinite(got[:, 1:Hq // 2]).all() and torch.isfinite(got[:, 0, :n - 1]).all()
+
+
+def close_bound(cache, q, lens):
+    """(out, bound) in 64 bits without a causal limit, of an attention whose weights are rounded once and
+    divided by the sum of what they were rounded to.  With p (1 + e), |e| <= u = 2^-8 (bf16), the quotient is
+    off by sum p e (v - o) / sum p (1 + e), at most u / (1 - u) sum p |v - o| (p normalised): a rounding that
+    all weights share falls out, and of one heavy weight what is left of it.  Beside it the result's own
+    rounding, u |o|, and the fp32 terms of tests/paged.py, here `rel`, times sum p |v|."""
+    q = q.double().numpy()
+    B, Hq, n, d = q.shape
+    Hkv = cache.k.shape[1]
+    out, tol = np.zeros_like(q), np.zeros_like(q)
+    for b in range(B):
+        for c in range(Hkv):
+            m = lens[b][c]
+            k, v = paged.cached_rows(cache, b, c, m)
+            for h in range(c * (Hq // Hkv), (c + 1) * (Hq // Hkv)):
+                x = q[b, h] @ k.T / math.sqrt(d)
+                size = np.abs(q[b, h]) @ np.abs(k).T / math.sqrt(d)
+                p = np.exp(x - x.max(1, keepdims=True))
+                p /= p.sum(1, keepdims=True)
+                o = p @ v
+                apart = np.stack([pi @ np.abs(v - oi) for pi, oi in zip(p, o)])
+                rel = 2 * ((d + 4) * paged.U32 * size.max(1) + 2 * paged.U32) + 2 * m * paged.U32
+                out[b, h] = o
+                tol[b, h] = paged.U16 * np.abs(o) + paged.U16 / (1 - paged.U16) * apart \
+                    + 1.01 * rel[:, None] * (p @ np.abs(v))
+    return out, tol
+
+
+@pytest.mark.parametrize("kind", [BF16, E4M3])
+@pytest.mark.parametrize("B,Hq,Hkv,T,n", [(2, 28, 4, 321, 1), (8, 64, 32, 1111, 1), (8, 96, 32, 700, 10),
+                                          (1, 8, 2, 3000, 5), (1, 8, 2, 321, 40),
+                                          (1, 8, 2, 3000, 40)])
+def test_weights_and_their_sum_are_rounded_alike(kind, B, Hq, Hkv, T, n):
+    """Peaked rows (queries of standard deviation 4): the heaviest weight's rounding cancels in the quotient.
+    (Not of int8 rows: their weights are rounded with the scale of V.)"""
+    d = 128
+    cache = make_cache(B, Hkv, T, d, kind, 64)
+    k, v = (rnd(s, B, Hkv, T, d) for s in (1, 2))
+    bd.cache_write(cache, k.to(DEV), v.to(DEV))
+    q = (4 * rnd(3, B, Hq, n, d)).to(BF16)
+    got = attend(cache, q, [[T] * Hkv] * B, causal=False, T=T).double().numpy()
+    want, tol = close_bound(cache, q, [[T] * Hkv] * B)
+    off = np.abs(got - want)
+    print("relative 2-norm", np.linalg.norm(off) / np.linalg.norm(want), flush=True)
+    assert (off <= tol).all(), (off / tol).max()

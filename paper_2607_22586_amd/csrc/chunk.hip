@@ -31,11 +31,13 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 32 * kWaves;         // query rows of a workgroup
 constexpr int kKeys = 64;                  // keys of a tile
 constexpr float kNone = -3e38f;            // running maximum before the first visible key
-// The reference m of a row's sums need not be its maximum, only near it: it moves
-// where a lane's 16 (few rows: 8 or 16) weights add up to this, so that no maximum
-// is formed in most tiles and the output is seldom rescaled.  The sums are at most
-// this much larger than they would be relative to the maximum.
-constexpr float kBehind = 0x1p8f;
+// The reference m of a row's sums need not be its maximum, only near it: it moves,
+// to kLead above the largest logit so far, where a lane's 16 (few rows: 8 or 16)
+// weights 2^(x - m) add up to kBehind, so that no maximum is formed in most tiles
+// and the output is seldom rescaled.  The lead is what the largest logit may gain
+// before that: no weight is above 1, and the sums are in range wherever those
+// relative to the maximum itself are (without it they were up to 2^8 times larger).
+constexpr float kLead = 8.f, kBehind = 1.f;
 
 __device__ __forceinline__ floatx16 mfma32(bf16x8 a, bf16x8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
                 float mx = kNone;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, logit(u, e, 0.f));
-                mx = fmaxf(half_max(mx), m);
+                mx = fmaxf(half_max(mx) + kLead, m);
                 const float f = fast_exp2(m - mx);
                 m = mx;
                 l *= f;
@@ -745,7 +747,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
                 for (int u = 0; u < NS; ++u)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[x][u][e]);
-                mx = fmaxf(quarter_max(mx) * a.scale, m[x]);
+                mx = fmaxf(quarter_max(mx) * a.scale + kLead, m[x]);
                 const float f = fast_exp2(m[x] - mx);
                 m[x] = mx;
                 l[x] *= f;

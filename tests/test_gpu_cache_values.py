@@ -113,3 +113,20 @@ def test_weights_and_their_sum_are_rounded_alike(kind, B, Hq, Hkv, T, n):
     off = np.abs(got - want)
     print("relative 2-norm", np.linalg.norm(off) / np.linalg.norm(want), flush=True)
     assert (off <= tol).all(), (off / tol).max()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("B,Hq,Hkv,n", [(16, 16, 16, 1), (16, 64, 16, 8), (8, 64, 16, 40)])
+def test_sums_of_large_values_stay_in_range(kind, B, Hq, Hkv, n):
+    """Values of 2^116 under weights that grow once, after the first keys of every wave, by 2^3.7: sums relative
+    to the largest weight are 2^10.3 times a value, which fp32 holds; relative to the first keys' weight they
+    would be 2^13.9 times it, which fp32 does not."""
+    T, d = 1500, 64
+    cache = make_cache(B, Hkv, T, d, kind, 64)
+    v = rnd(2, B, Hkv, 1, d).sign().expand(B, Hkv, T, d) * 2.0 ** 116
+    k = torch.zeros(B, Hkv, T, d)
+    k[:, :, 512:, 0] = 5.125
+    bd.cache_write(cache, k.to(DEV), v.to(DEV))
+    q = torch.zeros(B, Hq, n, d)
+    q[..., 0] = 4.0
+    check_attention(cache, q.to(BF16), [[T] * Hkv] * B, causal=False, T=T)

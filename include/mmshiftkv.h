@@ -395,10 +395,10 @@ int mmshiftkv_shape_scores(const mmskv_shape *shape, int32_t kind, int32_t windo
  * Row t of (b, c) is row t % page of page p = table[b * max_pages + t / page]:
  * element ((p * Hkv + c) * page + t % page) * d + j of k (and v), and, in the
  * 8-bit types, scale (p * Hkv + c) * page + t % page.  A row stands for its
- * values times its scale; the scales of MMSKV_E4M3 are powers of two of 2^-126
- * to 2^120 (what mmshiftkv_cache_write makes them; others give unspecified
- * results).  Sequences may share pages that are only read; a row
- * that two entries of one write name is written by both, in no order.  Entries
+ * values times its scale, a finite number; mmshiftkv_cache_write makes those of
+ * MMSKV_E4M3 powers of two, in which every call is exact (2^-126 to 2^120).
+ * Sequences may share pages that are only read; a row that two entries of one
+ * write name is written by both, in no order.  Entries
  * outside [0, n_pages) name no page: their rows are not written, and are zero
  * when they are read or attended to.
  *   k, v              [n_pages, Hkv, page, d] dtype, 16-byte aligned
@@ -460,10 +460,11 @@ int mmshiftkv_cache_read(const mmskv_shape *shape, const mmskv_pages *pages, con
  *   out[b,h,i,:] = sum_t p_t v_t,  p = softmax over the rows it sees of
  *                  q . k_t / sqrt(d)
  * with k, v the cached values times their scales.  bf16 products (exact for
- * the 8-bit values; the scales are applied in fp32 to the logits and to p),
- * fp32 accumulation and softmax, p rounded to bf16 for its product with v,
- * the result rounded once.  A query that sees no row gives zeros, and so do
- * the rows i >= nq of out.
+ * the 8-bit values), fp32 accumulation and softmax, p rounded to bf16 for its
+ * product with v, the result rounded once.  The scales are applied in fp32 to
+ * the logits and to p; those of MMSKV_E4M3, where Gh * n > 64, to the values:
+ * powers of two exactly, products with others are rounded to bf16.
+ * A query that sees no row gives zeros, and so do the rows i >= nq of out.
  * Reads shape->B, Hq, Hkv, T (an upper bound of lens, which fixes how the work
  * is split) and d; W is ignored.  Gh * n and B * Hkv up to 2^22 (more
  * -> MMSKV_EUNSUPPORTED).

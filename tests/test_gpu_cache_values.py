@@ -130,3 +130,36 @@ def test_sums_of_large_values_stay_in_range(kind, B, Hq, Hkv, n):
     q = torch.zeros(B, Hq, n, d)
     q[..., 0] = 4.0
     check_attention(cache, q.to(BF16), [[T] * Hkv] * B, causal=False, T=T)
+
+
+@pytest.mark.parametrize("Hq,Hkv,T,n", SPLITS + [(4, 1, 77, 20)])
+def test_e4m3_rows_of_any_scale(Hq, Hkv, T, n):
+    """Scales that are no powers of two, as another program may have quantised its rows.  A value times its
+    scale is rounded to bf16 where the staged kernel takes it: u |q| |k| more in a logit (p off by twice that,
+    as in tests/paged.py), u sum p |v| more in the result; only in part of the rows' tiles."""
+    d = 64
+    cache = make_cache(1, Hkv, T, d, E4M3, 16)
+    gen = torch.Generator().manual_seed(T + n)
+    shape = tuple(cache.k.shape)
+    for x, s, size in ((cache.k, cache.k_scale, 0.5), (cache.v, cache.v_scale, 3.0)):
+        x.copy_((torch.randn(shape, generator=gen) * 16).to(E4M3).to(DEV))
+        s.copy_((size / 16 * torch.exp2(2 * torch.rand(shape[:3], generator=gen) - 1)).to(DEV))
+    s = cache.k_scale                              # a third of the pages as cache_write leaves them
+    s[::3] = torch.exp2(torch.floor(torch.log2(s[::3])))
+    q = (0.5 * rnd(3, 1, Hq, n, d)).to(BF16)
+    lens = [[T] * Hkv]
+    got = attend(cache, q, lens, T=T).double().numpy()
+    want, tol = paged.attention(cache, q, torch.as_tensor(lens), None, True)
+    for c in range(Hkv):
+        k, v = paged.cached_rows(cache, 0, c, T)
+        for h in range(c * (Hq // Hkv), (c + 1) * (Hq // Hkv)):
+            size = np.abs(q[0, h].double().numpy()) @ np.abs(k).T / math.sqrt(d)
+            x = q[0, h].double().numpy() @ k.T / math.sqrt(d)
+            x = np.where(np.arange(T)[None] <= T - n + np.arange(n)[:, None], x, -np.inf)
+            p = np.exp(x - x.max(1, keepdims=True))
+            weight = (p / p.sum(1, keepdims=True)) @ np.abs(v)
+            # (e^y - 1 <= y e^y)
+            y = 2 * paged.U16 * size.max(1)[:, None]
+            tol[0, h] += (paged.U16 + y * np.exp(y)) * 1.02 * weight
+    off = np.abs(got - want)
+    assert (off <= tol).all(), (off / tol).max()

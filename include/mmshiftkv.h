@@ -427,7 +427,9 @@ typedef struct {
  *               a <= 448 * 2^e; y = e4m3(x / 2^e): a power of two costs a
  *               float type no precision, and the division is exact
  *   MMSKV_I8    a' = max(a, 2^-100), scale a' / 127, y = rint(x * (127 / a'))
- * every rounding to nearest even.
+ * every rounding to nearest even.  An infinity or NaN of the source: MMSKV_BF16
+ * keeps it, MMSKV_E4M3 has NaN in its place (beside an infinity the row's other
+ * values are rounded to multiples of 2^111), an MMSKV_I8 row is NaN as a whole.
  * Reads shape->B, Hkv, T and d (64 or 128); Hq and W are ignored.  n up to 2^27
  * (more -> MMSKV_EUNSUPPORTED).
  *   k, v    [B, Hkv, T, d] dtype (fp32 or bf16), strides k_strides / v_strides

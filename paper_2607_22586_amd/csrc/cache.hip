@@ -38,18 +38,27 @@ __device__ __forceinline__ void load8(const void* base, int64_t elem, float (&x)
     }
 }
 
-// Maximum over groups of 8 or 16 lanes: neighbours, pairs, then mirrored quads and
+// The larger of two magnitudes.  An e4m3 row holds its NaN in their places and the
+// scale is of the others; int8 has no place for one, so that its scale is to be NaN:
+// as whole numbers NaN is above infinity.
+template <int TYPE>
+__device__ __forceinline__ float larger(float x, float y) {
+    if constexpr (TYPE == kCacheI8) return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y)));
+    else return fmaxf(x, y);
+}
+
+// Largest of groups of 8 or 16 lanes: neighbours, pairs, then mirrored quads and
 // octets.
-template <int LANES>
+template <int TYPE, int LANES>
 __device__ __forceinline__ float group_max(float x) {
     const auto moved = [](float v, auto ctrl) {
         const int b = static_cast<int>(__float_as_uint(v));
         return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_update_dpp(b, b, decltype(ctrl)::value, 0xF, 0xF, false)));
     };
-    x = fmaxf(x, moved(x, Constant<0xB1>{}));     // quad_perm [1, 0, 3, 2]
-    x = fmaxf(x, moved(x, Constant<0x4E>{}));     // quad_perm [2, 3, 0, 1]
-    x = fmaxf(x, moved(x, Constant<0x141>{}));    // row_half_mirror
-    if constexpr (LANES == 16) x = fmaxf(x, moved(x, Constant<0x140>{}));     // row_mirror
+    x = larger<TYPE>(x, moved(x, Constant<0xB1>{}));     // quad_perm [1, 0, 3, 2]
+    x = larger<TYPE>(x, moved(x, Constant<0x4E>{}));     // quad_perm [2, 3, 0, 1]
+    x = larger<TYPE>(x, moved(x, Constant<0x141>{}));    // row_half_mirror
+    if constexpr (LANES == 16) x = larger<TYPE>(x, moved(x, Constant<0x140>{}));     // row_mirror
     return x;
 }
 
@@ -65,7 +74,7 @@ __device__ __forceinline__ float row_scale(float a, float* mul) {
         *mul = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
         return __uint_as_float(static_cast<uint32_t>(e) << 23);
     } else {
-        a = fmaxf(a, 0x1p-100f);                 // (the inverse stays finite, a row of zeros is zero)
+        a = a < 0x1p-100f ? 0x1p-100f : a;       // (the inverse stays finite, a row of zeros is zero; NaN stays)
         *mul = 127.f / a;
         return a / 127.f;
     }
@@ -83,8 +92,8 @@ __device__ __forceinline__ void store_row(void* pool, float* scales, int64_t row
     } else {
         float a = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) a = fmaxf(a, fabsf(x[j]));
-        a = group_max<LANES>(a);
+        for (int j = 0; j < 8; ++j) a = larger<TYPE>(a, fabsf(x[j]));
+        a = group_max<TYPE, LANES>(a);
         float mul;
         const float scale = row_scale<TYPE>(a, &mul);
         u32x2 y;

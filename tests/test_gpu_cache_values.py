@@ -163,3 +163,34 @@ def test_e4m3_rows_of_any_scale(Hq, Hkv, T, n):
             tol[0, h] += (paged.U16 + y * np.exp(y)) * 1.02 * weight
     off = np.abs(got - want)
     assert (off <= tol).all(), (off / tol).max()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("src", [F32, BF16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_written_infinities_and_nan(kind, src, d, bad):
+    """No source row with an infinity or NaN reads back as numbers: bf16 keeps it in its place, e4m3 holds NaN
+    there, an int8 row is NaN as a whole; rows beside it are as without it."""
+    k, v = (rnd(s, 1, 2, 40, d).to(src) for s in (1, 2))
+    k0, v0 = k.clone(), v.clone()
+    at = [(0, 3, 5), (0, 17, d - 1), (1, 39, 0)]   # head, row, element
+    for x in (k, v):
+        for c, t, j in at:
+            x[0, c, t, j] = bad
+    lens = i32([[40, 40]])
+    caches = [make_cache(1, 2, 40, d, kind, 16) for _ in range(2)]
+    bd.cache_write(caches[0], k.to(DEV), v.to(DEV))
+    bd.cache_write(caches[1], k0.to(DEV), v0.to(DEV))
+    for got, want, x in zip(*(bd.cache_read(c, lens, 40, F32) for c in caches), (k, v)):
+        got, want = got.cpu(), want.cpu()
+        rows = torch.zeros(2, 40, dtype=torch.bool)
+        for c, t, j in at:
+            rows[c, t] = True
+            if kind == I8:
+                assert torch.isnan(got[0, c, t]).all()
+            elif kind == E4M3:
+                assert torch.isnan(got[0, c, t, j]) and torch.isnan(got[0, c, t]).sum() == 1
+            else:
+                assert torch.equal(got[0, c, t].nan_to_num(7e30), x[0, c, t].to(BF16).float().nan_to_num(7e30))
+        assert torch.equal(got[0][~rows], want[0][~rows])

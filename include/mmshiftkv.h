@@ -407,7 +407,10 @@ int mmshiftkv_shape_scores(const mmskv_shape *shape, int32_t kind, int32_t windo
  *   page              rows of a page: a power of two, 16..1024
  *   dtype             MMSKV_BF16, MMSKV_E4M3 or MMSKV_I8
  * (others -> MMSKV_EUNSUPPORTED).  Rows that nothing has written may hold any
- * bits, NaN included: no call reads behind the lengths that it is given. */
+ * bits, NaN included, and so may table entries behind a sequence's rows: nothing
+ * behind the lengths that a call is given enters its results.  It may be read,
+ * though (rows to the end of a tile of 64, all max_pages entries of the table),
+ * and has to be memory of the pools and of the table. */
 typedef struct {
     void *k, *v;
     float *k_scale, *v_scale;
@@ -467,6 +470,10 @@ int mmshiftkv_cache_read(const mmskv_shape *shape, const mmskv_pages *pages, con
  * the logits and to p; those of MMSKV_E4M3, where Gh * n > 64, to the values:
  * powers of two exactly, products with others are rounded to bf16.
  * A query that sees no row gives zeros, and so do the rows i >= nq of out.
+ * Sums are divided last: a result is finite where the rows that it sees, times
+ * the largest |v|, are below 2^127.  An infinity or NaN in a row's k is seen by
+ * the queries that see the row; one in v may also reach, as 0 times it, queries
+ * of the same sequence before that row.
  * Reads shape->B, Hq, Hkv, T (an upper bound of lens, which fixes how the work
  * is split) and d; W is ignored.  Gh * n and B * Hkv up to 2^22 (more
  * -> MMSKV_EUNSUPPORTED).

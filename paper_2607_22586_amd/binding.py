@@ -760,7 +760,8 @@ def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_co
     """mmshiftkv_chunk_attention: the outputs [B, Hq, n, d] bf16 of the chunk's queries q [B, Hq, n, d]
     bf16 (n = 1: a decoding step) over the first lens[b, c] cached rows of each head, the chunk's own
     among them; q_counts[b] (None: n) queries of sequence b are there.  T is an upper bound of lens
-    (None: what the table can hold).  The result is laid out as q is unless `out` is given."""
+    (None: what the table can hold).  The result is laid out as q is unless `out` is given.  A chunk of
+    some sequences and single tokens of others are faster as two calls: n fixes how all are worked on."""
     i = _same_device(q, cache.k, lens, q_counts, workspace, out)
     if q.dtype != torch.bfloat16:
         raise TypeError("q is bf16")

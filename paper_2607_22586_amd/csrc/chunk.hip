@@ -53,16 +53,17 @@ __device__ __forceinline__ float half_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// sum + the two bf16 values of y, by one instruction.  The sum of a row's weights
-// is of the weights as the product with V takes them, rounded to bf16, so that the
-// quotient does not hold what their roundings have in common, nearly all of a heavy
-// weight's: 1111 bf16 rows, queries of standard deviation 4, results off by 0.0018
-// of their 2-norm (their own rounding: 0.0017), with the sum of the unrounded
-// weights by 0.0020.  (Against two additions of these: e4m3 chunks 0.5% faster, bf16
-// ones 1 to 2% slower.)  int8 weights are rounded with the scale of V, which the
-// sum has no part in: 0.0023 to 0.0025; rounding a value to int8 costs more.
+// sum + the two bf16 values of y, by one instruction (DOT) or two additions.  The
+// sum of a row's weights is of the weights as the product with V takes them, rounded
+// to bf16, so that the quotient does not hold what their roundings have in common,
+// nearly all of a heavy weight's: 1111 bf16 rows, queries of standard deviation 4,
+// results off by 0.0018 of their 2-norm (their own rounding: 0.0017), with the sum of
+// the unrounded weights by 0.0020.  (int8 weights are rounded with the scale of V,
+// which the sum has no part in: 0.0023 to 0.0025; rounding a value to int8 costs more.)
+template <bool DOT = true>
 __device__ __forceinline__ float add_pair(uint32_t y, float sum) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    if constexpr (!DOT) return sum + (__uint_as_float(y << 16) + __uint_as_float(y & 0xFFFF0000u));
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, y), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum,
                                            false);
 }
@@ -294,7 +295,9 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
                 }
             }
             const uint32_t y = pack_bf16(x[0], x[1]);
-            if (!kScaled) sum = add_pair(y, sum);
+            // (2048 queries over 32768 rows, additions / one instruction: bf16 2080 / 2150 us,
+            // e4m3 2012 / 1993)
+            if (!kScaled) sum = add_pair<TYPE != kCacheBf16>(y, sum);
             return y;
         };
         // m moved where half u leaves it behind

@@ -132,12 +132,12 @@ def test_sums_of_large_values_stay_in_range(kind, B, Hq, Hkv, n):
     check_attention(cache, q.to(BF16), [[T] * Hkv] * B, causal=False, T=T)
 
 
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("Hq,Hkv,T,n", SPLITS + [(4, 1, 77, 20)])
-def test_e4m3_rows_of_any_scale(Hq, Hkv, T, n):
+def test_e4m3_rows_of_any_scale(Hq, Hkv, T, n, d):
     """Scales that are no powers of two, as another program may have quantised its rows.  A value times its
     scale is rounded to bf16 where the staged kernel takes it: u |q| |k| more in a logit (p off by twice that,
     as in tests/paged.py), u sum p |v| more in the result; only in part of the rows' tiles."""
-    d = 64
     cache = make_cache(1, Hkv, T, d, E4M3, 16)
     gen = torch.Generator().manual_seed(T + n)
     shape = tuple(cache.k.shape)

@@ -14,9 +14,13 @@
 // (both products run over the keys in the order of the accumulator's rows); V^T
 // comes from the staged rows by transposing LDS reads.
 // What bounds it: the matrix pipe and the exponentials by turns, two waves a SIMD
-// (236 registers, 64 KB of LDS a workgroup).  2048 queries of 64 heads of 128 on 8
-// over 32768 rows reach 1060 TFLOP/s from e4m3, 1020 from bf16 and 900 from int8
-// rows, where a bf16 product of 8192 x 8192 x 8192 reaches 1230 on this card.
+// (d = 128: 238 registers for bf16 rows, 229 for e4m3, all 256 for int8, which keeps
+// 48 bytes a lane in scratch; 64 KB of LDS a workgroup, int8 65).  2048 queries of 64
+// heads of 128 on 8 over 32768 rows reach 1050 to 1070 TFLOP/s from e4m3, 1010 to 1030
+// from bf16 and 900 from int8 rows (96 conversions and packs and 32 products with V's
+// scales a lane and tile, where e4m3 has 32 conversions); a bf16 product of 8192 x 8192
+// x 8192 reaches 1230 on this card.  1024 queries of 28 heads on 4 over 16384 rows,
+// batch 4, reach 970, 945 and 820: 896 workgroups on 512 places.
 #include "pages.hpp"
 
 namespace mmskv {
@@ -1000,7 +1004,8 @@ hipError_t launch(const ChunkArgs& a, hipStream_t s) {
     else attend<D, kCacheI8>(a, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    // one round of loads of a row's splits (16 groups at most: two rounds above 128 splits)
+    // a row's splits in one round of loads (kMaxSplits: four of the eight places of 16
+    // groups; eight groups took the same time)
     const auto join = [&](auto groups) {
         constexpr int SG = decltype(groups)::value, kPer = kJoinThreads / (D / 8 * SG);
         const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
@@ -1019,7 +1024,8 @@ namespace {
 
 constexpr int kFewBlocks = 4 * kPlanCus;   // workgroups of few rows, where there are splits
 
-// Splits for few rows.  A workgroup has a CU for itself, so that the launch takes
+// Splits for few rows.  A workgroup has a CU for itself (its LDS; for d = 64 in 8 bits
+// and up to 32 rows two fit, which is not priced), so that the launch takes
 // as many turns as there are workgroups per CU, each of them 2 us and the rounds
 // of its split (a tile for each of its waves); a join reads and writes what the
 // splits left beside 3 us for its launch.  (What memory takes for the keys is the
@@ -1051,8 +1057,9 @@ int few_splits(int64_t heads, int rows, int T, int d, int dtype) {
 
 // Splits for more rows.  In ns, as measured at d = 128 (64): a tile takes a
 // workgroup 1500 (950) with a CU to itself, 2000 (1250) beside another, which is
-// how they run from one per CU up to two; it begins within two tiles' time.  A
-// join reads and writes what the splits left (4 TB/s) beside 3000 for its launch.
+// how they run from one per CU up to two (of d = 64, but for int8, three fit, which
+// is not priced); it begins within two tiles' time.  A join reads and writes what the
+// splits left (4 TB/s) beside 3000 for its launch.
 // (1024 queries of 28 heads on 4 over 8191 rows, 224 row tiles: 197 us with 1 split,
 // 142 with 2, 154 with 3; 512 of 32 on 8 over 4096, 128: 98 / 67 / 60 / 56 / 60 us
 // with 1 / 2 / 3 / 4 / 6; 1024 of 32 on 8 over 1024, 256: 31 with 1, 40 with 2.)

@@ -488,6 +488,61 @@ int mmshiftkv_chunk_attention(const mmskv_shape *shape, const mmskv_pages *pages
                               int32_t n, int32_t causal, uint16_t *out, const mmskv_strides *out_strides,
                               void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Pages that several sequences hold.  refs[p] is the number of table
+ * entries that name page p; pages of 0 are free.  The three calls below keep
+ * them so, and write the table of `pages` (and refs, lens and the pools): what
+ * a sequence holds follows from numbers of rows that only the device knows
+ * (selections leave them there), so its pages are given and taken there, in
+ * calls that a graph may capture.  A call gives the lowest-numbered pages that
+ * were free before it, by sequence and within a sequence by entry; pages that
+ * it takes back are free from the next call on.  Where they do not suffice, the
+ * sequence gets none, nor does any behind it that wants some: missing[b] is the
+ * number that sequence b wanted and did not get, else 0.
+ *   refs     [n_pages] int32, in and out
+ *   missing  [B] int32 out
+ * They read shape->B, Hkv and d; B * max_pages up to 2^28 (more
+ * -> MMSKV_EUNSUPPORTED).  Workspace: mmshiftkv_cache_book_workspace bytes
+ * (256-byte aligned; 0 for invalid sizes; never falls as B, Hkv, n_pages or
+ * max_pages grows), without clearing; calls that may overlap in time need
+ * workspaces of their own. */
+size_t mmshiftkv_cache_book_workspace(const mmskv_shape *shape, int32_t n_pages, int32_t max_pages);
+
+/* Holds the pages for max over c of rows[b,c] rows of each sequence, as many as
+ * the table's row can name: entries below that which name none get a page
+ * (whose rows hold anything), entries behind it become -1 and their pages are
+ * taken back, also of a sequence that gets none (0 rows: all are).
+ *   rows  [B, Hkv] int32 */
+int mmshiftkv_cache_hold(const mmskv_shape *shape, const mmskv_pages *pages, int32_t *refs, const int32_t *rows,
+                         int32_t *missing, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Makes sequence b a copy of sequence src[b] as that was before the call, all b
+ * at once (src may name a sequence that is itself replaced: the beams of a
+ * search).  With lens of the source: pages that all its heads have filled
+ * (entries below min over c of lens / page) are named by both from then on;
+ * those behind, to its longest head, are copied to new pages, the rows below
+ * lens of each head.  What b held is taken back, lens[b,:] becomes the source's;
+ * a sequence whose pages are missing stays as it was, and so do those of
+ * src[b] = b or outside [0, B).  Entries of the source that name none, and those
+ * behind its rows, are -1.  Rows of pages that are named twice must not be
+ * written; appending rows behind lens never does.
+ *   src   [B] int32;  lens  [B, Hkv] int32, in and out */
+int mmshiftkv_cache_fork(const mmskv_shape *shape, const mmskv_pages *pages, int32_t *refs, const int32_t *src,
+                         int32_t *lens, int32_t *missing, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Keeps some of the cached rows: row j < min(counts[b,c], n) of (b, c) becomes
+ * what row idx[b,c,j] was (the kept keys of a selection over the cached rows;
+ * any order, also twice; indices outside [0, lens[b,c]) and rows of entries that
+ * name no page give zeros with scale 1), bit for bit.  The rows go to new pages,
+ * so that sequences which share the old ones keep them; what b held is taken
+ * back and lens becomes the counts, clamped to [0, n].  A sequence whose pages
+ * are missing stays as it was, and so does one whose counts are all below 0.
+ * Rows that the table's row cannot name are dropped.
+ *   idx  [B, Hkv, n] int32;  counts [B, Hkv] int32 (may be lens itself)
+ *   lens [B, Hkv] int32, in and out; n up to 2^27 (more -> MMSKV_EUNSUPPORTED) */
+int mmshiftkv_cache_compact(const mmskv_shape *shape, const mmskv_pages *pages, int32_t *refs, int32_t *lens,
+                            const int32_t *idx, const int32_t *counts, int32_t n, int32_t *missing, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
 /* Human-readable text for an mmskv_status value (static storage). */
 const char *mmshiftkv_status_string(int status);
 

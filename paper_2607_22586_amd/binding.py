@@ -30,7 +30,9 @@ EXPORTED = ("mmshiftkv_build_proxies", "mmshiftkv_score_workspace", "mmshiftkv_s
             "mmshiftkv_hidden_proxies", "mmshiftkv_project_proxies", "mmshiftkv_decode_workspace",
             "mmshiftkv_decode_check", "mmshiftkv_window_rows", "mmshiftkv_shape_scores",
             "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
-            "mmshiftkv_chunk_attention_workspace", "mmshiftkv_chunk_attention")
+            "mmshiftkv_chunk_attention_workspace", "mmshiftkv_chunk_attention",
+            "mmshiftkv_cache_book_workspace", "mmshiftkv_cache_hold", "mmshiftkv_cache_fork",
+            "mmshiftkv_cache_compact")
 
 
 class Shape(ctypes.Structure):
@@ -113,6 +115,11 @@ def load_library(path: str | None = None):
     lib.mmshiftkv_chunk_attention_workspace.argtypes = [PS, I32]
     lib.mmshiftkv_chunk_attention_workspace.restype = SZ
     lib.mmshiftkv_chunk_attention.argtypes = [PS, PG, V, PT, V, V, I32, I32, V, PT, V, SZ, V]
+    lib.mmshiftkv_cache_book_workspace.argtypes = [PS, I32, I32]
+    lib.mmshiftkv_cache_book_workspace.restype = SZ
+    lib.mmshiftkv_cache_hold.argtypes = [PS, PG, V, V, V, V, SZ, V]
+    lib.mmshiftkv_cache_fork.argtypes = [PS, PG, V, V, V, V, V, SZ, V]
+    lib.mmshiftkv_cache_compact.argtypes = [PS, PG, V, V, V, V, I32, V, V, SZ, V]
     lib.mmshiftkv_status_string.argtypes = [ctypes.c_int]
     lib.mmshiftkv_status_string.restype = ctypes.c_char_p
     lib.mmshiftkv_version.restype = ctypes.c_int
@@ -123,7 +130,8 @@ def load_library(path: str | None = None):
                  "mmshiftkv_hidden_stats", "mmshiftkv_hidden_proxies", "mmshiftkv_project_proxies",
                  "mmshiftkv_decode_check", "mmshiftkv_window_rows", "mmshiftkv_shape_scores",
                  "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
-                 "mmshiftkv_chunk_attention"):
+                 "mmshiftkv_chunk_attention", "mmshiftkv_cache_hold", "mmshiftkv_cache_fork",
+                 "mmshiftkv_cache_compact"):
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
         _lib = lib
@@ -617,24 +625,40 @@ _CACHE_DTYPES = {torch.bfloat16: MMSKV_BF16, torch.float8_e4m3fn: MMSKV_E4M3, to
 class PagedCache:
     """Pages of K and V rows (mmskv_pages): k and v [n_pages, Hkv, page, d] as bfloat16,
     float8_e4m3fn or int8, the 8-bit ones with fp32 scales [n_pages, Hkv, page] (else None);
-    table [B, max_pages] int32, the pages of each sequence in order."""
+    table [B, max_pages] int32, the pages of each sequence in order; refs [n_pages] int32, the
+    entries of the table that name each page (only cache_hold, cache_fork and cache_compact read
+    and write them; None: pages that are never given or taken)."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor | None
     v_scale: torch.Tensor | None
     table: torch.Tensor
+    refs: torch.Tensor | None = None
 
     @classmethod
     def empty(cls, B: int, Hkv: int, T: int, d: int, dtype: torch.dtype = torch.bfloat16, page: int = 64,
               device="cuda:0") -> "PagedCache":
         """A cache of its own pages for B sequences of up to T rows (the rows are not cleared)."""
         per = max(1, -(-int(T) // page))
-        shape = (B * per, Hkv, page, d)
+        table = torch.arange(B * per, dtype=torch.int32, device=device).view(B, per)
+        return cls(*cls._pools(B * per, Hkv, page, d, dtype, device), table, torch.ones_like(table).view(-1))
+
+    @classmethod
+    def pool(cls, B: int, Hkv: int, n_pages: int, max_pages: int, d: int, dtype: torch.dtype = torch.bfloat16,
+             page: int = 64, device="cuda:0") -> "PagedCache":
+        """A cache of n_pages free pages that B sequences share, up to max_pages each (cache_hold)."""
+        return cls(*cls._pools(n_pages, Hkv, page, d, dtype, device),
+                   torch.full((B, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(n_pages, dtype=torch.int32, device=device))
+
+    @staticmethod
+    def _pools(n_pages, Hkv, page, d, dtype, device):
+        shape = (n_pages, Hkv, page, d)
         k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
         ks = vs = None
         if dtype != torch.bfloat16:
             ks, vs = (torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2))
-        return cls(k, v, ks, vs, torch.arange(B * per, dtype=torch.int32, device=device).view(B, per))
+        return k, v, ks, vs
 
     def c_pages(self) -> Pages:
         k, v, ks, vs, table = self.k, self.v, self.k_scale, self.v_scale, self.table
@@ -793,6 +817,69 @@ def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_co
     _enqueue("mmshiftkv_chunk_attention", i, shape, ref(pages), q.data_ptr(), ref(qs), q_counts, rows, n,
              1 if causal else 0, out.data_ptr(), ref(os), ws.data_ptr(), ws.numel() * ws.element_size())
     return out
+
+
+# ----------------------------------------------------------------------------
+# pages that several sequences hold
+# ----------------------------------------------------------------------------
+def cache_book_workspace(B, Hkv, n_pages, max_pages) -> int:
+    return int(load_library().mmshiftkv_cache_book_workspace(ctypes.byref(_shape(B, 0, Hkv, 0, 0, 0)), int(n_pages),
+                                                             int(max_pages)))
+
+
+def _book(name: str, cache: PagedCache, missing, workspace, *args):
+    """A call that changes the pages of `cache`; args: tensors ([B, ...] int32, contiguous) and numbers."""
+    tensors = [a for a in args if isinstance(a, torch.Tensor)]
+    i = _same_device(cache.k, cache.refs, missing, workspace, *tensors)
+    pages = cache.c_pages()
+    n_pages, Hkv, _, d = cache.k.shape
+    B, most = cache.table.shape
+    if cache.refs is None:
+        raise ValueError("the cache has no refs: its pages are not given or taken")
+    refs = _int32(cache.refs, (n_pages,), "refs")
+    if missing is None:
+        missing = cache.refs.new_empty((B,))
+    rows = _int32(missing, (B,), "missing")
+    ref = ctypes.byref
+    shape = ref(Shape(B, 0, Hkv, 0, 0, d))
+    ws = workspace
+    if ws is None:
+        ws = _ws(load_library().mmshiftkv_cache_book_workspace(shape, n_pages, most), cache.k.device)
+    _enqueue(name, i, shape, ref(pages), refs, *[_p(a) if isinstance(a, torch.Tensor) else a for a in args], rows,
+             ws.data_ptr(), ws.numel() * ws.element_size())
+    return missing
+
+
+def cache_hold(cache: PagedCache, rows: torch.Tensor, missing: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """mmshiftkv_cache_hold: each sequence holds the pages for max(rows[b]) rows (rows [B, Hkv] int32),
+    taken from the free ones or given back.  Returns missing [B] int32: the pages that it did not get."""
+    _int32(rows, (cache.table.shape[0], cache.k.shape[1]), "rows")
+    return _book("mmshiftkv_cache_hold", cache, missing, workspace, rows)
+
+
+def cache_fork(cache: PagedCache, src: torch.Tensor, lens: torch.Tensor, missing: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """mmshiftkv_cache_fork: sequence b becomes a copy of sequence src[b] (src [B] int32; b itself: it
+    stays) as that was before the call, sharing the pages that are full; lens [B, Hkv] int32 follows.
+    Returns missing [B] int32: the pages that it did not get (then it stays as it was)."""
+    B = cache.table.shape[0]
+    _int32(src, (B,), "src")
+    _int32(lens, (B, cache.k.shape[1]), "lens")
+    return _book("mmshiftkv_cache_fork", cache, missing, workspace, src, lens)
+
+
+def cache_compact(cache: PagedCache, lens: torch.Tensor, idx: torch.Tensor, counts: torch.Tensor,
+                  missing: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """mmshiftkv_cache_compact: the first counts[b, c] of the rows idx [B, Hkv, n] become the cached rows of
+    each head, on new pages, and lens [B, Hkv] follows (a Selected over the cached rows: its idx and counts;
+    all counts of a sequence below 0: it stays).  All int32.  Returns missing [B] int32, as cache_fork."""
+    shape = (cache.table.shape[0], cache.k.shape[1])
+    _int32(lens, shape, "lens")
+    _int32(counts, shape, "counts")
+    n = idx.shape[-1]
+    _int32(idx, shape + (n,), "idx")
+    return _book("mmshiftkv_cache_compact", cache, missing, workspace, lens, idx, counts, n)
 
 
 @dataclass

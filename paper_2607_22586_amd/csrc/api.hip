@@ -941,4 +941,101 @@ int mmshiftkv_chunk_attention(const mmskv_shape* shape, const mmskv_pages* pages
     return status_of(launch_chunk_attention(a, static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+
+constexpr int64_t kMaxEntries = 1 << 28;   // entries of a table whose changes are ranked
+
+int check_book(const mmskv_shape* s, const mmskv_pages* p, const void* refs, Pages* out) {
+    if (s == nullptr) return MMSKV_EINVAL;
+    if (s->B < 1 || s->B > 65535 || s->Hkv < 1 || s->Hkv > 65535 || s->d < 1) return MMSKV_EINVAL;
+    const int rc = check_pages(p, s->d, out);
+    if (rc) return rc;
+    if (refs == nullptr || !aligned(refs, 4)) return MMSKV_EINVAL;
+    if (static_cast<int64_t>(s->B) * p->max_pages > kMaxEntries) return MMSKV_EUNSUPPORTED;
+    return MMSKV_OK;
+}
+
+// The parts of the workspace, from `base` on; returns its bytes.
+size_t book_layout(int B, int Hkv, int n_pages, int max_pages, char* base, BookArgs* a) {
+    const size_t entries = static_cast<size_t>(B) * max_pages;
+    size_t at = 0;
+    const auto part = [&](size_t bytes) {
+        char* const p = base + at;
+        at += align_up(bytes);
+        return p;
+    };
+    a->taken = reinterpret_cast<int32_t*>(part(4));
+    a->want = reinterpret_cast<int32_t*>(part(4 * static_cast<size_t>(B)));
+    a->free = reinterpret_cast<int32_t*>(part(4 * static_cast<size_t>(book_chunks(n_pages))));
+    a->ids = reinterpret_cast<int32_t*>(part(4 * entries));
+    a->items = reinterpret_cast<int2*>(part(8 * entries));
+    a->old_table = reinterpret_cast<int32_t*>(part(4 * entries));
+    a->old_lens = reinterpret_cast<int32_t*>(part(4 * static_cast<size_t>(B) * Hkv));
+    return at;
+}
+
+// Shared validation and packing of the three calls.
+int prepare_book(const mmskv_shape* shape, const mmskv_pages* pages, int32_t* refs, int32_t* missing, void* ws,
+                 size_t ws_bytes, BookArgs* a) {
+    const int rc = check_book(shape, pages, refs, &a->pages);
+    if (rc) return rc;
+    if (missing == nullptr || !aligned(missing, 4)) return MMSKV_EINVAL;
+    a->table = const_cast<int32_t*>(pages->table);
+    a->refs = refs;
+    a->missing = missing;
+    a->B = shape->B;
+    a->Hkv = shape->Hkv;
+    a->d = shape->d;
+    a->chunks = book_chunks(pages->n_pages);
+    const size_t need = book_layout(a->B, a->Hkv, pages->n_pages, pages->max_pages, static_cast<char*>(ws), a);
+    if (ws == nullptr || !aligned(ws, kAlign) || ws_bytes < need) return MMSKV_EWORKSPACE;
+    return MMSKV_OK;
+}
+
+}  // namespace
+
+size_t mmshiftkv_cache_book_workspace(const mmskv_shape* shape, int32_t n_pages, int32_t max_pages) {
+    if (shape == nullptr || shape->B < 1 || shape->B > 65535 || shape->Hkv < 1 || shape->Hkv > 65535) return 0;
+    if (n_pages < 1 || max_pages < 1 || static_cast<int64_t>(shape->B) * max_pages > kMaxEntries) return 0;
+    BookArgs a = {};
+    return book_layout(shape->B, shape->Hkv, n_pages, max_pages, nullptr, &a);
+}
+
+int mmshiftkv_cache_hold(const mmskv_shape* shape, const mmskv_pages* pages, int32_t* refs, const int32_t* rows,
+                         int32_t* missing, void* workspace, size_t workspace_bytes, void* stream) {
+    if (rows == nullptr || !aligned(rows, 4)) return MMSKV_EINVAL;
+    BookArgs a = {};
+    const int rc = prepare_book(shape, pages, refs, missing, workspace, workspace_bytes, &a);
+    if (rc) return rc;
+    a.rows = rows;
+    return status_of(launch_book(a, kBookHold, static_cast<hipStream_t>(stream)));
+}
+
+int mmshiftkv_cache_fork(const mmskv_shape* shape, const mmskv_pages* pages, int32_t* refs, const int32_t* src,
+                         int32_t* lens, int32_t* missing, void* workspace, size_t workspace_bytes, void* stream) {
+    if (src == nullptr || lens == nullptr || !aligned(src, 4) || !aligned(lens, 4)) return MMSKV_EINVAL;
+    BookArgs a = {};
+    const int rc = prepare_book(shape, pages, refs, missing, workspace, workspace_bytes, &a);
+    if (rc) return rc;
+    a.src = src;
+    a.lens = lens;
+    return status_of(launch_book(a, kBookFork, static_cast<hipStream_t>(stream)));
+}
+
+int mmshiftkv_cache_compact(const mmskv_shape* shape, const mmskv_pages* pages, int32_t* refs, int32_t* lens,
+                            const int32_t* idx, const int32_t* counts, int32_t n, int32_t* missing, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    if (lens == nullptr || idx == nullptr || counts == nullptr || n < 1) return MMSKV_EINVAL;
+    if (!aligned(lens, 4) || !aligned(idx, 4) || !aligned(counts, 4)) return MMSKV_EINVAL;
+    if (n > kMaxCacheRows) return MMSKV_EUNSUPPORTED;
+    BookArgs a = {};
+    const int rc = prepare_book(shape, pages, refs, missing, workspace, workspace_bytes, &a);
+    if (rc) return rc;
+    a.lens = lens;
+    a.idx = idx;
+    a.rows = counts;
+    a.n = n;
+    return status_of(launch_book(a, kBookCompact, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

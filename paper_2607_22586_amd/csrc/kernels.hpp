@@ -213,6 +213,27 @@ int chunk_splits(int64_t heads, int rows, int T, int d, int dtype);
 // B, T or n grows.
 size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d);
 
+// Changes of the pages that sequences hold.
+constexpr int kBookHold = 1, kBookFork = 2, kBookCompact = 3;
+struct BookArgs {
+    Pages pages;
+    int32_t* table;            // pages.table, which these calls write
+    int32_t* refs;             // [n_pages] entries of the table that name each page
+    const int32_t* rows;       // [B, Hkv]: hold: rows to hold, compact: rows kept
+    const int32_t* src;        // [B] fork
+    const int32_t* idx;        // [B, Hkv, n] compact
+    int32_t* lens;             // [B, Hkv] fork and compact
+    int32_t* missing;          // [B]
+    int B, Hkv, d, n;
+    int64_t chunks;            // book_chunks(n_pages)
+    // workspace: of each sequence the pages wanted, of each chunk the free ones; of the
+    // new pages, in order, their number, their ids and (sequence, entry); the table and
+    // the lengths as they were
+    int32_t* want; int32_t* free; int32_t* taken; int32_t* ids; int2* items;
+    int32_t* old_table; int32_t* old_lens;
+};
+int64_t book_chunks(int n_pages);
+
 // Upper end of the lane sums (keys_per_sum terms of 2^s each) that the score
 // and decode kernels add relative to zero.  A row's total over T keys is
 // made of at most n = ceil(T / keys_per_sum) such sums, so with every one
@@ -251,5 +272,6 @@ hipError_t launch_shape_scores(const ShapeArgs& a, hipStream_t s);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t s);
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t s);
 hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t s);
+hipError_t launch_book(const BookArgs& a, int op, hipStream_t s);
 
 }  // namespace mmskv

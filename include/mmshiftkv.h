@@ -488,6 +488,33 @@ int mmshiftkv_chunk_attention(const mmskv_shape *shape, const mmskv_pages *pages
                               int32_t n, int32_t causal, uint16_t *out, const mmskv_strides *out_strides,
                               void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Attention of whole prompts over themselves, which gives the hidden states
+ * that the next layer's keys come from: each batch row is one sequence of T
+ * tokens, or (starts given, B = 1) the T tokens are n_seq sequences one behind
+ * the other, sequence s being the tokens starts[s] <= t < starts[s + 1].  Query i
+ * of head h (KV head c = h / Gh) sees the keys of its sequence, with causal = 1
+ * those t <= i of them:
+ *   out[b,h,i,:] = sum_t p_t v_t,  p = softmax over the keys it sees of
+ *                  q . k_t / sqrt(d)
+ *   lse[b,h,i]   = ln sum_t e^(q . k_t / sqrt(d))      (where lse is given)
+ * bf16 products, fp32 accumulation and softmax, p rounded to bf16 for its
+ * product with v, the result rounded once.  A key that a query does not see
+ * does not reach it, whatever it holds, infinities and NaN included (another
+ * sequence's, a later token's, padding).  Sums are divided last, as in
+ * mmshiftkv_chunk_attention.  Rows of out and lse in no sequence (before
+ * starts[0], or from starts[n_seq] on) are left as they were.
+ * Reads shape->B, Hq, Hkv, T and d (64 or 128); Gh * T and B * Hkv up to 2^22
+ * (more -> MMSKV_EUNSUPPORTED).
+ *   q       [B, Hq, T, d] bf16;  k, v [B, Hkv, T, d] bf16, with their strides
+ *   starts  [n_seq + 1] int32, ascending (sequences may be empty), taken as if
+ *           clamped to [0, T]; or NULL (n_seq is ignored)
+ *   out     [B, Hq, T, d] bf16, strides out_strides, rows not overlapping
+ *   lse     [B, Hq, T] fp32, contiguous, or NULL */
+int mmshiftkv_prompt_attention(const mmskv_shape *shape, const uint16_t *q, const mmskv_strides *q_strides,
+                               const uint16_t *k, const mmskv_strides *k_strides, const uint16_t *v,
+                               const mmskv_strides *v_strides, const int32_t *starts, int32_t n_seq, int32_t causal,
+                               uint16_t *out, const mmskv_strides *out_strides, float *lse, void *stream);
+
 /* ---- Pages that several sequences hold.  refs[p] is the number of table
  * entries that name page p; pages of 0 are free.  The three calls below keep
  * them so, and write the table of `pages` (and refs, lens and the pools): what

@@ -9,6 +9,6 @@ from .binding import (MMSKV_BF16, MMSKV_F32, MMSKV_MASS, MMSKV_VOTE, LayerOut, M
                       PagedCache, ScoreOut, Selected, SelectionConfig, build_proxies, cache_book_workspace,
                       cache_compact, cache_fork, cache_hold, cache_read, cache_write, chunk_attention,
                       chunk_attention_workspace, decode_check, decode_workspace,
-                      gather_kv, load_library,
+                      gather_kv, load_library, prompt_attention,
                       score, score_lse, score_mass, score_workspace, select_layer, select_topk,
                       select_workspace, status_string)

@@ -32,7 +32,7 @@ EXPORTED = ("mmshiftkv_build_proxies", "mmshiftkv_score_workspace", "mmshiftkv_s
             "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
             "mmshiftkv_chunk_attention_workspace", "mmshiftkv_chunk_attention",
             "mmshiftkv_cache_book_workspace", "mmshiftkv_cache_hold", "mmshiftkv_cache_fork",
-            "mmshiftkv_cache_compact")
+            "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention")
 
 
 class Shape(ctypes.Structure):
@@ -115,6 +115,7 @@ def load_library(path: str | None = None):
     lib.mmshiftkv_chunk_attention_workspace.argtypes = [PS, I32]
     lib.mmshiftkv_chunk_attention_workspace.restype = SZ
     lib.mmshiftkv_chunk_attention.argtypes = [PS, PG, V, PT, V, V, I32, I32, V, PT, V, SZ, V]
+    lib.mmshiftkv_prompt_attention.argtypes = [PS, V, PT, V, PT, V, PT, V, I32, I32, V, PT, V, V]
     lib.mmshiftkv_cache_book_workspace.argtypes = [PS, I32, I32]
     lib.mmshiftkv_cache_book_workspace.restype = SZ
     lib.mmshiftkv_cache_hold.argtypes = [PS, PG, V, V, V, V, SZ, V]
@@ -131,7 +132,7 @@ def load_library(path: str | None = None):
                  "mmshiftkv_decode_check", "mmshiftkv_window_rows", "mmshiftkv_shape_scores",
                  "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
                  "mmshiftkv_chunk_attention", "mmshiftkv_cache_hold", "mmshiftkv_cache_fork",
-                 "mmshiftkv_cache_compact"):
+                 "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention"):
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
         _lib = lib
@@ -817,6 +818,48 @@ def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_co
     _enqueue("mmshiftkv_chunk_attention", i, shape, ref(pages), q.data_ptr(), ref(qs), q_counts, rows, n,
              1 if causal else 0, out.data_ptr(), ref(os), ws.data_ptr(), ws.numel() * ws.element_size())
     return out
+
+
+# ----------------------------------------------------------------------------
+# whole prompts over themselves
+# ----------------------------------------------------------------------------
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor | None = None,
+                     causal: bool = True, with_lse: bool = False, out: torch.Tensor | None = None,
+                     lse: torch.Tensor | None = None):
+    """mmshiftkv_prompt_attention: the outputs [B, Hq, T, d] bf16 of q [B, Hq, T, d] over k, v [B, Hkv, T, d]
+    (bf16), each batch row a sequence; with starts [n + 1] int32 (B = 1) the T tokens are n sequences one
+    behind the other, sequence s the tokens starts[s] .. starts[s + 1] - 1 (rows in none are not written).
+    with_lse (or a preallocated lse [B, Hq, T] fp32): returns (out, lse), the log-sum-exp of each row's
+    logits.  The result is laid out as q is unless `out` is given."""
+    i = _same_device(q, k, v, starts, out, lse)
+    if q.dtype != torch.bfloat16 or k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+        raise TypeError("q, k and v are bf16")
+    qs, ks, vs = _row_strides(q), _row_strides(k), _row_strides(v)
+    B, Hq, T, d = q.shape
+    Hkv = k.shape[1]
+    if k.shape != v.shape or k.shape != (B, Hkv, T, d):
+        raise ValueError("k and v do not match q")
+    n_seq, first = 0, None
+    if starts is not None:
+        if starts.dim() != 1 or starts.shape[0] < 2 or B != 1:
+            raise ValueError("starts cut the tokens of one batch row: [n + 1] with B = 1")
+        n_seq = starts.shape[0] - 1
+        first = _int32(starts, (n_seq + 1,), "starts")
+    if out is None:
+        out = torch.empty_like(q)
+        if out.stride(3) != 1:
+            out = q.new_empty(q.shape)
+    elif out.dtype != torch.bfloat16 or out.shape != q.shape:
+        raise ValueError("preallocated out does not match")
+    os = _row_strides(out)
+    if lse is None:
+        lse = q.new_empty((B, Hq, T), dtype=torch.float32) if with_lse else None
+    elif lse.dtype != torch.float32 or lse.shape != (B, Hq, T) or not lse.is_contiguous():
+        raise ValueError("preallocated lse does not match")
+    ref = ctypes.byref
+    _enqueue("mmshiftkv_prompt_attention", i, ref(Shape(B, Hq, Hkv, T, 0, d)), q.data_ptr(), ref(qs), k.data_ptr(),
+             ref(ks), v.data_ptr(), ref(vs), first, n_seq, 1 if causal else 0, out.data_ptr(), ref(os), _p(lse))
+    return out if lse is None else (out, lse)
 
 
 # ----------------------------------------------------------------------------

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmmshiftkv.so")
 SOURCES = ["api.hip", "proxies.hip", "score.hip", "select.hip", "gather.hip", "hidden.hip", "decode.hip", "baselines.hip",
-           "cache.hip", "chunk.hip", "pages.hip"]
+           "cache.hip", "chunk.hip", "pages.hip", "prompt.hip"]
 HEADERS = ["common.hpp", "kernels.hpp", "normal.hpp", "pages.hpp"]
 ARCH = "gfx950"
 

@@ -1038,4 +1038,57 @@ int mmshiftkv_cache_compact(const mmskv_shape* shape, const mmskv_pages* pages, 
     return status_of(launch_book(a, kBookCompact, static_cast<hipStream_t>(stream)));
 }
 
+int mmshiftkv_prompt_attention(const mmskv_shape* shape, const uint16_t* q, const mmskv_strides* q_strides,
+                               const uint16_t* k, const mmskv_strides* k_strides, const uint16_t* v,
+                               const mmskv_strides* v_strides, const int32_t* starts, int32_t n_seq, int32_t causal,
+                               uint16_t* out, const mmskv_strides* out_strides, float* lse, void* stream) {
+    int rc = check_heads(shape);
+    if (rc) return rc;
+    if (shape->d < 1 || q == nullptr || k == nullptr || v == nullptr || out == nullptr) return MMSKV_EINVAL;
+    if (causal != 0 && causal != 1) return MMSKV_EINVAL;
+    if (starts != nullptr && (n_seq < 1 || shape->B != 1)) return MMSKV_EINVAL;
+    if (!aligned(starts, 4) || !aligned(lse, 4)) return MMSKV_EINVAL;
+    if (shape->d != 64 && shape->d != 128) return MMSKV_EUNSUPPORTED;
+    const int64_t gh = shape->Hq / shape->Hkv;
+    if (gh * shape->T > (1 << 22) || static_cast<int64_t>(shape->B) * shape->Hkv > kMaxChunkHeads) return MMSKV_EUNSUPPORTED;
+    rc = check_rows(q, q_strides, 2, true);
+    if (rc) return rc;
+    rc = check_rows(k, k_strides, 2, true);
+    if (rc) return rc;
+    rc = check_rows(v, v_strides, 2, true);
+    if (rc) return rc;
+    rc = check_out_rows(out, out_strides, 2, shape->B, shape->Hq, shape->T);
+    if (rc) return rc;
+    PromptArgs a = {};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = out;
+    a.qsb = q_strides->sb;
+    a.qsh = q_strides->sh;
+    a.qst = q_strides->st;
+    a.ksb = k_strides->sb;
+    a.ksh = k_strides->sh;
+    a.kst = k_strides->st;
+    a.vsb = v_strides->sb;
+    a.vsh = v_strides->sh;
+    a.vst = v_strides->st;
+    a.osb = out_strides->sb;
+    a.osh = out_strides->sh;
+    a.ost = out_strides->st;
+    a.starts = starts;
+    a.lse = lse;
+    a.B = shape->B;
+    a.Hq = shape->Hq;
+    a.Hkv = shape->Hkv;
+    a.T = shape->T;
+    a.d = shape->d;
+    a.Gh = static_cast<int>(gh);
+    a.n_seq = n_seq;
+    a.causal = causal;
+    a.rows = static_cast<int>(gh) * shape->T;
+    a.scale = static_cast<float>(query_scale(shape->d));
+    return status_of(launch_prompt_attention(a, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

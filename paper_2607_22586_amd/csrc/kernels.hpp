@@ -213,6 +213,18 @@ int chunk_splits(int64_t heads, int rows, int T, int d, int dtype);
 // B, T or n grows.
 size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d);
 
+struct PromptArgs {
+    const uint16_t* q;         // [B, Hq, T, d] bf16
+    const uint16_t* k; const uint16_t* v;   // [B, Hkv, T, d] bf16
+    uint16_t* out;             // [B, Hq, T, d] bf16
+    int64_t qsb, qsh, qst, ksb, ksh, kst, vsb, vsh, vst, osb, osh, ost;
+    const int32_t* starts;     // [n_seq + 1] or null: each batch row one sequence
+    float* lse;                // [B, Hq, T] or null
+    int B, Hq, Hkv, T, d, Gh, n_seq, causal;
+    int rows;                  // Gh * T query rows of a KV head, row i * Gh + g: token i of its head g
+    float scale;               // log2(e) / sqrt(d)
+};
+
 // Changes of the pages that sequences hold.
 constexpr int kBookHold = 1, kBookFork = 2, kBookCompact = 3;
 struct BookArgs {
@@ -272,6 +284,7 @@ hipError_t launch_shape_scores(const ShapeArgs& a, hipStream_t s);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t s);
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t s);
 hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t s);
+hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s);
 hipError_t launch_book(const BookArgs& a, int op, hipStream_t s);
 
 }  // namespace mmskv

@@ -488,6 +488,34 @@ int mmshiftkv_chunk_attention(const mmskv_shape *shape, const mmskv_pages *pages
                               int32_t n, int32_t causal, uint16_t *out, const mmskv_strides *out_strides,
                               void *workspace, size_t workspace_bytes, void *stream);
 
+/* mmshiftkv_chunk_attention for sequences that share their leading rows (the
+ * answers to one prompt), which are read once for all of them: the sequences b
+ * of group g = b / (B / groups) share the first shared[g,c] (clamped to [0,
+ * min(shared_T, T, max_pages * page)]) rows of each head.  Those are found by
+ * shared_table, row g of which is laid out as a row of the table; the table of
+ * `pages` names the rows from shared[g,c] on (its entries before are not used:
+ * they may name the same pages, as mmshiftkv_cache_fork leaves them, or none).
+ * lens counts all rows of a sequence, the shared ones among them; a sequence of
+ * fewer sees as many of those.  Otherwise as mmshiftkv_chunk_attention, and to
+ * rounding what it gives where both tables name the same rows; an infinity or
+ * NaN in a shared row's v may reach the queries of its group that do not see it.
+ * B is a multiple of groups (groups = 1: one prompt for all); B / groups * Gh * n
+ * and B * Hkv up to 2^22 (more -> MMSKV_EUNSUPPORTED).  T and shared_T are upper
+ * bounds of lens and shared, which fix how the work is split (shared_T = T is
+ * always right, a close bound is faster).
+ *   shared        [groups, Hkv] int32
+ *   shared_table  [groups, max_pages] int32, contiguous
+ * Workspace: mmshiftkv_shared_attention_workspace bytes (256-byte aligned; 0 for
+ * invalid sizes; they never fall as T or n grows, or B at the same B / groups),
+ * without clearing; calls that may overlap in time need workspaces of their
+ * own. */
+size_t mmshiftkv_shared_attention_workspace(const mmskv_shape *shape, int32_t groups, int32_t n);
+int mmshiftkv_shared_attention(const mmskv_shape *shape, const mmskv_pages *pages, const uint16_t *q,
+                               const mmskv_strides *q_strides, const int32_t *q_counts, const int32_t *lens,
+                               const int32_t *shared, const int32_t *shared_table, int32_t groups, int32_t shared_T,
+                               int32_t n, int32_t causal, uint16_t *out, const mmskv_strides *out_strides,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- Attention of whole prompts over themselves, which gives the hidden states
  * that the next layer's keys come from: each batch row is one sequence of T
  * tokens, or (starts given, B = 1) the T tokens are n_seq sequences one behind

@@ -32,7 +32,8 @@ EXPORTED = ("mmshiftkv_build_proxies", "mmshiftkv_score_workspace", "mmshiftkv_s
             "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
             "mmshiftkv_chunk_attention_workspace", "mmshiftkv_chunk_attention",
             "mmshiftkv_cache_book_workspace", "mmshiftkv_cache_hold", "mmshiftkv_cache_fork",
-            "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention")
+            "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention", "mmshiftkv_shared_attention_workspace",
+            "mmshiftkv_shared_attention")
 
 
 class Shape(ctypes.Structure):
@@ -115,6 +116,9 @@ def load_library(path: str | None = None):
     lib.mmshiftkv_chunk_attention_workspace.argtypes = [PS, I32]
     lib.mmshiftkv_chunk_attention_workspace.restype = SZ
     lib.mmshiftkv_chunk_attention.argtypes = [PS, PG, V, PT, V, V, I32, I32, V, PT, V, SZ, V]
+    lib.mmshiftkv_shared_attention_workspace.argtypes = [PS, I32, I32]
+    lib.mmshiftkv_shared_attention_workspace.restype = SZ
+    lib.mmshiftkv_shared_attention.argtypes = [PS, PG, V, PT, V, V, V, V, I32, I32, I32, I32, V, PT, V, SZ, V]
     lib.mmshiftkv_prompt_attention.argtypes = [PS, V, PT, V, PT, V, PT, V, I32, I32, V, PT, V, V]
     lib.mmshiftkv_cache_book_workspace.argtypes = [PS, I32, I32]
     lib.mmshiftkv_cache_book_workspace.restype = SZ
@@ -132,7 +136,7 @@ def load_library(path: str | None = None):
                  "mmshiftkv_decode_check", "mmshiftkv_window_rows", "mmshiftkv_shape_scores",
                  "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
                  "mmshiftkv_chunk_attention", "mmshiftkv_cache_hold", "mmshiftkv_cache_fork",
-                 "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention"):
+                 "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention", "mmshiftkv_shared_attention"):
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
         _lib = lib
@@ -817,6 +821,58 @@ def chunk_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, q_co
         ws = _ws(load_library().mmshiftkv_chunk_attention_workspace(shape, n), q.device)
     _enqueue("mmshiftkv_chunk_attention", i, shape, ref(pages), q.data_ptr(), ref(qs), q_counts, rows, n,
              1 if causal else 0, out.data_ptr(), ref(os), ws.data_ptr(), ws.numel() * ws.element_size())
+    return out
+
+
+def shared_attention_workspace(B, Hq, Hkv, T, d, n, groups) -> int:
+    return int(load_library().mmshiftkv_shared_attention_workspace(
+        ctypes.byref(_shape(B, Hq, Hkv, T, 0, d)), int(groups), int(n)))
+
+
+def shared_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, shared: torch.Tensor,
+                     shared_table: torch.Tensor | None = None, q_counts: torch.Tensor | None = None,
+                     T: int | None = None, shared_T: int | None = None, causal: bool = True,
+                     workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """mmshiftkv_shared_attention: chunk_attention for G groups of B / G sequences that share the first
+    shared[g, c] rows (shared [G, Hkv] int32), which are read once for a group.  shared_table [G, max_pages]
+    int32 names their pages (None: the table's row of each group's first sequence, as cache_fork leaves
+    it); T and shared_T are upper bounds of lens and shared (None: what the table can hold, and T)."""
+    i = _same_device(q, cache.k, lens, shared, shared_table, q_counts, workspace, out)
+    if q.dtype != torch.bfloat16:
+        raise TypeError("q is bf16")
+    qs = _row_strides(q)
+    B, Hq, n, d = q.shape
+    pages = cache.c_pages()
+    _, Hkv, page, row = cache.k.shape
+    if row != d or cache.table.shape[0] != B:
+        raise ValueError("q does not match the cache's row size or sequences")
+    rows = _int32(lens, (B, Hkv), "lens")
+    G = shared.shape[0]
+    prefix = _int32(shared, (G, Hkv), "shared")
+    if G < 1 or B % G:
+        raise ValueError("the sequences are groups of the same size: %d of %d" % (G, B))
+    if shared_table is None:
+        shared_table = cache.table[::B // G].contiguous()
+    named = _int32(shared_table, (G, cache.table.shape[1]), "shared_table")
+    if q_counts is not None:
+        q_counts = _int32(q_counts, (B,), "q_counts")
+    if out is None:
+        out = torch.empty_like(q)
+        if out.stride(3) != 1:
+            out = q.new_empty(q.shape)
+    elif out.dtype != torch.bfloat16 or out.shape != q.shape:
+        raise ValueError("preallocated out does not match")
+    os = _row_strides(out)
+    ref = ctypes.byref
+    most = cache.table.shape[1] * page
+    T = most if T is None else min(int(T), most)
+    shape = ref(Shape(B, Hq, Hkv, T, 0, d))
+    ws = workspace
+    if ws is None:
+        ws = _ws(load_library().mmshiftkv_shared_attention_workspace(shape, G, n), q.device)
+    _enqueue("mmshiftkv_shared_attention", i, shape, ref(pages), q.data_ptr(), ref(qs), q_counts, rows, prefix, named, G,
+             T if shared_T is None else max(1, min(int(shared_T), T)), n, 1 if causal else 0, out.data_ptr(), ref(os),
+             ws.data_ptr(), ws.numel() * ws.element_size())
     return out
 
 

@@ -813,6 +813,32 @@ int check_chunk(const mmskv_shape* s, int32_t n) {
     return MMSKV_OK;
 }
 
+// The arguments of an attention call (its pages are there already).
+void pack_chunk(const mmskv_shape* shape, const uint16_t* q, const mmskv_strides* q_strides, const int32_t* q_counts,
+                const int32_t* lens, int32_t n, int32_t causal, uint16_t* out, const mmskv_strides* out_strides,
+                ChunkArgs* a) {
+    a->q = q;
+    a->out = out;
+    a->qsb = q_strides->sb;
+    a->qsh = q_strides->sh;
+    a->qst = q_strides->st;
+    a->osb = out_strides->sb;
+    a->osh = out_strides->sh;
+    a->ost = out_strides->st;
+    a->q_counts = q_counts;
+    a->lens = lens;
+    a->B = shape->B;
+    a->Hq = shape->Hq;
+    a->Hkv = shape->Hkv;
+    a->d = shape->d;
+    a->Gh = shape->Hq / shape->Hkv;
+    a->n = n;
+    a->causal = causal;
+    a->max_len = shape->T < a->pages.cap ? shape->T : a->pages.cap;
+    a->rows = a->Gh * n;
+    a->scale = static_cast<float>(query_scale(shape->d));
+}
+
 size_t chunk_ws(const mmskv_shape* s, int32_t n) {
     return chunk_workspace_bound(static_cast<int64_t>(s->B) * s->Hkv, s->Hq / s->Hkv * n, s->T, s->d);
 }
@@ -909,27 +935,8 @@ int mmshiftkv_chunk_attention(const mmskv_shape* shape, const mmskv_pages* pages
     if (rc) return rc;
     rc = check_out_rows(out, out_strides, 2, shape->B, shape->Hq, n);
     if (rc) return rc;
+    pack_chunk(shape, q, q_strides, q_counts, lens, n, causal, out, out_strides, &a);
     const int64_t heads = static_cast<int64_t>(shape->B) * shape->Hkv;
-    a.q = q;
-    a.out = out;
-    a.qsb = q_strides->sb;
-    a.qsh = q_strides->sh;
-    a.qst = q_strides->st;
-    a.osb = out_strides->sb;
-    a.osh = out_strides->sh;
-    a.ost = out_strides->st;
-    a.q_counts = q_counts;
-    a.lens = lens;
-    a.B = shape->B;
-    a.Hq = shape->Hq;
-    a.Hkv = shape->Hkv;
-    a.d = shape->d;
-    a.Gh = shape->Hq / shape->Hkv;
-    a.n = n;
-    a.causal = causal;
-    a.max_len = shape->T < a.pages.cap ? shape->T : a.pages.cap;
-    a.rows = a.Gh * n;
-    a.scale = static_cast<float>(query_scale(shape->d));
     a.splits = chunk_splits(heads, a.rows, a.max_len, a.d, a.pages.dtype);
     const size_t need = chunk_ws(shape, n);
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < need) return MMSKV_EWORKSPACE;
@@ -1089,6 +1096,77 @@ int mmshiftkv_prompt_attention(const mmskv_shape* shape, const uint16_t* q, cons
     a.rows = static_cast<int>(gh) * shape->T;
     a.scale = static_cast<float>(query_scale(shape->d));
     return status_of(launch_prompt_attention(a, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+// Rows of partial sums of one part of an attention over a shared prefix.
+size_t part_rows_bytes(int64_t heads, int64_t rows, int T, int d) {
+    const size_t one = static_cast<size_t>(heads * rows) * (d * sizeof(float) + sizeof(float2)) + 256;
+    const size_t split = chunk_workspace_bound(heads, static_cast<int>(rows), T, d);
+    return split > one ? split : one;
+}
+
+int check_groups(const mmskv_shape* s, int32_t groups, int32_t n) {
+    const int rc = check_chunk(s, n);
+    if (rc) return rc;
+    if (groups < 1 || s->B % groups != 0) return MMSKV_EINVAL;
+    if (static_cast<int64_t>(s->B / groups) * (s->Hq / s->Hkv) * n > (1 << 22)) return MMSKV_EUNSUPPORTED;
+    return MMSKV_OK;
+}
+
+size_t shared_ws(const mmskv_shape* s, int32_t groups, int32_t n) {
+    const int64_t rows = static_cast<int64_t>(s->Hq / s->Hkv) * n;
+    return align_up(part_rows_bytes(static_cast<int64_t>(groups) * s->Hkv, rows * (s->B / groups), s->T, s->d)) +
+           align_up(part_rows_bytes(static_cast<int64_t>(s->B) * s->Hkv, rows, s->T, s->d));
+}
+
+}  // namespace
+
+size_t mmshiftkv_shared_attention_workspace(const mmskv_shape* shape, int32_t groups, int32_t n) {
+    return check_groups(shape, groups, n) == MMSKV_OK ? shared_ws(shape, groups, n) : 0;
+}
+
+int mmshiftkv_shared_attention(const mmskv_shape* shape, const mmskv_pages* pages, const uint16_t* q,
+                               const mmskv_strides* q_strides, const int32_t* q_counts, const int32_t* lens,
+                               const int32_t* shared, const int32_t* shared_table, int32_t groups, int32_t shared_T,
+                               int32_t n, int32_t causal, uint16_t* out, const mmskv_strides* out_strides,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_groups(shape, groups, n);
+    if (rc) return rc;
+    ChunkArgs a = {};
+    rc = check_pages(pages, shape->d, &a.pages);
+    if (rc) return rc;
+    if (shared == nullptr || shared_table == nullptr || shared_T < 1) return MMSKV_EINVAL;
+    if (!aligned(shared, 4) || !aligned(shared_table, 4)) return MMSKV_EINVAL;
+    if (q == nullptr || lens == nullptr || out == nullptr || (causal != 0 && causal != 1)) return MMSKV_EINVAL;
+    if (!aligned(lens, 4) || !aligned(q_counts, 4)) return MMSKV_EINVAL;
+    rc = check_rows(q, q_strides, 2, true);
+    if (rc) return rc;
+    rc = check_out_rows(out, out_strides, 2, shape->B, shape->Hq, n);
+    if (rc) return rc;
+    pack_chunk(shape, q, q_strides, q_counts, lens, n, causal, out, out_strides, &a);
+    a.shared = shared;
+    a.each = shape->B / groups;
+    a.shared_max = shared_T < a.max_len ? shared_T : a.max_len;
+    // the part behind the shared rows, whose plan takes all to be as long as the bounds say
+    ChunkArgs pre = a;
+    pre.B = groups;
+    pre.rows = a.each * a.rows;
+    pre.pages.table = shared_table;
+    pre.splits = chunk_splits(static_cast<int64_t>(groups) * a.Hkv, pre.rows, a.shared_max, a.d, a.pages.dtype);
+    const int mine = a.max_len - a.shared_max;
+    a.splits = chunk_splits(static_cast<int64_t>(a.B) * a.Hkv, a.rows, mine > 64 ? mine : 64, a.d, a.pages.dtype);
+    const size_t need = shared_ws(shape, groups, n);
+    if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < need) return MMSKV_EWORKSPACE;
+    const size_t rows = static_cast<size_t>(a.B) * a.Hkv * a.rows, all = (pre.splits + a.splits) * rows;
+    const size_t ml_off = align_up(all * a.d * sizeof(float));
+    if (ml_off + all * sizeof(float2) > need) return MMSKV_EWORKSPACE;
+    pre.part_o = static_cast<float*>(workspace);
+    pre.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ml_off);
+    a.part_o = pre.part_o + pre.splits * rows * a.d;
+    a.part_ml = pre.part_ml + pre.splits * rows;
+    return status_of(launch_shared_attention(pre, a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -82,7 +82,40 @@ __device__ __forceinline__ int staged(int r, int ch) {
     return r * (2 * D) + 16 * (ch ^ swz);
 }
 
-template <int D, int TYPE>
+// What a launch works on: all rows that a sequence sees; the rows that the sequences of
+// a group share, for the queries of all of them (b is the group, pages.table the groups'
+// and row r = (s * n + i) * Gh + g query i of the group's sequence s); or those behind
+// the shared ones.  The last two leave partial sums only.
+constexpr int kWhole = 0, kShared = 1, kOwn = 2;
+
+// A query row: its sequence, query, and head within the KV head.
+struct Query {
+    int b, i, g;
+};
+template <int PART>
+__device__ __forceinline__ Query query_of(const ChunkArgs& a, int b, int r) {
+    if constexpr (PART == kShared) {
+        const int per = a.Gh * a.n, s = r / per, x = r - s * per, i = x / a.Gh;
+        return {b * a.each + min(s, a.each - 1), i, x - i * a.Gh};
+    } else {
+        const int i = r / a.Gh;
+        return {b, i, r - i * a.Gh};
+    }
+}
+__device__ __forceinline__ int queries_of(const ChunkArgs& a, int b) {
+    return a.q_counts ? min(max(a.q_counts[b], 0), a.n) : a.n;
+}
+// Rows that the sequences of group g share.
+__device__ __forceinline__ int shared_rows(const ChunkArgs& a, int g, int c) {
+    return min(max(a.shared[static_cast<int64_t>(g) * a.Hkv + c], 0), a.shared_max);
+}
+// The last key that a query that is there sees (below 0: none), of the shared rows.
+__device__ __forceinline__ int last_shared(const ChunkArgs& a, const Query& q, int c, int nq, int shared) {
+    const int len = min(max(a.lens[static_cast<int64_t>(q.b) * a.Hkv + c], 0), a.max_len);
+    return min(a.causal ? len - nq + q.i : len - 1, shared - 1);
+}
+
+template <int D, int TYPE, int PART = kWhole>
 __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     constexpr int KC = D / 16;             // 16-dim steps of S
     constexpr int NT = D / 32;             // 32-dim tiles of O
@@ -104,20 +137,39 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane >> 5;
 
-    const int nq = a.q_counts ? min(max(a.q_counts[b], 0), a.n) : a.n;
-    const int len = min(max(a.lens[bc], 0), a.max_len);
     // this lane's query row, and the last key that it sees (below 0: none)
     const int r = r0 + 32 * wave + (lane & 31);
-    const int i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
+    const Query qr = query_of<PART>(a, b, r);
+    const int i = qr.i, h = c * a.Gh + qr.g;
+    const int nq = queries_of(a, qr.b);
     const bool there = r < a.rows && i < nq;
-    const int last = !there ? -1 : (a.causal ? len - nq + i : len - 1);
-    // keys that all rows of the workgroup see (those that are not there aside)
-    const int all_see = a.causal ? len - nq + r0 / a.Gh + 1 : len;
-    // keys that the workgroup's rows see together, and this split's part of them
-    const int i_end = min((min(r0 + kRows, a.rows) - 1) / a.Gh, nq - 1);
-    const int end = i_end < r0 / a.Gh ? 0 : max(a.causal ? len - nq + i_end + 1 : len, 0);
-    const int tiles = (end + kKeys - 1) / kKeys, per = (tiles + a.splits - 1) / a.splits;
-    const int tile0 = split * per, tile1 = min(tile0 + per, tiles);
+    int last, all_see, end, low = 0;
+    if constexpr (PART == kShared) {
+        // keys that all rows of the workgroup see, and that some row sees
+        __shared__ int most[2][kWaves];
+        const int shared = shared_rows(a, b, c);
+        last = there ? last_shared(a, qr, c, nq, shared) : -1;
+        int lo = there ? last + 1 : shared, hi = last + 1;
+#pragma unroll
+        for (int x = 1; x < 32; x *= 2) lo = min(lo, __shfl_xor(lo, x)), hi = max(hi, __shfl_xor(hi, x));
+        if (lane == 0) most[0][wave] = lo, most[1][wave] = hi;
+        __syncthreads();
+        all_see = min(min(most[0][0], most[0][1]), min(most[0][2], most[0][3]));
+        end = max(max(most[1][0], most[1][1]), max(most[1][2], most[1][3]));
+    } else {
+        const int len = min(max(a.lens[bc], 0), a.max_len);
+        last = !there ? -1 : (a.causal ? len - nq + i : len - 1);
+        // keys that all rows of the workgroup see (those that are not there aside)
+        all_see = a.causal ? len - nq + r0 / a.Gh + 1 : len;
+        // keys that the workgroup's rows see together
+        const int i_end = min((min(r0 + kRows, a.rows) - 1) / a.Gh, nq - 1);
+        end = i_end < r0 / a.Gh ? 0 : max(a.causal ? len - nq + i_end + 1 : len, 0);
+        if constexpr (PART == kOwn) low = shared_rows(a, b / a.each, c);   // the first key
+    }
+    // this split's tiles
+    const int tiles0 = low / kKeys, tiles = max((end + kKeys - 1) / kKeys, tiles0);
+    const int per = (tiles - tiles0 + a.splits - 1) / a.splits;
+    const int tile0 = tiles0 + split * per, tile1 = min(tile0 + per, tiles);
 
     // A wave stages rows kWaveRows * wave .. of a tile, which are on one page:
     // consecutive bytes of K and of V, by way of registers, so that the next
@@ -203,14 +255,14 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
             }
         }
     };
-    // Rows of V behind the last key may hold anything: zeros, for p = 0 to meet
+    // Rows of V behind the last key (and before the first) may hold anything: zeros, for p = 0 to meet
     // (their logits are masked).  By the wave that staged them.
     auto clear_tail = [&](int tile, int buf) {
-        if ((tile + 1) * kKeys <= end) return;
+        if ((tile + 1) * kKeys <= end && (PART != kOwn || tile * kKeys >= low)) return;
         constexpr int kOut = 2 * D / 16;
         for (int x = lane; x < kWaveRows * kOut; x += kWave) {
             const int row = kWaveRows * wave + x / kOut;
-            if (tile * kKeys + row < end) continue;
+            if (tile * kKeys + row < end && (PART != kOwn || tile * kKeys + row >= low)) continue;
             *reinterpret_cast<u32x4*>(vt[buf] + row * 2 * D + 16 * (x % kOut)) = u32x4{0u, 0u, 0u, 0u};
             if (kScaled) vsc[buf][row] = 0.f;
         }
@@ -218,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
 
     bf16x8 qf[KC];
     {
-        const uint16_t* q = a.q + b * a.qsb + h * a.qsh + i * a.qst + 8 * half;
+        const uint16_t* q = a.q + qr.b * a.qsb + h * a.qsh + i * a.qst + 8 * half;
 #pragma unroll
         for (int kc = 0; kc < KC; ++kc) qf[kc] = there ? load_bf16x8(q + 16 * kc) : zero_bf16x8();
     }
@@ -250,6 +302,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         va += 8 * (lane & 1);
         asm volatile("" : "+v"(ka), "+v"(va));
         const int rel = last - key0 - 4 * half;
+        // (kOwn: keys low .. last, by one comparison)
+        const uint32_t from = key0 + 4 * half - low, seen = max(last - low + 1, 0);
         floatx16 s[2];
         floatx4 kw[4], vw[4];              // scales of a half's keys
         auto scales = [&](int u) {
@@ -283,7 +337,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         // logit e of half u, scaled; a masked one is -inf whatever its row's scale
         auto logit = [&](int u, int e, float less) {
             float x = fmaf(s[u][e], kScaled ? kw[e >> 2][e & 3] : scale, -less);
-            if (MASKED) x = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? x : -INFINITY;
+            if (MASKED && PART != kOwn) x = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? x : -INFINITY;
+            if (MASKED && PART == kOwn) x = from + (32 * u + 8 * (e >> 2) + (e & 3)) < seen ? x : -INFINITY;
             return x;
         };
         // p of values 2 j, 2 j + 1 of half u relative to m, as bf16; their sum
@@ -401,13 +456,20 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         ++tile, buf ^= 1;
     };
     const int whole = min(max(all_see, 0) / kKeys, tile1);
-    while (tile < whole) step(Constant<0>{});
-    while (tile < tile1) step(Constant<1>{});
+    if constexpr (PART == kOwn) {
+        while (tile < tile1) {
+            if (tile < whole && tile * kKeys >= low) step(Constant<0>{});
+            else step(Constant<1>{});
+        }
+    } else {
+        while (tile < whole) step(Constant<0>{});
+        while (tile < tile1) step(Constant<1>{});
+    }
     l = half_sum(l);
     if (r >= a.rows) return;
     if (!there) l = 0.f;                   // (took part where nothing is masked)
     // value 4 w + j of o[t] is dim 32 t + 8 w + 4 half + j
-    if (a.splits > 1) {
+    if (PART != kWhole || a.splits > 1) {
         const int64_t pr = (static_cast<int64_t>(split) * gridDim.x + bc) * a.rows + r;
         float* po = a.part_o + pr * D + 4 * half;
 #pragma unroll
@@ -528,7 +590,7 @@ __device__ __forceinline__ void load_group(const char* src, char* dst, int row0,
 }
 
 // Workgroup: WAVES waves; (b, c) and a split of its keys.
-template <int D, int TYPE, int NR, int WAVES>
+template <int D, int TYPE, int NR, int WAVES, int PART = kWhole>
 __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
     using T = FewTile<D, TYPE, WAVES>;
     constexpr int kWaves = WAVES, kThreads = 64 * WAVES;
@@ -548,11 +610,14 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
     const int quarter = lane >> 4;
     char* const base = lds[wave];
 
-    const int nq = a.q_counts ? min(max(a.q_counts[b], 0), a.n) : a.n;
-    const int len = min(max(a.lens[bc], 0), a.max_len);
-    const int end = nq > 0 ? len : 0;      // keys that the rows see together
-    const int tiles = (end + T::kKeys - 1) / T::kKeys, per = (tiles + a.splits - 1) / a.splits;
-    const int tile0 = split * per + wave, tile1 = min(split * per + per, tiles);
+    // (kShared: queries of several sequences)
+    const int nq = PART == kShared ? 0 : queries_of(a, b);
+    const int len = PART == kShared ? shared_rows(a, b, c) : min(max(a.lens[bc], 0), a.max_len);
+    const int end = PART == kShared || nq > 0 ? len : 0;       // keys that the rows see together
+    const int low = PART == kOwn ? shared_rows(a, b / a.each, c) : 0;      // the first of them
+    const int tiles0 = low / T::kKeys, tiles = max((end + T::kKeys - 1) / T::kKeys, tiles0);
+    const int per = (tiles - tiles0 + a.splits - 1) / a.splits;
+    const int first0 = tiles0 + split * per, tile0 = first0 + wave, tile1 = min(first0 + per, tiles);
 
     // pages of the 16-row groups of a tile (-1: none)
     struct Ids {
@@ -602,10 +667,12 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
 #pragma unroll
     for (int j = 0; j < NR * 16 * QC / kWave; j += kWaves) {
         if (j + wave >= NR * 16 * QC / kWave) break;
-        const int r = (j + wave) * (kWave / QC) + lane / QC, i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
+        const int r = (j + wave) * (kWave / QC) + lane / QC;
+        const Query qr = query_of<PART>(a, b, r);
+        const int i = qr.i, h = c * a.Gh + qr.g;
         const int ch = (lane % QC) ^ ((QC == 16 ? r : r >> 1) & (QC - 1));
-        const bool there = r < a.rows && i < nq;
-        const char* src = there ? reinterpret_cast<const char*>(a.q + b * a.qsb + h * a.qsh + i * a.qst + 8 * ch)
+        const bool there = r < a.rows && i < (PART == kShared ? queries_of(a, qr.b) : nq);
+        const char* src = there ? reinterpret_cast<const char*>(a.q + qr.b * a.qsb + h * a.qsh + i * a.qst + 8 * ch)
                                 : reinterpret_cast<const char*>(kNoRows);
         load16_to_lds(src, qs + (j + wave) * 1024);
     }
@@ -620,13 +687,25 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
 
     // the last key that each of this lane's rows sees (below 0: none)
     int last[NR];
+    // keys that every row sees
+    int all_see = PART == kShared ? len : a.causal ? max(len - nq + 1, 0) : len;
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
-        const int r = 16 * x + (lane & 15), i = r / a.Gh;
-        last[x] = r < a.rows && i < nq ? (a.causal ? len - nq + i : len - 1) : -1;
+        const int r = 16 * x + (lane & 15);
+        if constexpr (PART == kShared) {
+            const Query qr = query_of<PART>(a, b, r);
+            const int n = queries_of(a, qr.b);
+            const bool there = r < a.rows && qr.i < n;
+            last[x] = there ? last_shared(a, qr, c, n, len) : -1;
+            int lo = there ? last[x] + 1 : len;
+#pragma unroll
+            for (int z = 1; z < 16; z *= 2) lo = min(lo, __shfl_xor(lo, z));
+            all_see = min(all_see, __builtin_amdgcn_readfirstlane(lo));
+        } else {
+            const int i = r / a.Gh;
+            last[x] = r < a.rows && i < nq ? (a.causal ? len - nq + i : len - 1) : -1;
+        }
     }
-    // keys that every row sees
-    const int all_see = a.causal ? max(len - nq + 1, 0) : len;
 
     floatx4 o[NR][NT];
     float m[NR], l[NR];
@@ -677,13 +756,13 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
         __builtin_amdgcn_sched_barrier(0);
         ids = pages_of(tile + 2 * kWaves);
         const int key0 = tile * T::kKeys;
-        if (key0 + T::kKeys > end) {
-            // rows behind the last key may hold anything: zeros, with zero scales
+        if (key0 + T::kKeys > end || (PART == kOwn && key0 < low)) {
+            // rows behind the last key (and before the first) may hold anything: zeros, with zero scales
             char* const vt = base + STAGE * T::kStage + T::kTile;
             float* const sc = reinterpret_cast<float*>(vt + T::kTile);
             for (int i = lane; i < T::kKeys * T::kCh; i += kWave)
-                if (key0 + i / T::kCh >= end) *reinterpret_cast<u32x4*>(vt + i * 16) = u32x4{0u, 0u, 0u, 0u};
-            if (T::kScaled && lane < T::kKeys && key0 + lane >= end) sc[lane] = 0.f, sc[T::kKeys + lane] = 0.f;
+                if (key0 + i / T::kCh >= end || (PART == kOwn && key0 + i / T::kCh < low)) *reinterpret_cast<u32x4*>(vt + i * 16) = u32x4{0u, 0u, 0u, 0u};
+            if (T::kScaled && lane < T::kKeys && (key0 + lane >= end || (PART == kOwn && key0 + lane < low))) sc[lane] = 0.f, sc[T::kKeys + lane] = 0.f;
         }
         // value e of s[x][u] is key key0 + 32 (u / 2) + 8 quarter + 4 (u % 2) + e
         floatx4 s[NR][NS];
@@ -742,16 +821,18 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
                 for (int x = 0; x < NR; ++x) s[x][u] *= __builtin_bit_cast(floatx4, w[u]);
             }
         }
-        if (key0 + T::kKeys > all_see) {
+        if (key0 + T::kKeys > all_see || (PART == kOwn && key0 < low)) {
             asm volatile("");              // (a branch: few tiles come here)
 #pragma unroll
             for (int x = 0; x < NR; ++x) {
-                const int rel = last[x] - key0 - 8 * quarter;
+                const int rel = last[x] - key0 - 8 * quarter, before = low - key0 - 8 * quarter;
 #pragma unroll
                 for (int u = 0; u < NS; ++u)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[x][u][e] = 32 * (u >> 1) + 4 * (u & 1) + e <= rel ? s[x][u][e] : -INFINITY;
+                    for (int e = 0; e < 4; ++e) {
+                        const int at = 32 * (u >> 1) + 4 * (u & 1) + e;
+                        s[x][u][e] = at <= rel && (PART != kOwn || at >= before) ? s[x][u][e] : -INFINITY;
+                    }
             }
         }
         bf16x8 p[NR][NS / 2];
@@ -865,7 +946,9 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
     __syncthreads();
     constexpr int G = D / 8;               // lanes of a row, 8 dims each
     for (int it = tid; it < a.rows * G; it += kThreads) {
-        const int r = it / G, d0 = 8 * (it - r * G), i = r / a.Gh;
+        const int r = it / G, d0 = 8 * (it - r * G);
+        const Query qr = query_of<PART>(a, b, r);
+        const int i = qr.i;
         float M = kNone, L = 0.f, x[8] = {};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml[w][r].x);
@@ -879,8 +962,8 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = fmaf(y0[e], f, x[e]), x[4 + e] = fmaf(y1[e], f, x[4 + e]);
         }
-        if (i >= nq) L = 0.f;              // (a row that is not there took part where nothing is masked)
-        if (a.splits > 1) {
+        if (i >= (PART == kShared ? queries_of(a, qr.b) : nq)) L = 0.f;    // (a row that is not there took part where nothing is masked)
+        if (PART != kWhole || a.splits > 1) {
             const int64_t pr = (static_cast<int64_t>(split) * gridDim.x + bc) * a.rows + r;
             float* po = a.part_o + pr * D + d0;
             *reinterpret_cast<float4*>(po) = make_float4(x[0], x[1], x[2], x[3]);
@@ -888,7 +971,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
             if (d0 == 0) a.part_ml[pr] = make_float2(M, L);
         } else {
             const float inv = 1.f / L;
-            const int h = c * a.Gh + (r - i * a.Gh);
+            const int h = c * a.Gh + qr.g;
             u32x4 v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = pack_bf16(x[2 * j] * inv, x[2 * j + 1] * inv);
@@ -906,7 +989,9 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
 constexpr int kJoinThreads = 256;
 constexpr int kJoinPer = 8;
 
-template <int D, int SG>
+// PARTS: the first a.shared_splits splits are of the rows that the sequences of a group
+// share, in whose order of rows they lie.
+template <int D, int SG, bool PARTS = false>
 __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
     constexpr int LANES = D / 8, kRowThreads = LANES * SG, kPerBlock = kJoinThreads / kRowThreads;
     __shared__ __align__(16) float sums[SG > 1 ? kJoinThreads : 1][8];
@@ -915,13 +1000,21 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
     const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * kPerBlock + threadIdx.x / kRowThreads;
     const int64_t rd = min(row, rows - 1);             // (rows behind the last one read it and write nothing)
+    int64_t rd_shared = rd;
+    if constexpr (PARTS) {
+        const int64_t bc = rd / a.rows;
+        const int b = static_cast<int>(bc / a.Hkv), c = static_cast<int>(bc - static_cast<int64_t>(b) * a.Hkv);
+        const int grp = b / a.each, s = b - grp * a.each;
+        rd_shared = ((static_cast<int64_t>(grp) * a.Hkv + c) * a.each + s) * a.rows + (rd - bc * a.rows);
+    }
     float m = kNone, l = 0.f, o[8] = {};
     for (int s0 = g; s0 < a.splits; s0 += SG * kJoinPer) {
         float2 v[kJoinPer];
         float4 x[kJoinPer], y[kJoinPer];
 #pragma unroll
         for (int j = 0; j < kJoinPer; ++j) {
-            const int64_t at = min(s0 + j * SG, a.splits - 1) * rows + rd;
+            const int sp = min(s0 + j * SG, a.splits - 1);
+            const int64_t at = sp * rows + (PARTS && sp < a.shared_splits ? rd_shared : rd);
             const float* po = a.part_o + at * D + 8 * lane;
             v[j] = a.part_ml[at];
             x[j] = *reinterpret_cast<const float4*>(po);
@@ -982,40 +1075,63 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
 constexpr int kMaxSplits = 64;             // splits of a head's rows
 constexpr int64_t kTileBlocks = 4 * kPlanCus;   // workgroups of many rows, where there are splits
 
-template <int D, int TYPE>
+template <int D, int TYPE, int PART = kWhole>
 void attend(const ChunkArgs& a, hipStream_t s) {
     const unsigned heads = static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hkv);
     if (a.rows > kFewRows) {
         const int tiles = (a.rows + kRows - 1) / kRows;
-        hipLaunchKernelGGL((chunk_kernel<D, TYPE>), dim3(heads, tiles * a.splits), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((chunk_kernel<D, TYPE, PART>), dim3(heads, tiles * a.splits), dim3(kThreads), 0, s, a);
         return;
     }
     const dim3 grid(heads, a.splits);
     constexpr int W = few_waves(D, TYPE, 1);
-    if (a.rows <= 16) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 1, W>), grid, dim3(64 * W), 0, s, a);
-    else if (a.rows <= 32) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 2, W>), grid, dim3(64 * W), 0, s, a);
-    else hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 4, 4>), grid, dim3(kThreads), 0, s, a);
+    if (a.rows <= 16) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 1, W, PART>), grid, dim3(64 * W), 0, s, a);
+    else if (a.rows <= 32) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 2, W, PART>), grid, dim3(64 * W), 0, s, a);
+    else hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 4, 4, PART>), grid, dim3(kThreads), 0, s, a);
+}
+
+template <int D, int PART = kWhole>
+hipError_t attend_type(const ChunkArgs& a, hipStream_t s) {
+    if (a.pages.dtype == kCacheBf16) attend<D, kCacheBf16, PART>(a, s);
+    else if (a.pages.dtype == kCacheE4m3) attend<D, kCacheE4m3, PART>(a, s);
+    else attend<D, kCacheI8, PART>(a, s);
+    return hipGetLastError();
+}
+
+template <int D, bool PARTS = false>
+hipError_t join(const ChunkArgs& a, hipStream_t s) {
+    // a row's splits in one round of loads (kMaxSplits: four of the eight places of 16
+    // groups; eight groups took the same time)
+    const auto run = [&](auto groups) {
+        constexpr int SG = decltype(groups)::value, kPer = kJoinThreads / (D / 8 * SG);
+        const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
+        hipLaunchKernelGGL((chunk_join_kernel<D, SG, PARTS>), dim3(static_cast<unsigned>((rows + kPer - 1) / kPer)),
+                           dim3(kJoinThreads), 0, s, a);
+    };
+    if (a.splits <= kJoinPer) run(Constant<1>{});
+    else if (a.splits <= 4 * kJoinPer) run(Constant<4>{});
+    else run(Constant<16>{});
+    return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch(const ChunkArgs& a, hipStream_t s) {
-    if (a.pages.dtype == kCacheBf16) attend<D, kCacheBf16>(a, s);
-    else if (a.pages.dtype == kCacheE4m3) attend<D, kCacheE4m3>(a, s);
-    else attend<D, kCacheI8>(a, s);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    // a row's splits in one round of loads (kMaxSplits: four of the eight places of 16
-    // groups; eight groups took the same time)
-    const auto join = [&](auto groups) {
-        constexpr int SG = decltype(groups)::value, kPer = kJoinThreads / (D / 8 * SG);
-        const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
-        hipLaunchKernelGGL((chunk_join_kernel<D, SG>), dim3(static_cast<unsigned>((rows + kPer - 1) / kPer)),
-                           dim3(kJoinThreads), 0, s, a);
-    };
-    if (a.splits <= kJoinPer) join(Constant<1>{});
-    else if (a.splits <= 4 * kJoinPer) join(Constant<4>{});
-    else join(Constant<16>{});
-    return hipGetLastError();
+    const hipError_t e = attend_type<D>(a, s);
+    return e != hipSuccess || a.splits == 1 ? e : join<D>(a, s);
+}
+
+template <int D>
+hipError_t launch_parts(const ChunkArgs& shared, const ChunkArgs& own, hipStream_t s) {
+    hipError_t e = attend_type<D, kShared>(shared, s);
+    if (e != hipSuccess) return e;
+    e = attend_type<D, kOwn>(own, s);
+    if (e != hipSuccess) return e;
+    ChunkArgs a = own;
+    a.part_o = shared.part_o;
+    a.part_ml = shared.part_ml;
+    a.shared_splits = shared.splits;
+    a.splits = shared.splits + own.splits;
+    return join<D, true>(a, s);
 }
 
 }  // namespace
@@ -1103,6 +1219,10 @@ size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d) {
 
 hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t s) {
     return a.d == 64 ? launch<64>(a, s) : launch<128>(a, s);
+}
+
+hipError_t launch_shared_attention(const ChunkArgs& shared, const ChunkArgs& own, hipStream_t s) {
+    return own.d == 64 ? launch_parts<64>(shared, own, s) : launch_parts<128>(shared, own, s);
 }
 
 }  // namespace mmskv

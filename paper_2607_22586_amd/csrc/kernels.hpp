@@ -207,6 +207,12 @@ struct ChunkArgs {
     float scale;               // log2(e) / sqrt(d)
     float* part_o;             // [splits, B, Hkv, rows, d] sums of 2^(x - m) v (splits > 1)
     float2* part_ml;           // [splits, B, Hkv, rows] (m, sum of 2^(x - m)), base 2
+    // attention over a shared prefix: B is the number of groups in the launch over the
+    // shared rows, whose rows are each * Gh * n
+    const int32_t* shared;     // [groups, Hkv] leading rows that a group's sequences share
+    int each;                  // sequences of a group
+    int shared_max;            // upper bound of shared
+    int shared_splits;         // in the join: splits of the shared rows among a.splits
 };
 int chunk_splits(int64_t heads, int rows, int T, int d, int dtype);
 // Workspace bytes that suffice for every plan of a problem and never fall as
@@ -284,6 +290,8 @@ hipError_t launch_shape_scores(const ShapeArgs& a, hipStream_t s);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t s);
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t s);
 hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t s);
+// Both parts' sums in one array: shared.splits, then own.splits.
+hipError_t launch_shared_attention(const ChunkArgs& shared, const ChunkArgs& own, hipStream_t s);
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s);
 hipError_t launch_book(const BookArgs& a, int op, hipStream_t s);
 

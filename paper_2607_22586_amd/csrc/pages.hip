@@ -143,17 +143,18 @@ __global__ void __launch_bounds__(kBookThreads) book_plan_kernel(BookArgs a) {
     int run = 0;                           // free pages before the chunks looked at
     for (int64_t x0 = 0; x0 < a.chunks && want > 0 && run < hi; x0 += kBookThreads) {
         const int n = x0 + tid < a.chunks ? a.free[x0 + tid] : 0;
-        upto[tid] = block_scan(n, lds, &total);
-        __syncthreads();
-        for (int i = 0; i < kBookThreads && run + total > lo; ++i) {
-            const int before = run + (i ? upto[i - 1] : 0), after = run + upto[i];
-            if (before == after || after <= lo) continue;
-            if (before >= hi) break;
+        const int mine = run + block_scan(n, lds, &total);
+        upto[tid] = mine;
+        // the chunks that hold free pages of ranks in [lo, hi)
+        const int i0 = __syncthreads_count(mine <= lo), i1 = min(__syncthreads_count(mine < hi), kBookThreads - 1);
+        for (int i = i0; i <= i1; ++i) {
+            const int before = i ? upto[i - 1] : run;
+            if (before == upto[i]) continue;
             const int64_t p0 = (x0 + i) * kChunk + tid * (kChunk / kBookThreads);
-            int mine = 0, all;
+            int here = 0, all;
 #pragma unroll
-            for (int j = 0; j < kChunk / kBookThreads; ++j) mine += p0 + j < a.pages.n_pages && a.refs[p0 + j] == 0;
-            int rank = before + block_scan(mine, lds, &all) - mine;
+            for (int j = 0; j < kChunk / kBookThreads; ++j) here += p0 + j < a.pages.n_pages && a.refs[p0 + j] == 0;
+            int rank = before + block_scan(here, lds, &all) - here;
 #pragma unroll
             for (int j = 0; j < kChunk / kBookThreads; ++j) {
                 if (p0 + j >= a.pages.n_pages || a.refs[p0 + j] != 0) continue;

@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
     const uint32_t sees = there ? hi - lo : 0;
     const int key00 = lo_first;            // the first tile's first key
     const int tiles = (hi_last - key00 + kKeys - 1) / kKeys;
-    // tiles [clear0, clear1): every row of the tile that is there sees all keys
+    // tiles [clear0, clear1): every row that is there sees all keys
     const int clear0 = (lo_last - key00 + kKeys - 1) / kKeys, clear1 = (hi_first - key00) / kKeys;
 
     const uint16_t* const kb = a.k + b * a.ksb + c * a.ksh;
@@ -141,17 +141,35 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
     // staged order stands for.
     const auto k_tile = [&](auto which) { return decltype(which)::value ? kt1 : kt0; };
     const auto v_tile = [&](auto which) { return decltype(which)::value ? vt1 : vt0; };
-    auto load = [&](int tile, auto which) {
-        const int key0 = key00 + tile * kKeys, row0 = kWaveRows * wave + lane / kCh;
-        const char* const ks = reinterpret_cast<const char*>(kb + key0 * a.kst);
-        const char* const vs = reinterpret_cast<const char*>(vb + key0 * a.vst);
-        const int most = a.T - 1 - key0;   // (rows behind the last token: the last, which their mask keeps out)
+    // In-tile offsets of 32 bits beside addresses that the whole wave has in common.
+    const int ld_row = lane / kCh;
+    uint32_t k_off[kLoads], v_off[kLoads];
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int r = row0 + j * (64 / kCh), t = min(r, most), to = (kWaveRows * wave + j * (64 / kCh)) * 2 * D;
-            const int ch = (staged<D>(r, lane % kCh) - r * 2 * D);
-            load_tile16(ks + 2 * static_cast<int64_t>(t) * a.kst + ch, k_tile(which) + to);
-            load_tile16(vs + 2 * static_cast<int64_t>(t) * a.vst + ch, v_tile(which) + to);
+    for (int j = 0; j < kLoads; ++j) {
+        const int r = kWaveRows * wave + j * (64 / kCh) + ld_row, ch = staged<D>(r, lane % kCh) - r * 2 * D;
+        k_off[j] = 2 * static_cast<uint32_t>(ld_row * a.kst) + ch;
+        v_off[j] = 2 * static_cast<uint32_t>(ld_row * a.vst) + ch;
+    }
+    auto load = [&](int key0, auto which) {
+        char* const kd = k_tile(which) + kWaveRows * wave * 2 * D;
+        char* const vd = v_tile(which) + kWaveRows * wave * 2 * D;
+        const int t0 = key0 + kWaveRows * wave;
+        if (t0 + kWaveRows <= a.T) {
+            const char* const ks = reinterpret_cast<const char*>(kb + t0 * a.kst);
+            const char* const vs = reinterpret_cast<const char*>(vb + t0 * a.vst);
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                load_tile16(ks + j * (64 / kCh) * 2 * a.kst + k_off[j], kd + 1024 * j);
+                load_tile16(vs + j * (64 / kCh) * 2 * a.vst + v_off[j], vd + 1024 * j);
+            }
+        } else {                           // (rows behind the last token: the last, which their mask keeps out)
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int r = j * (64 / kCh) + ld_row;
+                const int64_t t = min(t0 + r, a.T - 1), over = t - ld_row;
+                load_tile16(reinterpret_cast<const char*>(kb + over * a.kst) + k_off[j], kd + 1024 * j);
+                load_tile16(reinterpret_cast<const char*>(vb + over * a.vst) + v_off[j], vd + 1024 * j);
+            }
         }
     };
 
@@ -332,32 +350,45 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
                 }
         }
     };
-    const auto is_clear = [&](int tile) { return tile >= clear0 && tile < clear1; };
 
-    if (tid < 2) poisoned[tid] = -1;
-    __syncthreads();
-    load(0, Constant<0>{});
-    wait_vm<0>();
-    if (!is_clear(0)) clean(0, Constant<0>{});
-    __syncthreads();
-    auto step = [&](int tile, auto which) {
+    // The tiles that some row sees in part first (those before the clear ones, then those
+    // behind: the rows' own keys, whose logits are likely large), each half of them in a
+    // loop of its own.  The stages take turns so that the clear ones begin with stage 0.
+    const int masked = tiles - max(clear1 - clear0, 0), ahead = min(clear0, masked);
+    const auto key_of = [&](int n) {       // first key of the n-th tile worked on
+        const int tile = n < ahead ? n : n < masked ? n + (tiles - masked) : n - masked + ahead;
+        return key00 + tile * kKeys;
+    };
+    auto step = [&](int n, auto which, auto part) {
         constexpr int W = decltype(which)::value;
-        const bool more = tile + 1 < tiles;
-        if (more) load(tile + 1, Constant<1 - W>{});
-        const int key0 = key00 + tile * kKeys;
-        if (is_clear(tile)) {
-            attend(key0, which, Constant<0>{});
-        } else {
-            attend(key0, which, Constant<1>{});
-            if (poisoned[W] == tile) add_poison(key0);
-        }
+        if (n + 1 < tiles) load(key_of(n + 1), Constant<1 - W>{});
+        attend(key_of(n), which, part);
+        if (decltype(part)::value && poisoned[W] == n) add_poison(key_of(n));
         wait_vm<0>();
-        if (more && !is_clear(tile + 1)) clean(tile + 1, Constant<1 - W>{});
+        if (decltype(part)::value && n + 1 < masked) clean(n + 1, Constant<1 - W>{});
         __syncthreads();
     };
-    for (int tile = 0; tile < tiles; tile += 2) {
-        step(tile, Constant<0>{});
-        if (tile + 1 < tiles) step(tile + 1, Constant<1>{});
+    if (tid < 2) poisoned[tid] = -1;
+    __syncthreads();
+    if (masked & 1) {
+        load(key_of(0), Constant<1>{});
+        wait_vm<0>();
+        clean(0, Constant<1>{});
+    } else {
+        load(key_of(0), Constant<0>{});
+        wait_vm<0>();
+        if (masked) clean(0, Constant<0>{});
+    }
+    __syncthreads();
+    int n = 0;
+    if (masked & 1) step(n++, Constant<1>{}, Constant<1>{});
+    while (n < masked) {
+        step(n++, Constant<0>{}, Constant<1>{});
+        step(n++, Constant<1>{}, Constant<1>{});
+    }
+    while (n < tiles) {
+        step(n++, Constant<0>{}, Constant<0>{});
+        if (n < tiles) step(n++, Constant<1>{}, Constant<0>{});
     }
     l = half_sum(l);
     if (LSE) l_all = half_sum(l_all);

@@ -23,6 +23,9 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
+// (lambdas of a kernel's registers that are called in several places)
+#define kInline __attribute__((always_inline))
+
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 32 * kWaves;         // query rows of a workgroup
@@ -150,28 +153,23 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
         k_off[j] = 2 * static_cast<uint32_t>(ld_row * a.kst) + ch;
         v_off[j] = 2 * static_cast<uint32_t>(ld_row * a.vst) + ch;
     }
-    auto load = [&](int key0, auto which) {
-        char* const kd = k_tile(which) + kWaveRows * wave * 2 * D;
-        char* const vd = v_tile(which) + kWaveRows * wave * 2 * D;
+    auto load = [&](const uint16_t* base, int64_t stride, const uint32_t (&off)[kLoads], int key0, char* tile) kInline {
+        char* const to = tile + kWaveRows * wave * 2 * D;
         const int t0 = key0 + kWaveRows * wave;
         if (t0 + kWaveRows <= a.T) {
-            const char* const ks = reinterpret_cast<const char*>(kb + t0 * a.kst);
-            const char* const vs = reinterpret_cast<const char*>(vb + t0 * a.vst);
+            const char* const src = reinterpret_cast<const char*>(base + t0 * stride);
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                load_tile16(ks + j * (64 / kCh) * 2 * a.kst + k_off[j], kd + 1024 * j);
-                load_tile16(vs + j * (64 / kCh) * 2 * a.vst + v_off[j], vd + 1024 * j);
-            }
+            for (int j = 0; j < kLoads; ++j) load_tile16(src + j * (64 / kCh) * 2 * stride + off[j], to + 1024 * j);
         } else {                           // (rows behind the last token: the last, which their mask keeps out)
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
-                const int r = j * (64 / kCh) + ld_row;
-                const int64_t t = min(t0 + r, a.T - 1), over = t - ld_row;
-                load_tile16(reinterpret_cast<const char*>(kb + over * a.kst) + k_off[j], kd + 1024 * j);
-                load_tile16(reinterpret_cast<const char*>(vb + over * a.vst) + v_off[j], vd + 1024 * j);
+                const int64_t t = min(t0 + j * (64 / kCh) + ld_row, a.T - 1) - ld_row;
+                load_tile16(reinterpret_cast<const char*>(base + t * stride) + off[j], to + 1024 * j);
             }
         }
     };
+    const auto load_k = [&](int key0, auto which) kInline { load(kb, a.kst, k_off, key0, k_tile(which)); };
+    const auto load_v = [&](int key0, auto which) kInline { load(vb, a.vst, v_off, key0, v_tile(which)); };
 
     bf16x8 qf[KC];
     {
@@ -186,124 +184,101 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
         for (int j = 0; j < 16; ++j) o[t][j] = 0.f;
     float m = kNone, l = 0.f, l_all = 0.f;             // (l_all: of the weights before their rounding)
 
-    // One tile in two 32-key halves u, as a sequence of steps of one matrix instruction
-    // with vector instructions to run beside it: the exponentials of half 0 with the
-    // second half's S, those of half 1 with the first half's part of O.  Value e of s[u] is key key0 + 32 u + 8 (e / 4) +
-    // 4 half + e % 4.  MASKED: some row does not see all.
-    auto attend = [&](int key0, auto which, auto masked) {
-        const char* const kt = k_tile(which);
-        char* const vt = v_tile(which);
-        constexpr bool MASKED = decltype(masked)::value != 0;
-        constexpr int N = KC;              // steps of a phase: KC = 2 NT
-        constexpr int PAIRS = 8 / N;       // pairs of exponentials of a step
-        constexpr int AHEAD = 4;           // steps from a read of LDS to its use
-        static_assert(N == 2 * NT, "as many steps in S as in O");
-        int ka = staged<D>(lane & 31, half), va = staged<D>(4 * half + ((lane & 15) >> 2), (lane & 16) / 8 + ((lane & 3) >> 1));
-        va += 8 * (lane & 1);
-        asm volatile("" : "+v"(ka), "+v"(va));         // (formed where they are used, not kept)
-        const uint32_t rel = key0 + 4 * half - lo;
-        floatx16 s[2];
-        auto k_frag = [&](int j) {         // step j % N of half j / N
-            return load_bf16x8(reinterpret_cast<const uint16_t*>(kt + j / N * 32 * 2 * D + (ka ^ (32 * (j % N)))));
-        };
-        auto v_frag = [&](int j) {         // half j / N, step j % N: keys 16 w .., dims 32 t ..
-            typedef s16x4 __attribute__((address_space(3))) * lds4;
-            const int u = j / N, w = j % N / NT, t = j % NT;
-            u32x4 v;
+    // The keys are worked on in halves of a tile, 32 at a time, as a sequence of steps,
+    // each with a matrix instruction of the next half's S, one of the part that the half
+    // before has in O, and this half's exponentials beside them: the matrix pipe and the
+    // vector one have about the same to do in every step.  (Left to itself the compiler
+    // puts the matrix instructions of a phase first, and a SIMD's two waves do not fill
+    // the gaps.)  Value e of a lane's s is key key0 + 8 (e / 4) + 4 half + e % 4.
+    // MASKED: some row does not see all keys.
+    floatx16 s[2];                         // of this half and the next, in turn
+    uint32_t p[2][8];                      // weights of this half and the one before, pairs of bf16
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (lds4)(vt + (32 * u + 16 * w + 8 * z) * 2 * D + (va ^ (64 * t + 32 * z))));
-                const u32x2 y = __builtin_bit_cast(u32x2, x);
-                v[2 * z] = y[0];
-                v[2 * z + 1] = y[1];
-            }
-            return __builtin_bit_cast(bf16x8, v);
-        };
-        auto logit = [&](int u, int e, float less) {
-            float x = fmaf(s[u][e], a.scale, -less);
-            if (MASKED) x = rel + (32 * u + 8 * (e >> 2) + (e & 3)) < sees ? x : -INFINITY;
+    for (int j = 0; j < 8; ++j) p[1][j] = 0;
+    const int ka0 = staged<D>(lane & 31, half);
+    const int va0 = staged<D>(4 * half + ((lane & 15) >> 2), (lane & 16) / 8 + ((lane & 3) >> 1)) + 8 * (lane & 1);
+    auto k_frag = [&](const char* kt, int ka, int j) kInline {             // dims 16 j ..
+        return load_bf16x8(reinterpret_cast<const uint16_t*>(kt + (ka ^ (32 * j))));
+    };
+    auto v_frag = [&](char* vt, int va, int j) kInline {                   // keys 16 w .., dims 32 t ..
+        typedef s16x4 __attribute__((address_space(3))) * lds4;
+        const int w = j / NT, t = j % NT;
+        u32x4 v;
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            const s16x4 x =
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vt + (16 * w + 8 * z) * 2 * D + (va ^ (64 * t + 32 * z))));
+            const u32x2 y = __builtin_bit_cast(u32x2, x);
+            v[2 * z] = y[0];
+            v[2 * z + 1] = y[1];
+        }
+        return __builtin_bit_cast(bf16x8, v);
+    };
+    auto p_frag = [](const uint32_t (&x)[8], int w) kInline {
+        return __builtin_bit_cast(bf16x8, (u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]}));
+    };
+    const auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+    // which: this half's place in s and p; kt, vt: the next half's K, the V of the one before
+    auto attend = [&](int key0, auto which, auto masked, const char* kt, char* vt) kInline {
+        constexpr int U = decltype(which)::value;
+        constexpr bool MASKED = decltype(masked)::value != 0;
+        constexpr int N = KC;              // steps: KC of S, 2 NT of O
+        constexpr int PAIRS = 8 / N;       // pairs of exponentials of a step
+        constexpr int AHEAD = 2;           // steps from a read of LDS to its use
+        static_assert(N == 2 * NT, "as many steps in S as in O");
+        int ka = ka0, va = va0;
+        asm volatile("" : "+v"(ka), "+v"(va));         // (permuted addresses are formed where they are used, not kept)
+        const uint32_t rel = key0 + 4 * half - lo;
+        auto logit = [&](int e, float less) kInline {
+            float x = fmaf(s[U][e], a.scale, -less);
+            if (MASKED) x = rel + (8 * (e >> 2) + (e & 3)) < sees ? x : -INFINITY;
             return x;
         };
-        // p of values 2 j, 2 j + 1 of half u relative to m, as bf16.  The quotient's sum is
-        // of the weights as the product with V takes them, so that what their roundings
-        // have in common leaves it; the log-sum-exp's is of the weights before.
-        struct Sums {
-            float rounded = 0.f, all = 0.f;
-        };
-        auto pair = [&](int u, int j, Sums& sum) {
-            const float x0 = fast_exp2(logit(u, 2 * j, m)), x1 = fast_exp2(logit(u, 2 * j + 1, m));
+        // Weights of values 2 j, 2 j + 1 relative to m, as bf16.  The quotient's sum is of
+        // the weights as the product with V takes them, so that what their roundings have
+        // in common leaves it; the log-sum-exp's is of the weights before.
+        float sum = 0.f, sum_all = 0.f;
+        auto pair = [&](int j) kInline {
+            const float x0 = fast_exp2(logit(2 * j, m)), x1 = fast_exp2(logit(2 * j + 1, m));
             const uint32_t y = pack_bf16(x0, x1);
-            sum.rounded += __uint_as_float(y << 16) + __uint_as_float(y & 0xFFFF0000u);
-            if (LSE) sum.all += x0 + x1;
-            return y;
+            sum += __uint_as_float(y << 16) + __uint_as_float(y & 0xFFFF0000u);
+            if (LSE) sum_all += x0 + x1;
+            p[U][j] = y;
         };
-        auto settle = [&](int u, uint32_t (&p)[8], Sums sum) {
-            if (__any(!(sum.rounded < kBehind))) {
-                float mx = kNone;
+        bf16x8 fk[N], fv[N];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, logit(u, e, 0.f));
-                mx = fmaxf(half_max(mx) + kLead, m);
-                const float f = fast_exp2(m - mx);
-                m = mx;
-                l *= f;
-                l_all *= f;
+        for (int j = 0; j < AHEAD; ++j) fk[j] = k_frag(kt, ka, j), fv[j] = v_frag(vt, va, j);
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) o[t][j] *= f;
-                sum = Sums{};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) p[j] = pair(u, j, sum);
-            }
-            l += sum.rounded;
-            l_all += sum.all;
-        };
-        auto p_frag = [](const uint32_t (&p)[8], int w) {
-            return __builtin_bit_cast(bf16x8, (u32x4{p[4 * w], p[4 * w + 1], p[4 * w + 2], p[4 * w + 3]}));
-        };
-        const auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-
-        bf16x8 f[2 * N];
-        uint32_t p0[8], p1[8];
-        Sums sum;
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) f[j] = k_frag(j);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
-#pragma unroll
-        for (int j = 0; j < 2 * N; ++j) {
-            fence();
-            if (j + AHEAD < 2 * N) f[j + AHEAD] = k_frag(j + AHEAD);
-            s[j / N] = mfma32(f[j], qf[j % N], s[j / N]);
-            if (j >= N) {
-#pragma unroll
-                for (int z = 0; z < PAIRS; ++z) p0[(j - N) * PAIRS + z] = pair(0, (j - N) * PAIRS + z, sum);
-            }
-        }
-        fence();
-        settle(0, p0, sum);
-        sum = Sums{};
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) f[j] = v_frag(j);
+        for (int e = 0; e < 16; ++e) s[1 - U][e] = 0.f;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             fence();
-            f[j + AHEAD] = v_frag(j + AHEAD);
-            o[j % NT] = mfma32(f[j], p_frag(p0, j / NT), o[j % NT]);
+            if (j + AHEAD < N) fk[j + AHEAD] = k_frag(kt, ka, j + AHEAD), fv[j + AHEAD] = v_frag(vt, va, j + AHEAD);
+            s[1 - U] = mfma32(fk[j], qf[j], s[1 - U]);
+            o[j % NT] = mfma32(fv[j], p_frag(p[1 - U], j / NT), o[j % NT]);
 #pragma unroll
-            for (int z = 0; z < PAIRS; ++z) p1[j * PAIRS + z] = pair(1, j * PAIRS + z, sum);
+            for (int z = 0; z < PAIRS; ++z) pair(j * PAIRS + z);
         }
         fence();
-        settle(1, p1, sum);
+        if (__any(!(sum < kBehind))) {     // the reference moves
+            float mx = kNone;
 #pragma unroll
-        for (int j = N; j < 2 * N; ++j) {
-            fence();
-            if (j + AHEAD < 2 * N) f[j + AHEAD] = v_frag(j + AHEAD);
-            o[j % NT] = mfma32(f[j], p_frag(p1, (j - N) / NT), o[j % NT]);
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, logit(e, 0.f));
+            mx = fmaxf(half_max(mx) + kLead, m);
+            const float f = fast_exp2(m - mx);
+            m = mx;
+            l *= f;
+            l_all *= f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[t][j] *= f;
+            sum = sum_all = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) pair(j);
         }
+        l += sum;
+        l_all += sum_all;
         fence();
     };
 
@@ -311,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
     // in its V would.  Tiles that some row sees in part are looked over as they are
     // staged; values that are not finite become zeros there, and are added by hand to
     // the rows that see them (whose results are then not finite whatever the weight).
-    auto clean = [&](int tile, auto which) {           // (a wave: of what it has staged itself)
+    auto clean = [&](int tile, auto which) kInline {           // (a wave: of what it has staged itself)
         char* const at = v_tile(which) + kWaveRows * wave * 2 * D + 16 * lane;
         u32x4 x[kLoads];
         bool bad = false;
@@ -333,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
         }
         poisoned[decltype(which)::value] = tile;
     };
-    auto add_poison = [&](int key0) {
+    auto add_poison = [&](int key0) kInline {
         for (int x = 0; x < kKeys; ++x) {
             const int64_t t = min(key0 + x, a.T - 1);
             const bool seen = static_cast<uint32_t>(key0 + x - lo) < sees;
@@ -359,36 +334,63 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
         const int tile = n < ahead ? n : n < masked ? n + (tiles - masked) : n - masked + ahead;
         return key00 + tile * kKeys;
     };
-    auto step = [&](int n, auto which, auto part) {
+    // Tile n, in stage W: K of the next tile and V of this one have landed by the middle
+    // of it, where the stages of K of this tile and V of the one before are free again.
+    constexpr int kHalf = kKeys / 2 * 2 * D;
+    auto step = [&](int n, auto which, auto part) kInline {
         constexpr int W = decltype(which)::value;
-        if (n + 1 < tiles) load(key_of(n + 1), Constant<1 - W>{});
-        attend(key_of(n), which, part);
-        if (decltype(part)::value && poisoned[W] == n) add_poison(key_of(n));
+        const int key0 = key_of(n);
+        attend(key0, Constant<0>{}, part, k_tile(which) + kHalf, v_tile(Constant<1 - W>{}) + kHalf);
         wait_vm<0>();
-        if (decltype(part)::value && n + 1 < masked) clean(n + 1, Constant<1 - W>{});
+        if (decltype(part)::value) clean(n, which);
         __syncthreads();
+        if (n + 2 < tiles) load_k(key_of(n + 2), which);
+        if (n + 1 < tiles) load_v(key_of(n + 1), Constant<1 - W>{});
+        attend(key0 + kKeys / 2, Constant<1>{}, part, k_tile(Constant<1 - W>{}), v_tile(which));
+        if (decltype(part)::value && poisoned[W] == n) add_poison(key0);
     };
-    if (tid < 2) poisoned[tid] = -1;
-    __syncthreads();
-    if (masked & 1) {
-        load(key_of(0), Constant<1>{});
+    // before the first tile, in stage W: its first half's S, and no weights for the half
+    // before, whose V are zeros
+    auto begin = [&](auto which) kInline {
+        constexpr int W = decltype(which)::value;
+        load_k(key_of(0), which);
+        char* const vt = v_tile(Constant<1 - W>{}) + kHalf;
+        for (int x = 16 * tid; x < kHalf; x += 16 * kThreads) *reinterpret_cast<u32x4*>(vt + x) = u32x4{0u, 0u, 0u, 0u};
         wait_vm<0>();
-        clean(0, Constant<1>{});
-    } else {
-        load(key_of(0), Constant<0>{});
-        wait_vm<0>();
-        if (masked) clean(0, Constant<0>{});
-    }
-    __syncthreads();
+        __syncthreads();
+        if (tiles > 1) load_k(key_of(1), Constant<1 - W>{});
+        load_v(key_of(0), which);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < KC; ++j) s[0] = mfma32(k_frag(k_tile(which), ka0, j), qf[j], s[0]);
+    };
+    auto end = [&](auto which) kInline {           // the last half's part of O, of the tile in stage W
+#pragma unroll
+        for (int j = 0; j < KC; ++j)
+            o[j % NT] = mfma32(v_frag(v_tile(which) + kHalf, va0, j), p_frag(p[1], j / NT), o[j % NT]);
+    };
+    if (tid < 2) poisoned[tid] = -1;       // (seen by all behind the barriers of begin)
     int n = 0;
-    if (masked & 1) step(n++, Constant<1>{}, Constant<1>{});
+    if (masked & 1) {
+        begin(Constant<1>{});
+        step(n++, Constant<1>{}, Constant<1>{});
+    } else {
+        begin(Constant<0>{});
+    }
     while (n < masked) {
         step(n++, Constant<0>{}, Constant<1>{});
         step(n++, Constant<1>{}, Constant<1>{});
     }
-    while (n < tiles) {
+    while (n + 1 < tiles) {
         step(n++, Constant<0>{}, Constant<0>{});
-        if (n < tiles) step(n++, Constant<1>{}, Constant<0>{});
+        step(n++, Constant<1>{}, Constant<0>{});
+    }
+    if (n < tiles) {
+        step(n++, Constant<0>{}, Constant<0>{});
+        end(Constant<0>{});
+    } else {
+        end(Constant<1>{});
     }
     l = half_sum(l);
     if (LSE) l_all = half_sum(l_all);

@@ -1149,14 +1149,11 @@ int mmshiftkv_shared_attention(const mmskv_shape* shape, const mmskv_pages* page
     a.shared = shared;
     a.each = shape->B / groups;
     a.shared_max = shared_T < a.max_len ? shared_T : a.max_len;
-    // the part behind the shared rows, whose plan takes all to be as long as the bounds say
     ChunkArgs pre = a;
     pre.B = groups;
     pre.rows = a.each * a.rows;
     pre.pages.table = shared_table;
-    pre.splits = chunk_splits(static_cast<int64_t>(groups) * a.Hkv, pre.rows, a.shared_max, a.d, a.pages.dtype);
-    const int mine = a.max_len - a.shared_max;
-    a.splits = chunk_splits(static_cast<int64_t>(a.B) * a.Hkv, a.rows, mine > 64 ? mine : 64, a.d, a.pages.dtype);
+    plan_parts(&pre, &a);
     const size_t need = shared_ws(shape, groups, n);
     if (workspace == nullptr || !aligned(workspace, kAlign) || workspace_bytes < need) return MMSKV_EWORKSPACE;
     const size_t rows = static_cast<size_t>(a.B) * a.Hkv * a.rows, all = (pre.splits + a.splits) * rows;

@@ -82,19 +82,36 @@ __device__ __forceinline__ int staged(int r, int ch) {
     return r * (2 * D) + 16 * (ch ^ swz);
 }
 
-// What a launch works on: all rows that a sequence sees; the rows that the sequences of
-// a group share, for the queries of all of them (b is the group, pages.table the groups'
-// and row r = (s * n + i) * Gh + g query i of the group's sequence s); or those behind
-// the shared ones.  The last two leave partial sums only.
-constexpr int kWhole = 0, kShared = 1, kOwn = 2;
+// What a workgroup works on: all rows that a sequence sees (PARTS = false); or one of the
+// two parts of an attention over a shared prefix, of which it leaves partial sums: the
+// rows that the sequences of a group share, for the queries of all of them (b is the
+// group, pages.table the groups' and row r = (s * n + i) * Gh + g query i of the group's
+// sequence s), or those behind the shared ones.
+template <bool PARTS>
+struct Work {
+    ChunkArgs a;
+    bool shared;                           // which part
+    int bc, slot, slots;                   // (b, c), and the place among the workgroups of it
+};
+template <bool PARTS, class ARGS>
+__device__ __forceinline__ Work<PARTS> work_of(const ARGS& all) {
+    if constexpr (PARTS) {
+        const bool shared = static_cast<int>(blockIdx.x) < all.first_own;
+        const ChunkArgs a = shared ? all.shared : all.own;
+        const int x = blockIdx.x - (shared ? 0 : all.first_own), heads = a.B * a.Hkv, slot = x / heads;
+        const int slots = (shared ? all.first_own : static_cast<int>(gridDim.x) - all.first_own) / heads;
+        return {a, shared, x - slot * heads, slot, slots};
+    } else {
+        return {all, false, static_cast<int>(blockIdx.x), static_cast<int>(blockIdx.y), static_cast<int>(gridDim.y)};
+    }
+}
 
 // A query row: its sequence, query, and head within the KV head.
 struct Query {
     int b, i, g;
 };
-template <int PART>
-__device__ __forceinline__ Query query_of(const ChunkArgs& a, int b, int r) {
-    if constexpr (PART == kShared) {
+__device__ __forceinline__ Query query_of(const ChunkArgs& a, bool shared, int b, int r) {
+    if (shared) {
         const int per = a.Gh * a.n, s = r / per, x = r - s * per, i = x / a.Gh;
         return {b * a.each + min(s, a.each - 1), i, x - i * a.Gh};
     } else {
@@ -115,8 +132,11 @@ __device__ __forceinline__ int last_shared(const ChunkArgs& a, const Query& q, i
     return min(a.causal ? len - nq + q.i : len - 1, shared - 1);
 }
 
-template <int D, int TYPE, int PART = kWhole>
-__global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
+template <int D, int TYPE, bool PARTS = false, class ARGS = ChunkArgs>
+__global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
+    const Work<PARTS> job = work_of<PARTS>(all);
+    const ChunkArgs& a = job.a;
+    const bool shared = PARTS && job.shared;
     constexpr int KC = D / 16;             // 16-dim steps of S
     constexpr int NT = D / 32;             // 32-dim tiles of O
     constexpr int kRow = D * kCacheBytes<TYPE>;      // bytes of a cached row
@@ -129,27 +149,27 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     __shared__ __align__(16) char vt[2][kKeys * 2 * D];
     __shared__ __align__(16) float ksc[2][kScaled ? kKeys : 4], vsc[2][kScaled ? kKeys : 4];
 
-    const int bc = blockIdx.x, b = bc / a.Hkv, c = bc - b * a.Hkv;
+    const int bc = job.bc, b = bc / a.Hkv, c = bc - b * a.Hkv;
     // the last rows, which see most keys, first, with all their splits
-    const int r0 = static_cast<int>((gridDim.y - 1 - blockIdx.y) / a.splits) * kRows;
-    const int split = blockIdx.y % a.splits;
+    const int r0 = (job.slots - 1 - job.slot) / a.splits * kRows;
+    const int split = job.slot % a.splits;
     const int tid = threadIdx.x, lane = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane >> 5;
 
     // this lane's query row, and the last key that it sees (below 0: none)
     const int r = r0 + 32 * wave + (lane & 31);
-    const Query qr = query_of<PART>(a, b, r);
+    const Query qr = query_of(a, shared, b, r);
     const int i = qr.i, h = c * a.Gh + qr.g;
     const int nq = queries_of(a, qr.b);
     const bool there = r < a.rows && i < nq;
     int last, all_see, end, low = 0;
-    if constexpr (PART == kShared) {
+    __shared__ int most[PARTS ? 2 : 1][kWaves];
+    if (PARTS && shared) {
         // keys that all rows of the workgroup see, and that some row sees
-        __shared__ int most[2][kWaves];
-        const int shared = shared_rows(a, b, c);
-        last = there ? last_shared(a, qr, c, nq, shared) : -1;
-        int lo = there ? last + 1 : shared, hi = last + 1;
+        const int rows = shared_rows(a, b, c);
+        last = there ? last_shared(a, qr, c, nq, rows) : -1;
+        int lo = there ? last + 1 : rows, hi = last + 1;
 #pragma unroll
         for (int x = 1; x < 32; x *= 2) lo = min(lo, __shfl_xor(lo, x)), hi = max(hi, __shfl_xor(hi, x));
         if (lane == 0) most[0][wave] = lo, most[1][wave] = hi;
@@ -164,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         // keys that the workgroup's rows see together
         const int i_end = min((min(r0 + kRows, a.rows) - 1) / a.Gh, nq - 1);
         end = i_end < r0 / a.Gh ? 0 : max(a.causal ? len - nq + i_end + 1 : len, 0);
-        if constexpr (PART == kOwn) low = shared_rows(a, b / a.each, c);   // the first key
+        if (PARTS) low = shared_rows(a, b / a.each, c);        // the first key
     }
     // this split's tiles
     const int tiles0 = low / kKeys, tiles = max((end + kKeys - 1) / kKeys, tiles0);
@@ -258,11 +278,11 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
     // Rows of V behind the last key (and before the first) may hold anything: zeros, for p = 0 to meet
     // (their logits are masked).  By the wave that staged them.
     auto clear_tail = [&](int tile, int buf) {
-        if ((tile + 1) * kKeys <= end && (PART != kOwn || tile * kKeys >= low)) return;
+        if ((tile + 1) * kKeys <= end && (!PARTS || tile * kKeys >= low)) return;
         constexpr int kOut = 2 * D / 16;
         for (int x = lane; x < kWaveRows * kOut; x += kWave) {
             const int row = kWaveRows * wave + x / kOut;
-            if (tile * kKeys + row < end && (PART != kOwn || tile * kKeys + row >= low)) continue;
+            if (tile * kKeys + row < end && (!PARTS || tile * kKeys + row >= low)) continue;
             *reinterpret_cast<u32x4*>(vt[buf] + row * 2 * D + 16 * (x % kOut)) = u32x4{0u, 0u, 0u, 0u};
             if (kScaled) vsc[buf][row] = 0.f;
         }
@@ -302,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         va += 8 * (lane & 1);
         asm volatile("" : "+v"(ka), "+v"(va));
         const int rel = last - key0 - 4 * half;
-        // (kOwn: keys low .. last, by one comparison)
+        // (parts: keys low .. last, by one comparison)
         const uint32_t from = key0 + 4 * half - low, seen = max(last - low + 1, 0);
         floatx16 s[2];
         floatx4 kw[4], vw[4];              // scales of a half's keys
@@ -337,8 +357,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         // logit e of half u, scaled; a masked one is -inf whatever its row's scale
         auto logit = [&](int u, int e, float less) {
             float x = fmaf(s[u][e], kScaled ? kw[e >> 2][e & 3] : scale, -less);
-            if (MASKED && PART != kOwn) x = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? x : -INFINITY;
-            if (MASKED && PART == kOwn) x = from + (32 * u + 8 * (e >> 2) + (e & 3)) < seen ? x : -INFINITY;
+            if (MASKED && !PARTS) x = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? x : -INFINITY;
+            if (MASKED && PARTS) x = from + (32 * u + 8 * (e >> 2) + (e & 3)) < seen ? x : -INFINITY;
             return x;
         };
         // p of values 2 j, 2 j + 1 of half u relative to m, as bf16; their sum
@@ -443,11 +463,17 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         if (tile + 1 < tile1) load(tile + 1);
         // (behind the last tile the registers' old values, which nobody reads)
         bool other = false;
-        attend(tile * kKeys, buf, masked, [&](int j) {
+        const auto staging = [&](int j) {
             if (j == 0) other = other_scales();
 #pragma unroll
             for (int z = j * kPieces / KC; z < (j + 1) * kPieces / KC; ++z) store_piece(buf ^ 1, z);
-        });
+        };
+        if constexpr (decltype(masked)::value == 2) {
+#pragma unroll
+            for (int j = 0; j < KC; ++j) staging(j);
+        } else {
+            attend(tile * kKeys, buf, masked, staging);
+        }
         if (tile + 1 < tile1) {
             if (other) stage_again(buf ^ 1);
             clear_tail(tile + 1, buf ^ 1);
@@ -456,21 +482,23 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ChunkArgs a) {
         ++tile, buf ^= 1;
     };
     const int whole = min(max(all_see, 0) / kKeys, tile1);
-    if constexpr (PART == kOwn) {
-        while (tile < tile1) {
-            if (tile < whole && tile * kKeys >= low) step(Constant<0>{});
-            else step(Constant<1>{});
+    if constexpr (PARTS) {
+        if (!__any(there)) {               // a wave without rows stages its part of the tiles
+            while (tile < tile1) step(Constant<2>{});
+            if (half == 0 && r < a.rows)   // (rows that are not there: no weight, whatever their sums hold)
+                a.part_ml[(static_cast<int64_t>(split) * (a.B * a.Hkv) + bc) * a.rows + r] = make_float2(kNone, 0.f);
+            return;
         }
-    } else {
-        while (tile < whole) step(Constant<0>{});
-        while (tile < tile1) step(Constant<1>{});
+        if (tile < tile1 && tile * kKeys < low) step(Constant<1>{});
     }
+    while (tile < whole) step(Constant<0>{});
+    while (tile < tile1) step(Constant<1>{});
     l = half_sum(l);
     if (r >= a.rows) return;
     if (!there) l = 0.f;                   // (took part where nothing is masked)
     // value 4 w + j of o[t] is dim 32 t + 8 w + 4 half + j
-    if (PART != kWhole || a.splits > 1) {
-        const int64_t pr = (static_cast<int64_t>(split) * gridDim.x + bc) * a.rows + r;
+    if (PARTS || a.splits > 1) {
+        const int64_t pr = (static_cast<int64_t>(split) * (a.B * a.Hkv) + bc) * a.rows + r;
         float* po = a.part_o + pr * D + 4 * half;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -590,8 +618,11 @@ __device__ __forceinline__ void load_group(const char* src, char* dst, int row0,
 }
 
 // Workgroup: WAVES waves; (b, c) and a split of its keys.
-template <int D, int TYPE, int NR, int WAVES, int PART = kWhole>
-__global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
+template <int D, int TYPE, int NR, int WAVES, bool PARTS = false, class ARGS = ChunkArgs>
+__global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
+    const Work<PARTS> job = work_of<PARTS>(all);
+    const ChunkArgs& a = job.a;
+    const bool shared = PARTS && job.shared;
     using T = FewTile<D, TYPE, WAVES>;
     constexpr int kWaves = WAVES, kThreads = 64 * WAVES;
     constexpr int KC = D / 32;             // 32-dim steps of S
@@ -604,17 +635,17 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
     __shared__ __align__(16) char qs[NR * 16 * 2 * D];
     __shared__ float2 ml[kWaves][NR * 16];
 
-    const int bc = blockIdx.x, b = bc / a.Hkv, c = bc - b * a.Hkv, split = blockIdx.y;
+    const int bc = job.bc, b = bc / a.Hkv, c = bc - b * a.Hkv, split = job.slot;
     const int tid = threadIdx.x, lane = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int quarter = lane >> 4;
     char* const base = lds[wave];
 
-    // (kShared: queries of several sequences)
-    const int nq = PART == kShared ? 0 : queries_of(a, b);
-    const int len = PART == kShared ? shared_rows(a, b, c) : min(max(a.lens[bc], 0), a.max_len);
-    const int end = PART == kShared || nq > 0 ? len : 0;       // keys that the rows see together
-    const int low = PART == kOwn ? shared_rows(a, b / a.each, c) : 0;      // the first of them
+    // (shared: queries of several sequences)
+    const int nq = shared ? 0 : queries_of(a, b);
+    const int len = shared ? shared_rows(a, b, c) : min(max(a.lens[bc], 0), a.max_len);
+    const int end = shared || nq > 0 ? len : 0;        // keys that the rows see together
+    const int low = PARTS && !shared ? shared_rows(a, b / a.each, c) : 0;  // the first of them
     const int tiles0 = low / T::kKeys, tiles = max((end + T::kKeys - 1) / T::kKeys, tiles0);
     const int per = (tiles - tiles0 + a.splits - 1) / a.splits;
     const int first0 = tiles0 + split * per, tile0 = first0 + wave, tile1 = min(first0 + per, tiles);
@@ -668,10 +699,10 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
     for (int j = 0; j < NR * 16 * QC / kWave; j += kWaves) {
         if (j + wave >= NR * 16 * QC / kWave) break;
         const int r = (j + wave) * (kWave / QC) + lane / QC;
-        const Query qr = query_of<PART>(a, b, r);
+        const Query qr = query_of(a, shared, b, r);
         const int i = qr.i, h = c * a.Gh + qr.g;
         const int ch = (lane % QC) ^ ((QC == 16 ? r : r >> 1) & (QC - 1));
-        const bool there = r < a.rows && i < (PART == kShared ? queries_of(a, qr.b) : nq);
+        const bool there = r < a.rows && i < (shared ? queries_of(a, qr.b) : nq);
         const char* src = there ? reinterpret_cast<const char*>(a.q + qr.b * a.qsb + h * a.qsh + i * a.qst + 8 * ch)
                                 : reinterpret_cast<const char*>(kNoRows);
         load16_to_lds(src, qs + (j + wave) * 1024);
@@ -688,12 +719,12 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
     // the last key that each of this lane's rows sees (below 0: none)
     int last[NR];
     // keys that every row sees
-    int all_see = PART == kShared ? len : a.causal ? max(len - nq + 1, 0) : len;
+    int all_see = shared ? len : a.causal ? max(len - nq + 1, 0) : len;
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
         const int r = 16 * x + (lane & 15);
-        if constexpr (PART == kShared) {
-            const Query qr = query_of<PART>(a, b, r);
+        if (shared) {
+            const Query qr = query_of(a, shared, b, r);
             const int n = queries_of(a, qr.b);
             const bool there = r < a.rows && qr.i < n;
             last[x] = there ? last_shared(a, qr, c, n, len) : -1;
@@ -756,13 +787,13 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
         __builtin_amdgcn_sched_barrier(0);
         ids = pages_of(tile + 2 * kWaves);
         const int key0 = tile * T::kKeys;
-        if (key0 + T::kKeys > end || (PART == kOwn && key0 < low)) {
+        if (key0 + T::kKeys > end || (PARTS && key0 < low)) {
             // rows behind the last key (and before the first) may hold anything: zeros, with zero scales
             char* const vt = base + STAGE * T::kStage + T::kTile;
             float* const sc = reinterpret_cast<float*>(vt + T::kTile);
             for (int i = lane; i < T::kKeys * T::kCh; i += kWave)
-                if (key0 + i / T::kCh >= end || (PART == kOwn && key0 + i / T::kCh < low)) *reinterpret_cast<u32x4*>(vt + i * 16) = u32x4{0u, 0u, 0u, 0u};
-            if (T::kScaled && lane < T::kKeys && (key0 + lane >= end || (PART == kOwn && key0 + lane < low))) sc[lane] = 0.f, sc[T::kKeys + lane] = 0.f;
+                if (key0 + i / T::kCh >= end || (PARTS && key0 + i / T::kCh < low)) *reinterpret_cast<u32x4*>(vt + i * 16) = u32x4{0u, 0u, 0u, 0u};
+            if (T::kScaled && lane < T::kKeys && (key0 + lane >= end || (PARTS && key0 + lane < low))) sc[lane] = 0.f, sc[T::kKeys + lane] = 0.f;
         }
         // value e of s[x][u] is key key0 + 32 (u / 2) + 8 quarter + 4 (u % 2) + e
         floatx4 s[NR][NS];
@@ -821,7 +852,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
                 for (int x = 0; x < NR; ++x) s[x][u] *= __builtin_bit_cast(floatx4, w[u]);
             }
         }
-        if (key0 + T::kKeys > all_see || (PART == kOwn && key0 < low)) {
+        if (key0 + T::kKeys > all_see || (PARTS && key0 < low)) {
             asm volatile("");              // (a branch: few tiles come here)
 #pragma unroll
             for (int x = 0; x < NR; ++x) {
@@ -831,7 +862,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int at = 32 * (u >> 1) + 4 * (u & 1) + e;
-                        s[x][u][e] = at <= rel && (PART != kOwn || at >= before) ? s[x][u][e] : -INFINITY;
+                        s[x][u][e] = at <= rel && (!PARTS || at >= before) ? s[x][u][e] : -INFINITY;
                     }
             }
         }
@@ -947,7 +978,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
     constexpr int G = D / 8;               // lanes of a row, 8 dims each
     for (int it = tid; it < a.rows * G; it += kThreads) {
         const int r = it / G, d0 = 8 * (it - r * G);
-        const Query qr = query_of<PART>(a, b, r);
+        const Query qr = query_of(a, shared, b, r);
         const int i = qr.i;
         float M = kNone, L = 0.f, x[8] = {};
 #pragma unroll
@@ -962,9 +993,9 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ChunkArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = fmaf(y0[e], f, x[e]), x[4 + e] = fmaf(y1[e], f, x[4 + e]);
         }
-        if (i >= (PART == kShared ? queries_of(a, qr.b) : nq)) L = 0.f;    // (a row that is not there took part where nothing is masked)
-        if (PART != kWhole || a.splits > 1) {
-            const int64_t pr = (static_cast<int64_t>(split) * gridDim.x + bc) * a.rows + r;
+        if (i >= (shared ? queries_of(a, qr.b) : nq)) L = 0.f;    // (a row that is not there took part where nothing is masked)
+        if (PARTS || a.splits > 1) {
+            const int64_t pr = (static_cast<int64_t>(split) * (a.B * a.Hkv) + bc) * a.rows + r;
             float* po = a.part_o + pr * D + d0;
             *reinterpret_cast<float4*>(po) = make_float4(x[0], x[1], x[2], x[3]);
             *reinterpret_cast<float4*>(po + 4) = make_float4(x[4], x[5], x[6], x[7]);
@@ -1075,27 +1106,45 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
 constexpr int kMaxSplits = 64;             // splits of a head's rows
 constexpr int64_t kTileBlocks = 4 * kPlanCus;   // workgroups of many rows, where there are splits
 
-template <int D, int TYPE, int PART = kWhole>
+template <int D, int TYPE>
 void attend(const ChunkArgs& a, hipStream_t s) {
     const unsigned heads = static_cast<unsigned>(static_cast<int64_t>(a.B) * a.Hkv);
     if (a.rows > kFewRows) {
         const int tiles = (a.rows + kRows - 1) / kRows;
-        hipLaunchKernelGGL((chunk_kernel<D, TYPE, PART>), dim3(heads, tiles * a.splits), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((chunk_kernel<D, TYPE>), dim3(heads, tiles * a.splits), dim3(kThreads), 0, s, a);
         return;
     }
     const dim3 grid(heads, a.splits);
     constexpr int W = few_waves(D, TYPE, 1);
-    if (a.rows <= 16) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 1, W, PART>), grid, dim3(64 * W), 0, s, a);
-    else if (a.rows <= 32) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 2, W, PART>), grid, dim3(64 * W), 0, s, a);
-    else hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 4, 4, PART>), grid, dim3(kThreads), 0, s, a);
+    if (a.rows <= 16) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 1, W>), grid, dim3(64 * W), 0, s, a);
+    else if (a.rows <= 32) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 2, W>), grid, dim3(64 * W), 0, s, a);
+    else hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 4, 4>), grid, dim3(kThreads), 0, s, a);
 }
 
-template <int D, int PART = kWhole>
-hipError_t attend_type(const ChunkArgs& a, hipStream_t s) {
-    if (a.pages.dtype == kCacheBf16) attend<D, kCacheBf16, PART>(a, s);
-    else if (a.pages.dtype == kCacheE4m3) attend<D, kCacheE4m3, PART>(a, s);
-    else attend<D, kCacheI8, PART>(a, s);
-    return hipGetLastError();
+// Both parts of an attention over a shared prefix, or one of them (the other's
+// workgroups are none), on the kernel for `few` rows or the one for more.
+struct PartsArgs {
+    ChunkArgs shared, own;
+    int first_own;                         // workgroups of the shared rows, which come first
+};
+
+template <int D, int TYPE>
+void attend_parts(const ChunkArgs& shared, const ChunkArgs& own, bool do_shared, bool do_own, bool few, hipStream_t s) {
+    const auto blocks = [&](const ChunkArgs& a) {
+        return static_cast<int64_t>(a.B) * a.Hkv * a.splits * (few ? 1 : (a.rows + kRows - 1) / kRows);
+    };
+    const int64_t first = do_shared ? blocks(shared) : 0;
+    const dim3 grid(static_cast<unsigned>(first + (do_own ? blocks(own) : 0)));
+    const PartsArgs p{shared, own, static_cast<int>(first)};
+    if (!few) {
+        hipLaunchKernelGGL((chunk_kernel<D, TYPE, true, PartsArgs>), grid, dim3(kThreads), 0, s, p);
+        return;
+    }
+    const int rows = do_shared ? shared.rows : own.rows;   // (those of a group are at least a sequence's)
+    constexpr int W = few_waves(D, TYPE, 1);
+    if (rows <= 16) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 1, W, true, PartsArgs>), grid, dim3(64 * W), 0, s, p);
+    else if (rows <= 32) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 2, W, true, PartsArgs>), grid, dim3(64 * W), 0, s, p);
+    else hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 4, 4, true, PartsArgs>), grid, dim3(kThreads), 0, s, p);
 }
 
 template <int D, bool PARTS = false>
@@ -1116,15 +1165,35 @@ hipError_t join(const ChunkArgs& a, hipStream_t s) {
 
 template <int D>
 hipError_t launch(const ChunkArgs& a, hipStream_t s) {
-    const hipError_t e = attend_type<D>(a, s);
+    if (a.pages.dtype == kCacheBf16) attend<D, kCacheBf16>(a, s);
+    else if (a.pages.dtype == kCacheE4m3) attend<D, kCacheE4m3>(a, s);
+    else attend<D, kCacheI8>(a, s);
+    const hipError_t e = hipGetLastError();
     return e != hipSuccess || a.splits == 1 ? e : join<D>(a, s);
+}
+
+// Whether both parts run in one launch: the kernel for many rows also takes few rows of
+// up to kOwnKeys keys (a tile of them takes it as long as many rows do).
+constexpr int kOwnKeys = 1024;
+bool one_launch(const ChunkArgs& shared, const ChunkArgs& own) {
+    return shared.rows <= kFewRows || own.rows > kFewRows || own.max_len - own.shared_max <= kOwnKeys;
 }
 
 template <int D>
 hipError_t launch_parts(const ChunkArgs& shared, const ChunkArgs& own, hipStream_t s) {
-    hipError_t e = attend_type<D, kShared>(shared, s);
-    if (e != hipSuccess) return e;
-    e = attend_type<D, kOwn>(own, s);
+    const auto attend_type = [&](bool do_shared, bool do_own, bool few) {
+        if (own.pages.dtype == kCacheBf16) attend_parts<D, kCacheBf16>(shared, own, do_shared, do_own, few, s);
+        else if (own.pages.dtype == kCacheE4m3) attend_parts<D, kCacheE4m3>(shared, own, do_shared, do_own, few, s);
+        else attend_parts<D, kCacheI8>(shared, own, do_shared, do_own, few, s);
+        return hipGetLastError();
+    };
+    hipError_t e;
+    if (one_launch(shared, own)) {
+        e = attend_type(true, true, shared.rows <= kFewRows);
+    } else {
+        e = attend_type(true, false, false);
+        if (e == hipSuccess) e = attend_type(false, true, true);
+    }
     if (e != hipSuccess) return e;
     ChunkArgs a = own;
     a.part_o = shared.part_o;
@@ -1151,7 +1220,8 @@ constexpr int kFewBlocks = 4 * kPlanCus;   // workgroups of few rows, where ther
 // is best at 321 rows, 6.6 us, twelve at 1100, 8.2 against 11.3, 48 or more at
 // 16384, 13.8 against 101; for 16 sequences of 16384 rows four, 97 against 105 with
 // 2 and 166 with 1; for 32 of 1100 e4m3 rows one, 11.9 against 13.8 with 2.)
-int few_splits(int64_t heads, int rows, int T, int d, int dtype) {
+// A part of an attention over a shared prefix is joined anyway: without the launch.
+int few_splits(int64_t heads, int rows, int T, int d, int dtype, bool part = false) {
     const int keys = d == 128 && dtype == kCacheBf16 ? 32 : 64;
     const int nr = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     int64_t round;
@@ -1165,7 +1235,7 @@ int few_splits(int64_t heads, int rows, int T, int d, int dtype) {
     for (int s = 1; s <= kMaxSplits && s <= rounds && (s == 1 || s * heads <= kFewBlocks); ++s) {
         const int64_t turns = (heads * s + kPlanCus - 1) / kPlanCus;
         const int64_t work = turns * ((rounds + s - 1) / s * round + 2000);
-        const int64_t cost = work + (s > 1 ? 3000 + heads * rows * s * d * 2 / 1000 : 0);
+        const int64_t cost = work + (s > 1 || part ? (part ? 0 : 3000) + heads * rows * s * d * 2 / 1000 : 0);
         if (s == 1 || cost < best) best = cost, best_s = s;
     }
     return best_s;
@@ -1179,15 +1249,17 @@ int few_splits(int64_t heads, int rows, int T, int d, int dtype) {
 // (1024 queries of 28 heads on 4 over 8191 rows, 224 row tiles: 197 us with 1 split,
 // 142 with 2, 154 with 3; 512 of 32 on 8 over 4096, 128: 98 / 67 / 60 / 56 / 60 us
 // with 1 / 2 / 3 / 4 / 6; 1024 of 32 on 8 over 1024, 256: 31 with 1, 40 with 2.)
-int tile_splits(int64_t heads, int rows, int T, int d) {
+int tile_splits(int64_t heads, int rows, int T, int d, bool part = false) {
     const int64_t alone = d == 64 ? 950 : 1500, paired = d == 64 ? 1250 : 2000;
     const int64_t base = heads * ((rows + kRows - 1) / kRows), tiles = (T + kKeys - 1) / kKeys;
     int64_t best = 0;
     int best_s = 1;
-    for (int s = 1; s <= kMaxSplits && s <= tiles && (s == 1 || base * s <= kTileBlocks); ++s) {
+    // (a part's few rows: the workspace has a place for 128 keys or more of a split)
+    const int64_t most = rows <= kFewRows ? T / 128 + 1 : tiles;
+    for (int s = 1; s <= kMaxSplits && s <= most && (s == 1 || base * s <= kTileBlocks); ++s) {
         const int64_t n = base * s, rest = n % (2 * kPlanCus);
         const int64_t turns = n / (2 * kPlanCus) * paired + (rest == 0 ? 0 : rest <= kPlanCus ? alone : paired);
-        const int64_t join = s > 1 ? 3000 + heads * rows * s * d * 3 / 1000 : 0;
+        const int64_t join = s > 1 || part ? (part ? 0 : 3000) + heads * rows * s * d * 3 / 1000 : 0;
         const int64_t cost = turns * ((tiles + s - 1) / s + 2) + join;
         if (s == 1 || cost < best) best = cost, best_s = s;
     }
@@ -1199,6 +1271,17 @@ int tile_splits(int64_t heads, int rows, int T, int d) {
 int chunk_splits(int64_t heads, int rows, int T, int d, int dtype) {
     if (rows <= kFewRows) return few_splits(heads, rows, T, d, dtype);
     return tile_splits(heads, rows, T, d);
+}
+
+void plan_parts(ChunkArgs* shared, ChunkArgs* own) {
+    const auto splits = [](const ChunkArgs& a, int T, bool few) {
+        const int64_t heads = static_cast<int64_t>(a.B) * a.Hkv;
+        return few ? few_splits(heads, a.rows, T, a.d, a.pages.dtype, true) : tile_splits(heads, a.rows, T, a.d, true);
+    };
+    const int mine = own->max_len - own->shared_max;
+    const bool few = shared->rows <= kFewRows;
+    shared->splits = splits(*shared, own->shared_max, few);
+    own->splits = splits(*own, mine > kKeys ? mine : kKeys, one_launch(*shared, *own) ? few : true);
 }
 
 size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d) {

@@ -290,7 +290,9 @@ hipError_t launch_shape_scores(const ShapeArgs& a, hipStream_t s);
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t s);
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t s);
 hipError_t launch_chunk_attention(const ChunkArgs& a, hipStream_t s);
-// Both parts' sums in one array: shared.splits, then own.splits.
+// The splits of the two parts of an attention over a shared prefix, and their launch:
+// both parts' sums in one array, shared.splits and then own.splits.
+void plan_parts(ChunkArgs* shared, ChunkArgs* own);
 hipError_t launch_shared_attention(const ChunkArgs& shared, const ChunkArgs& own, hipStream_t s);
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s);
 hipError_t launch_book(const BookArgs& a, int op, hipStream_t s);

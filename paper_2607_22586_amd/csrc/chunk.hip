@@ -1128,13 +1128,24 @@ struct PartsArgs {
     int first_own;                         // workgroups of the shared rows, which come first
 };
 
+// Workgroups of a part on either kernel, and whether both parts run in one launch: where
+// all of theirs have a place at once, on the kernel for the shared rows (a CU has places
+// for one workgroup of few rows, two of more).  Else the own rows' would only begin when
+// shared ones end, on a kernel that may take longer for them.  (15 sequences' 4 tokens
+// over 5003 int8 rows and up to 333 own ones: 18 us in one launch, 26 in two; 64 tokens
+// over 32768 and up to 600: 126 in one, 123 in two, 171 with the parts' workgroups mixed.)
+int64_t part_blocks(const ChunkArgs& a, bool few) {
+    return static_cast<int64_t>(a.B) * a.Hkv * a.splits * (few ? 1 : (a.rows + kRows - 1) / kRows);
+}
+bool one_launch(const ChunkArgs& shared, const ChunkArgs& own) {
+    const bool few = shared.rows <= kFewRows;
+    return part_blocks(shared, few) + part_blocks(own, few) <= (few ? 1 : 2) * kPlanCus;
+}
+
 template <int D, int TYPE>
 void attend_parts(const ChunkArgs& shared, const ChunkArgs& own, bool do_shared, bool do_own, bool few, hipStream_t s) {
-    const auto blocks = [&](const ChunkArgs& a) {
-        return static_cast<int64_t>(a.B) * a.Hkv * a.splits * (few ? 1 : (a.rows + kRows - 1) / kRows);
-    };
-    const int64_t first = do_shared ? blocks(shared) : 0;
-    const dim3 grid(static_cast<unsigned>(first + (do_own ? blocks(own) : 0)));
+    const int64_t first = do_shared ? part_blocks(shared, few) : 0;
+    const dim3 grid(static_cast<unsigned>(first + (do_own ? part_blocks(own, few) : 0)));
     const PartsArgs p{shared, own, static_cast<int>(first)};
     if (!few) {
         hipLaunchKernelGGL((chunk_kernel<D, TYPE, true, PartsArgs>), grid, dim3(kThreads), 0, s, p);
@@ -1172,13 +1183,6 @@ hipError_t launch(const ChunkArgs& a, hipStream_t s) {
     return e != hipSuccess || a.splits == 1 ? e : join<D>(a, s);
 }
 
-// Whether both parts run in one launch: the kernel for many rows also takes few rows of
-// up to kOwnKeys keys (a tile of them takes it as long as many rows do).
-constexpr int kOwnKeys = 1024;
-bool one_launch(const ChunkArgs& shared, const ChunkArgs& own) {
-    return shared.rows <= kFewRows || own.rows > kFewRows || own.max_len - own.shared_max <= kOwnKeys;
-}
-
 template <int D>
 hipError_t launch_parts(const ChunkArgs& shared, const ChunkArgs& own, hipStream_t s) {
     const auto attend_type = [&](bool do_shared, bool do_own, bool few) {
@@ -1188,11 +1192,11 @@ hipError_t launch_parts(const ChunkArgs& shared, const ChunkArgs& own, hipStream
         return hipGetLastError();
     };
     hipError_t e;
-    if (one_launch(shared, own)) {
+    if (own.one_launch) {
         e = attend_type(true, true, shared.rows <= kFewRows);
     } else {
-        e = attend_type(true, false, false);
-        if (e == hipSuccess) e = attend_type(false, true, true);
+        e = attend_type(true, false, shared.rows <= kFewRows);
+        if (e == hipSuccess) e = attend_type(false, true, own.rows <= kFewRows);
     }
     if (e != hipSuccess) return e;
     ChunkArgs a = own;
@@ -1278,10 +1282,12 @@ void plan_parts(ChunkArgs* shared, ChunkArgs* own) {
         const int64_t heads = static_cast<int64_t>(a.B) * a.Hkv;
         return few ? few_splits(heads, a.rows, T, a.d, a.pages.dtype, true) : tile_splits(heads, a.rows, T, a.d, true);
     };
-    const int mine = own->max_len - own->shared_max;
+    const int mine = own->max_len - own->shared_max > kKeys ? own->max_len - own->shared_max : kKeys;
     const bool few = shared->rows <= kFewRows;
     shared->splits = splits(*shared, own->shared_max, few);
-    own->splits = splits(*own, mine > kKeys ? mine : kKeys, one_launch(*shared, *own) ? few : true);
+    own->splits = splits(*own, mine, few);
+    own->one_launch = one_launch(*shared, *own);
+    if (!own->one_launch) own->splits = splits(*own, mine, own->rows <= kFewRows);
 }
 
 size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d) {

@@ -43,24 +43,30 @@ struct Extent {
     int most, least;
 };
 
-// Largest and smallest of a sequence's numbers of rows (every thread gets them).
-__device__ __forceinline__ Extent extent(const int32_t* rows, int Hkv, int* lds) {
+// Largest and smallest of a sequence's numbers of rows, over a wave.
+__device__ __forceinline__ Extent wave_extent(const int32_t* rows, int Hkv, int first, int step) {
     int most = INT32_MIN, least = INT32_MAX;
-    for (int c = threadIdx.x; c < Hkv; c += kBookThreads) {
-        most = max(most, rows[c]);
-        least = min(least, rows[c]);
+    for (int c = first; c < Hkv; c += step) {
+        const int n = rows[c];
+        most = max(most, n);
+        least = min(least, n);
     }
 #pragma unroll
     for (int s = kWave / 2; s > 0; s /= 2) {
         most = max(most, __shfl_xor(most, s));
         least = min(least, __shfl_xor(least, s));
     }
+    return {most, least};
+}
+// The same over a workgroup (every thread gets them).
+__device__ __forceinline__ Extent extent(const int32_t* rows, int Hkv, int* lds) {
+    Extent e = wave_extent(rows, Hkv, threadIdx.x, kBookThreads);
     __syncthreads();
-    if (lane_id() == 0) lds[2 * (threadIdx.x / kWave)] = most, lds[2 * (threadIdx.x / kWave) + 1] = least;
+    if (lane_id() == 0) lds[2 * (threadIdx.x / kWave)] = e.most, lds[2 * (threadIdx.x / kWave) + 1] = e.least;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kBookThreads / kWave; ++w) most = max(most, lds[2 * w]), least = min(least, lds[2 * w + 1]);
-    return {most, least};
+    for (int w = 0; w < kBookThreads / kWave; ++w) e = {max(e.most, lds[2 * w]), min(e.least, lds[2 * w + 1])};
+    return e;
 }
 
 // What a call makes of a sequence's row of the table: entries j < keep as those of
@@ -71,18 +77,19 @@ struct Change {
     bool moves;
 };
 
-template <int OP>
-__device__ __forceinline__ Change change_of(const BookArgs& a, int b, const int32_t* lens, int* lds) {
+// (extent_of: the extent of a sequence's numbers of rows)
+template <int OP, class EXTENT>
+__device__ __forceinline__ Change change_of(const BookArgs& a, int b, const int32_t* lens, EXTENT&& extent_of) {
     const auto pages_of = [&](int rows) { return (min(max(rows, 0), a.pages.cap) + (1 << a.pages.shift) - 1) >> a.pages.shift; };
     if constexpr (OP == kBookHold) {
-        return {b, 0, pages_of(extent(a.rows + static_cast<int64_t>(b) * a.Hkv, a.Hkv, lds).most), true};
+        return {b, 0, pages_of(extent_of(a.rows + static_cast<int64_t>(b) * a.Hkv).most), true};
     } else if constexpr (OP == kBookFork) {
         const int from = a.src[b];
         const bool moves = static_cast<uint32_t>(from) < static_cast<uint32_t>(a.B) && from != b;
-        const Extent e = extent(lens + static_cast<int64_t>(moves ? from : b) * a.Hkv, a.Hkv, lds);
+        const Extent e = extent_of(lens + static_cast<int64_t>(moves ? from : b) * a.Hkv);
         return {from, min(max(e.least, 0), a.pages.cap) >> a.pages.shift, pages_of(e.most), moves};
     } else {
-        const Extent e = extent(a.rows + static_cast<int64_t>(b) * a.Hkv, a.Hkv, lds);
+        const Extent e = extent_of(a.rows + static_cast<int64_t>(b) * a.Hkv);
         return {b, 0, pages_of(min(e.most, a.n)), e.most >= 0};
     }
 }
@@ -92,6 +99,19 @@ template <int OP>
 __device__ __forceinline__ bool wants(const BookArgs& a, const Change& c, int j, int id) {
     if (!c.moves || j >= c.end) return false;
     return OP == kBookHold ? !named(a.pages, id) : OP == kBookFork ? j >= c.keep && named(a.pages, id) : true;
+}
+
+// What entry j, which named `id` before, names after the call if it gets no new page.
+template <int OP>
+__device__ __forceinline__ int stays(const BookArgs& a, const Change& c, int j, int id) {
+    return j < c.end && (OP == kBookHold || (OP == kBookFork && j < c.keep)) && named(a.pages, id) ? id : -1;
+}
+
+// The rows of head h of sequence b after a fork or a compaction.
+template <int OP>
+__device__ __forceinline__ int new_len(const BookArgs& a, const Change& c, int b, int h) {
+    return OP == kBookFork ? a.old_lens[static_cast<int64_t>(c.from) * a.Hkv + h]
+                           : min(max(a.rows[static_cast<int64_t>(b) * a.Hkv + h], 0), a.n);
 }
 
 template <int OP>
@@ -112,7 +132,7 @@ __global__ void __launch_bounds__(kBookThreads) book_count_kernel(BookArgs a) {
         return;
     }
     if (b == 0 && tid == 0) *a.taken = 0;
-    const Change c = change_of<OP>(a, b, a.lens, lds);
+    const Change c = change_of<OP>(a, b, a.lens, [&](const int32_t* rows) { return extent(rows, a.Hkv, lds); });
     const int64_t row = static_cast<int64_t>(b) * a.pages.max_pages;
     const int64_t theirs = static_cast<int64_t>(c.moves ? c.from : b) * a.pages.max_pages;
     int x = 0;
@@ -133,7 +153,7 @@ template <int OP>
 __global__ void __launch_bounds__(kBookThreads) book_plan_kernel(BookArgs a) {
     __shared__ int lds[2 * kBookThreads / kWave], upto[kBookThreads];
     const int b = blockIdx.x, tid = threadIdx.x;
-    const Change c = change_of<OP>(a, b, a.old_lens, lds);
+    const Change c = change_of<OP>(a, b, a.old_lens, [&](const int32_t* rows) { return extent(rows, a.Hkv, lds); });
     // this sequence's ranks [lo, hi) (sums of at most B * max_pages entries)
     int x = 0, lo, total;
     for (int i = tid; i < b; i += kBookThreads) x += a.want[i];
@@ -182,21 +202,131 @@ __global__ void __launch_bounds__(kBookThreads) book_plan_kernel(BookArgs a) {
         const int at = rank + block_scan(take, lds, &total) - 1;
         rank += total;
         if (j >= a.pages.max_pages) continue;
-        int now = -1;
-        if (take) {
-            if (ok) {
-                now = a.ids[at];
-                if (OP != kBookHold) a.items[at] = make_int2(b, j);
-            }
-        } else if (j < c.end && (OP == kBookHold || (OP == kBookFork && j < c.keep)) && named(a.pages, id)) {
-            now = id;
-        }
-        a.table[row + j] = now;
+        a.table[row + j] = take ? (ok ? a.ids[at] : -1) : stays<OP>(a, c, j, id);
+        if (OP != kBookHold && take) a.items[at] = make_int2(b, j);
     }
     if (OP == kBookHold) return;
-    for (int h = tid; h < a.Hkv; h += kBookThreads) {
-        const int64_t at = static_cast<int64_t>(b) * a.Hkv + h;
-        a.lens[at] = OP == kBookFork ? a.old_lens[static_cast<int64_t>(c.from) * a.Hkv + h] : min(max(a.rows[at], 0), a.n);
+    for (int h = tid; h < a.Hkv; h += kBookThreads) a.lens[static_cast<int64_t>(b) * a.Hkv + h] = new_len<OP>(a, c, b, h);
+}
+
+// All of it but the copies for small pools and tables, in one workgroup: the free pages
+// as a list in LDS, a thread for what each sequence asks for, and then for a few
+// consecutive entries of the table, all of whose loads are on their way at once: the rank
+// of a wanted page is the number of those before it, whatever the sequence.
+constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / kWave;
+constexpr int kSmallSeqs = 1024, kSmallHeads = 64;
+constexpr int kSmallEach = 8;              // pages, and entries, of a thread
+constexpr int kSmallPages = kSmallEach * kSmallThreads, kSmallEntries = kSmallEach * kSmallThreads;
+
+template <int OP>
+__global__ void __launch_bounds__(kSmallThreads) book_small_kernel(BookArgs a) {
+    __shared__ int free_ids[kSmallPages], part[2][kSmallWaves];
+    __shared__ int from[kSmallSeqs], keep[kSmallSeqs], end[kSmallSeqs], upto[kSmallSeqs + 1];
+    const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave, most = a.pages.max_pages;
+    // Inclusive prefix sum over the workgroup, and its total.
+    const auto scan = [&](int x, int which, int* total) {
+        x = wave_incl_scan(x);
+        if (lane == kWave - 1) part[which][wave] = x;
+        __syncthreads();
+        int before = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < kSmallWaves; ++w) {
+            const int n = part[which][w];
+            before += w < wave ? n : 0;
+            all += n;
+        }
+        *total = all;
+        return x + before;
+    };
+    // the free pages, a thread's consecutive ones
+    const int per = (a.pages.n_pages + kSmallThreads - 1) / kSmallThreads, p0 = tid * per;
+    uint32_t is_free = 0;
+    int count[kSmallEach];
+#pragma unroll
+    for (int j = 0; j < kSmallEach; ++j) count[j] = a.refs[min(p0 + j, a.pages.n_pages - 1)];
+#pragma unroll
+    for (int j = 0; j < kSmallEach; ++j)
+        is_free |= static_cast<uint32_t>(j < per && p0 + j < a.pages.n_pages && count[j] == 0) << j;
+    if (tid < a.B) {
+        const Change c = change_of<OP>(a, tid, a.lens, [&](const int32_t* rows) {
+            Extent e{INT32_MIN, INT32_MAX};
+            for (int h0 = 0; h0 < a.Hkv; h0 += 8) {
+                int n[8];
+#pragma unroll
+                for (int h = 0; h < 8; ++h) n[h] = rows[min(h0 + h, a.Hkv - 1)];
+#pragma unroll
+                for (int h = 0; h < 8; ++h) e = {max(e.most, n[h]), min(e.least, n[h])};
+            }
+            return e;
+        });
+        from[tid] = c.moves ? c.from : -1;
+        keep[tid] = c.keep;
+        end[tid] = c.end;
+    }
+    if (OP != kBookHold)
+        for (int x = tid; x < a.B * a.Hkv; x += kSmallThreads) a.old_lens[x] = a.lens[x];
+    if (tid == 0) upto[0] = 0, *a.taken = 0;
+    int n_free, wanted;
+    int rank = scan(__popc(is_free), 0, &n_free) - __popc(is_free);
+    for (uint32_t x = is_free; x != 0; x &= x - 1) free_ids[rank++] = p0 + __ffs(x) - 1;
+    // a thread's consecutive entries: their sequence (-1: none), place in its row, what they
+    // and the entries that they become copies of name
+    const int entries = a.B * most, each = (entries + kSmallThreads - 1) / kSmallThreads;
+    int seq[kSmallEach], own[kSmallEach], theirs[kSmallEach];
+    const auto change = [&](int b) {
+        const int x = from[b];
+        return Change{x < 0 ? b : x, keep[b], end[b], x >= 0};
+    };
+#pragma unroll
+    for (int x = 0; x < kSmallEach; ++x) {
+        const int e = tid * each + x;
+        seq[x] = x < each && e < entries ? e / most : -1;
+        own[x] = theirs[x] = -1;
+        if (seq[x] >= 0) {
+            own[x] = a.table[e];
+            theirs[x] = a.table[change(seq[x]).from * most + e - seq[x] * most];
+        }
+    }
+    uint32_t take = 0;
+#pragma unroll
+    for (int x = 0; x < kSmallEach; ++x) {
+        if (seq[x] < 0) continue;
+        const int e = tid * each + x;
+        a.old_table[e] = own[x];
+        take |= static_cast<uint32_t>(wants<OP>(a, change(seq[x]), e - seq[x] * most, theirs[x])) << x;
+    }
+    const int first = scan(__popc(take), 1, &wanted) - __popc(take);
+#pragma unroll
+    for (int x = 0; x < kSmallEach; ++x) {
+        const int e = tid * each + x;
+        if (seq[x] >= 0 && e + 1 == (seq[x] + 1) * most) upto[seq[x] + 1] = first + __popc(take & ((2u << x) - 1));
+    }
+    __syncthreads();                       // (and the table has been read)
+    if (tid < a.B) {
+        const int want = upto[tid + 1] - upto[tid];
+        const bool fits = want == 0 || upto[tid + 1] <= n_free;
+        a.missing[tid] = fits ? 0 : want;
+        if (want > 0 && fits) atomicMax(a.taken, upto[tid + 1]);
+    }
+    if (OP != kBookHold)
+        for (int x = tid; x < a.B * a.Hkv; x += kSmallThreads) {
+            const int b = x / a.Hkv;
+            if (from[b] >= 0 && (upto[b + 1] == upto[b] || upto[b + 1] <= n_free))
+                a.lens[x] = new_len<OP>(a, Change{from[b], 0, 0, true}, b, x - b * a.Hkv);
+        }
+#pragma unroll
+    for (int x = 0; x < kSmallEach; ++x) {
+        if (seq[x] < 0) continue;
+        const int b = seq[x], e = tid * each + x, j = e - b * most, at = first + __popc(take & ((1u << x) - 1));
+        const Change c = change(b);
+        const bool new_page = take >> x & 1, fits = upto[b + 1] == upto[b] || upto[b + 1] <= n_free;
+        if (!c.moves || (OP != kBookHold && !fits)) continue;
+        const int now = new_page ? (fits ? free_ids[at] : -1) : stays<OP>(a, c, j, theirs[x]);
+        if (OP != kBookHold && new_page) a.items[at] = make_int2(b, j), a.ids[at] = now;
+        if (now == own[x]) continue;
+        a.table[e] = now;
+        if (named(a.pages, own[x])) atomicSub(a.refs + own[x], 1);
+        if (named(a.pages, now)) atomicAdd(a.refs + now, 1);
     }
 }
 
@@ -217,7 +347,7 @@ __global__ void __launch_bounds__(kBookThreads) book_hold_kernel(BookArgs a) { c
 // Rows of one head of one new page, 16 bytes a lane: a group of lanes has a row of K
 // and of V.  Fork: the rows of the page that the source has there; compact: the rows
 // that idx names, zeros (scale 1) where it names none.
-template <int OP, int ROW>                 // bytes of a row
+template <int OP, int ROW, bool COUNT>     // bytes of a row; whether the counters are left to it
 __global__ void __launch_bounds__(kBookThreads) book_copy_kernel(BookArgs a) {
     constexpr int kCh = ROW / 16, kPer = kBookThreads / kCh;
     const int page = 1 << a.pages.shift, ch = threadIdx.x % kCh;
@@ -255,24 +385,34 @@ __global__ void __launch_bounds__(kBookThreads) book_copy_kernel(BookArgs a) {
             if (a.pages.dtype != kCacheBf16 && ch == 0) a.pages.k_scale[to + r] = ks, a.pages.v_scale[to + r] = vs;
         }
     }
-    count_changes(a);
+    if (COUNT) count_changes(a);
 }
 
 template <int OP>
 hipError_t launch(const BookArgs& a, hipStream_t s) {
     const int64_t entries = static_cast<int64_t>(a.B) * a.pages.max_pages;
-    hipLaunchKernelGGL((book_count_kernel<OP>), dim3(static_cast<unsigned>(a.B + a.chunks)), dim3(kBookThreads), 0, s, a);
-    hipLaunchKernelGGL((book_plan_kernel<OP>), dim3(a.B), dim3(kBookThreads), 0, s, a);
-    const int64_t blocks = (entries + kBookThreads - 1) / kBookThreads;
+    const bool small = a.pages.n_pages <= kSmallPages && a.B <= kSmallSeqs && a.Hkv <= kSmallHeads && entries <= kSmallEntries;
+    if (small) {
+        hipLaunchKernelGGL((book_small_kernel<OP>), dim3(1), dim3(kSmallThreads), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((book_count_kernel<OP>), dim3(static_cast<unsigned>(a.B + a.chunks)), dim3(kBookThreads), 0, s, a);
+        hipLaunchKernelGGL((book_plan_kernel<OP>), dim3(a.B), dim3(kBookThreads), 0, s, a);
+    }
     if constexpr (OP == kBookHold) {
-        hipLaunchKernelGGL(book_hold_kernel, dim3(static_cast<unsigned>(blocks < 1024 ? blocks : 1024)), dim3(kBookThreads), 0, s, a);
+        const int64_t blocks = (entries + kBookThreads - 1) / kBookThreads;
+        if (!small) hipLaunchKernelGGL(book_hold_kernel, dim3(static_cast<unsigned>(blocks < 1024 ? blocks : 1024)), dim3(kBookThreads), 0, s, a);
     } else {
         const int64_t units = entries * a.Hkv;         // (as many new pages as there are entries, at most)
         const dim3 grid(static_cast<unsigned>(units < 8 * kPlanCus ? units : 8 * kPlanCus)), threads(kBookThreads);
+        const auto copy = [&](auto row) {
+            constexpr int ROW = decltype(row)::value;
+            if (small) hipLaunchKernelGGL((book_copy_kernel<OP, ROW, false>), grid, threads, 0, s, a);
+            else hipLaunchKernelGGL((book_copy_kernel<OP, ROW, true>), grid, threads, 0, s, a);
+        };
         const int row = a.d * (a.pages.dtype == kCacheBf16 ? 2 : 1);
-        if (row == 256) hipLaunchKernelGGL((book_copy_kernel<OP, 256>), grid, threads, 0, s, a);
-        else if (row == 128) hipLaunchKernelGGL((book_copy_kernel<OP, 128>), grid, threads, 0, s, a);
-        else hipLaunchKernelGGL((book_copy_kernel<OP, 64>), grid, threads, 0, s, a);
+        if (row == 256) copy(Constant<256>{});
+        else if (row == 128) copy(Constant<128>{});
+        else copy(Constant<64>{});
     }
     return hipGetLastError();
 }

@@ -230,6 +230,7 @@ struct PromptArgs {
     int B, Hq, Hkv, T, d, Gh, n_seq, causal;
     int rows;                  // Gh * T query rows of a KV head, row i * Gh + g: token i of its head g
     float scale;               // log2(e) / sqrt(d)
+    bool by_head;              // the launch's order of workgroups, by head or by row tile
 };
 
 // Changes of the pages that sequences hold.

@@ -26,9 +26,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // (lambdas of a kernel's registers that are called in several places)
 #define kInline __attribute__((always_inline))
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
-constexpr int kRows = 32 * kWaves;         // query rows of a workgroup
 constexpr int kKeys = 64;                  // keys of a tile
 constexpr float kNone = -3e38f;            // reference before the first visible key
 // The reference moves, to kLead above the largest logit so far, where a lane's 16
@@ -46,6 +43,16 @@ __device__ __forceinline__ float half_max(float x) {
 __device__ __forceinline__ float half_sum(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// sum + the two bf16 values of y, by one instruction (DOT) or two additions: the vector
+// pipe bounds d = 64, at d = 128 the additions let the clock be higher.
+template <bool DOT>
+__device__ __forceinline__ float add_pair(uint32_t y, float sum) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    if constexpr (!DOT) return sum + (__uint_as_float(y << 16) + __uint_as_float(y & 0xFFFF0000u));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, y), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum,
+                                           false);
 }
 
 // Byte of 16-byte chunk ch of row r of a staged tile; the chunks of a row are
@@ -72,8 +79,11 @@ struct Span {
     int lo, hi;
 };
 
-template <int D, bool LSE>
-__global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
+template <int D, bool LSE, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
+    constexpr int kWaves = WAVES, kThreads = 64 * WAVES;
+    constexpr int kRows = 32 * WAVES;      // query rows of a workgroup
+    constexpr int kWords = kRows / 64;
     constexpr int KC = D / 16;             // 16-dim steps of S
     constexpr int NT = D / 32;             // 32-dim tiles of O
     constexpr int kCh = D / 8;             // 16-byte chunks of a row
@@ -82,16 +92,27 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
     // (a variable for each stage: the compiler then sees which reads of LDS need not
     // wait for the loads to it that are under way)
     __shared__ __align__(16) char kt0[kKeys * 2 * D], kt1[kKeys * 2 * D], vt0[kKeys * 2 * D], vt1[kKeys * 2 * D];
-    __shared__ unsigned long long begins[2];           // tokens of the row tile that begin a sequence
+    __shared__ unsigned long long begins[kWords];      // tokens of the row tile that begin a sequence
     __shared__ int edge[3];                // last start at or before the tile, first behind it, end of the last sequence
     __shared__ int poisoned[2];            // by buffer: the last tile staged there with values of V that are not finite
 
-    const int bc = blockIdx.x, b = bc / a.Hkv, c = bc - b * a.Hkv;
-    const int r0 = static_cast<int>(gridDim.y - 1 - blockIdx.y) * kRows;   // the last rows, which see most keys, first
+    // Consecutive workgroups are on different XCDs.  Of long sequences each XCD has a KV
+    // head of its own with all row tiles, as long as there are eight heads, so that its
+    // cache serves them the same keys (4 x 32 heads of 8192 tokens on 32: 2.47 -> 2.19
+    // ms); the heads that are left are shared by all.  Of shorter ones all heads' long
+    // rows come first (32 heads of 4096 on 32: 164 us, by head 184).
+    const uint32_t heads = a.B * a.Hkv, row_tiles = (a.rows + kRows - 1) / kRows;
+    const uint32_t alone = a.by_head ? heads / 8 * 8 : 0, shared = heads - alone;
+    const uint32_t own = alone / 8 * row_tiles;        // workgroups of an XCD with heads of its own
+    const uint32_t turn = blockIdx.x / 8, rest = blockIdx.x - 8 * own;
+    const uint32_t bc = turn < own ? blockIdx.x % 8 + turn / row_tiles * 8 : alone + rest % shared;
+    const int b = bc / a.Hkv, c = bc - b * a.Hkv;
+    // the last rows, which see most keys, first
+    const int r0 = (row_tiles - 1 - (turn < own ? turn % row_tiles : rest / shared)) * kRows;
     const int tid = threadIdx.x, lane = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane >> 5;
-    const int i0 = r0 / a.Gh, i1 = min((r0 + kRows - 1) / a.Gh, a.T - 1);  // tokens of the row tile: at most 128
+    const int i0 = r0 / a.Gh, i1 = min((r0 + kRows - 1) / a.Gh, a.T - 1);  // tokens of the row tile
 
     // this lane's row and the keys [lo, hi) that it sees; `first`, `last`: tokens of the
     // tile that are in some sequence
@@ -99,7 +120,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
     const int i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
     int lo = 0, hi = a.T, first = i0, last = i1, lo_first = 0, lo_last = 0, hi_first = a.T, hi_last = a.T;
     if (a.starts) {
-        if (tid < 2) begins[tid] = 0;
+        if (tid < kWords) begins[tid] = 0;
         if (tid < 3) edge[tid] = tid == 1 ? a.T : tid == 0 ? -1 : 0;
         __syncthreads();
         for (int s = tid; s <= a.n_seq; s += kThreads) {
@@ -110,20 +131,31 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
             if (s == a.n_seq) edge[2] = t;
         }
         __syncthreads();
-        const unsigned long long w0 = begins[0], w1 = begins[1];
+        unsigned long long word[kWords];
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) word[w] = begins[w];
         const int before = edge[0], behind = edge[1], end = edge[2];
         const auto span = [&](int t) {     // of token t of the tile
-            const int x = t - i0;
-            const unsigned long long below0 = x >= 63 ? ~0ull : (2ull << x) - 1;       // bits up to x
-            const unsigned long long below1 = x < 64 ? 0ull : x >= 127 ? ~0ull : (2ull << (x - 64)) - 1;
-            const unsigned long long p0 = w0 & below0, p1 = w1 & below1, n0 = w0 & ~below0, n1 = w1 & ~below1;
-            Span y;
-            y.lo = p1 ? i0 + 127 - __builtin_clzll(p1) : p0 ? i0 + 63 - __builtin_clzll(p0) : before;
-            y.hi = n0 ? i0 + __builtin_ctzll(n0) : n1 ? i0 + 64 + __builtin_ctzll(n1) : behind;
+            Span y{before, behind};
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {         // the bits up to t, and those behind
+                const int x = t - i0 - 64 * w;
+                const unsigned long long upto = x < 0 ? 0ull : x >= 63 ? ~0ull : (2ull << x) - 1;
+                if (word[w] & upto) y.lo = i0 + 64 * w + 63 - __builtin_clzll(word[w] & upto);
+            }
+#pragma unroll
+            for (int w = kWords - 1; w >= 0; --w) {
+                const int x = t - i0 - 64 * w;
+                const unsigned long long upto = x < 0 ? 0ull : x >= 63 ? ~0ull : (2ull << x) - 1;
+                if (word[w] & ~upto) y.hi = i0 + 64 * w + __builtin_ctzll(word[w] & ~upto);
+            }
             return y;
         };
         // tokens before the first start (no start at or before them) are in no sequence
-        first = before >= 0 ? i0 : w0 ? i0 + __builtin_ctzll(w0) : w1 ? i0 + 64 + __builtin_ctzll(w1) : i1 + 1;
+        if (before < 0) first = i1 + 1;
+#pragma unroll
+        for (int w = kWords - 1; w >= 0; --w)
+            if (before < 0 && word[w]) first = i0 + 64 * w + __builtin_ctzll(word[w]);
         last = min(i1, end - 1);
         if (first > last) return;
         const Span y = span(min(max(i, i0), i1)), f = span(first), g = span(last);
@@ -241,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
         auto pair = [&](int j) kInline {
             const float x0 = fast_exp2(logit(2 * j, m)), x1 = fast_exp2(logit(2 * j + 1, m));
             const uint32_t y = pack_bf16(x0, x1);
-            sum += __uint_as_float(y << 16) + __uint_as_float(y & 0xFFFF0000u);
+            sum = add_pair<D == 64>(y, sum);
             if (LSE) sum_all += x0 + x1;
             p[U][j] = y;
         };
@@ -394,29 +426,48 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_kernel(PromptArgs a) {
     }
     l = half_sum(l);
     if (LSE) l_all = half_sum(l_all);
-    if (!there) return;
+    if (LSE && there && half == 0)
+        a.lse[(static_cast<int64_t>(b) * a.Hq + h) * a.T + i] = (m + __builtin_amdgcn_logf(l_all)) * 0.6931471805599453f;
+    // Results by way of LDS, so that a store writes whole rows: a wave's 32 rows, their
+    // chunks permuted by the row.  Value 4 w + j of o[t] is dim 32 t + 8 w + 4 half + j.
     const float inv = 1.f / l;
-    uint16_t* out = a.out + b * a.osb + h * a.osh + i * a.ost + 4 * half;
-    // value 4 w + j of o[t] is dim 32 t + 8 w + 4 half + j
+    const int64_t to = there ? b * a.osb + h * a.osh + i * a.ost : -1;     // this lane's row
+    __syncthreads();                       // (the last tile has been read)
+    static_assert(kWaves * 64 * D <= 2 * kKeys * 2 * D * 2, "rows fit the stages");
+    char* const rows = (wave < kWaves / 2 ? kt0 : vt0) + 64 * D * (wave % (kWaves / 2));
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-            *reinterpret_cast<u32x2*>(out + 32 * t + 8 * w) =
+            *reinterpret_cast<u32x2*>(rows + (lane & 31) * 2 * D + 16 * ((4 * t + w) ^ (lane & (kCh - 1))) + 8 * half) =
                 u32x2{pack_bf16(o[t][4 * w] * inv, o[t][4 * w + 1] * inv),
                       pack_bf16(o[t][4 * w + 2] * inv, o[t][4 * w + 3] * inv)};
-    if (LSE && half == 0)
-        a.lse[(static_cast<int64_t>(b) * a.Hq + h) * a.T + i] = (m + __builtin_amdgcn_logf(l_all)) * 0.6931471805599453f;
+#pragma unroll
+    for (int j = 0; j < 32; j += kWave / kCh) {
+        const int row = j + lane / kCh, ch = lane % kCh;
+        const u32x4 y = *reinterpret_cast<const u32x4*>(rows + row * 2 * D + 16 * (ch ^ (row & (kCh - 1))));
+        const int64_t at = __shfl(to, row);
+        if (at >= 0) *reinterpret_cast<u32x4*>(a.out + at + 8 * ch) = y;
+    }
 }
 
 }  // namespace
 
-hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s) {
-    const dim3 grid(static_cast<unsigned>(a.B * a.Hkv), (a.rows + kRows - 1) / kRows);
-    if (a.d == 64 && a.lse) hipLaunchKernelGGL((prompt_kernel<64, true>), grid, dim3(kThreads), 0, s, a);
-    else if (a.d == 64) hipLaunchKernelGGL((prompt_kernel<64, false>), grid, dim3(kThreads), 0, s, a);
-    else if (a.lse) hipLaunchKernelGGL((prompt_kernel<128, true>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((prompt_kernel<128, false>), grid, dim3(kThreads), 0, s, a);
+hipError_t launch_prompt_attention(const PromptArgs& args, hipStream_t s) {
+    constexpr int kLong = 8192;            // tokens of a sequence, on average
+    PromptArgs a = args;
+    a.by_head = a.T / (a.starts ? a.n_seq : 1) >= kLong;
+    const auto run = [&](auto d, auto waves) {
+        constexpr int D = decltype(d)::value, W = decltype(waves)::value, kRows = 32 * W;
+        const dim3 grid(static_cast<unsigned>(a.B) * a.Hkv * ((a.rows + kRows - 1) / kRows));
+        if (a.lse) hipLaunchKernelGGL((prompt_kernel<D, true, W>), grid, dim3(64 * W), 0, s, a);
+        else hipLaunchKernelGGL((prompt_kernel<D, false, W>), grid, dim3(64 * W), 0, s, a);
+    };
+    // Eight waves fetch a tile for twice the rows, which at d = 128 lets the matrix pipe
+    // run at a higher clock; four have twice the workgroups, and less beside the diagonal.
+    if (a.d == 64) run(Constant<64>{}, Constant<4>{});
+    else if (a.by_head) run(Constant<128>{}, Constant<8>{});
+    else run(Constant<128>{}, Constant<4>{});
     return hipGetLastError();
 }
 

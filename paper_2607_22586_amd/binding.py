@@ -926,26 +926,25 @@ def cache_book_workspace(B, Hkv, n_pages, max_pages) -> int:
                                                              int(max_pages)))
 
 
-def _book(name: str, cache: PagedCache, missing, workspace, *args):
-    """A call that changes the pages of `cache`; args: tensors ([B, ...] int32, contiguous) and numbers."""
-    tensors = [a for a in args if isinstance(a, torch.Tensor)]
-    i = _same_device(cache.k, cache.refs, missing, workspace, *tensors)
-    pages = cache.c_pages()
-    n_pages, Hkv, _, d = cache.k.shape
-    B, most = cache.table.shape
-    if cache.refs is None:
+def _book(name: str, cache: PagedCache, missing, workspace, tensors, *args):
+    """A call that changes the pages of `cache`; tensors: those of the call, args: their pointers and numbers."""
+    k, refs = cache.k, cache.refs
+    if refs is None:
         raise ValueError("the cache has no refs: its pages are not given or taken")
-    refs = _int32(cache.refs, (n_pages,), "refs")
+    i = _same_device(k, refs, missing, workspace, *tensors)
+    pages = cache.c_pages()
+    n_pages, Hkv, _, d = k.shape
+    B, most = cache.table.shape
+    counts = _int32(refs, (n_pages,), "refs")
     if missing is None:
-        missing = cache.refs.new_empty((B,))
-    rows = _int32(missing, (B,), "missing")
+        missing = refs.new_empty(B)
+    lack = _int32(missing, (B,), "missing")
     ref = ctypes.byref
     shape = ref(Shape(B, 0, Hkv, 0, 0, d))
     ws = workspace
     if ws is None:
-        ws = _ws(load_library().mmshiftkv_cache_book_workspace(shape, n_pages, most), cache.k.device)
-    _enqueue(name, i, shape, ref(pages), refs, *[_p(a) if isinstance(a, torch.Tensor) else a for a in args], rows,
-             ws.data_ptr(), ws.numel() * ws.element_size())
+        ws = _ws(load_library().mmshiftkv_cache_book_workspace(shape, n_pages, most), k.device)
+    _enqueue(name, i, shape, ref(pages), counts, *args, lack, ws.data_ptr(), ws.numel() * ws.element_size())
     return missing
 
 
@@ -953,8 +952,8 @@ def cache_hold(cache: PagedCache, rows: torch.Tensor, missing: torch.Tensor | No
                workspace: torch.Tensor | None = None) -> torch.Tensor:
     """mmshiftkv_cache_hold: each sequence holds the pages for max(rows[b]) rows (rows [B, Hkv] int32),
     taken from the free ones or given back.  Returns missing [B] int32: the pages that it did not get."""
-    _int32(rows, (cache.table.shape[0], cache.k.shape[1]), "rows")
-    return _book("mmshiftkv_cache_hold", cache, missing, workspace, rows)
+    at = _int32(rows, (cache.table.shape[0], cache.k.shape[1]), "rows")
+    return _book("mmshiftkv_cache_hold", cache, missing, workspace, (rows,), at)
 
 
 def cache_fork(cache: PagedCache, src: torch.Tensor, lens: torch.Tensor, missing: torch.Tensor | None = None,
@@ -963,9 +962,8 @@ def cache_fork(cache: PagedCache, src: torch.Tensor, lens: torch.Tensor, missing
     stays) as that was before the call, sharing the pages that are full; lens [B, Hkv] int32 follows.
     Returns missing [B] int32: the pages that it did not get (then it stays as it was)."""
     B = cache.table.shape[0]
-    _int32(src, (B,), "src")
-    _int32(lens, (B, cache.k.shape[1]), "lens")
-    return _book("mmshiftkv_cache_fork", cache, missing, workspace, src, lens)
+    args = _int32(src, (B,), "src"), _int32(lens, (B, cache.k.shape[1]), "lens")
+    return _book("mmshiftkv_cache_fork", cache, missing, workspace, (src, lens), *args)
 
 
 def cache_compact(cache: PagedCache, lens: torch.Tensor, idx: torch.Tensor, counts: torch.Tensor,
@@ -974,11 +972,9 @@ def cache_compact(cache: PagedCache, lens: torch.Tensor, idx: torch.Tensor, coun
     each head, on new pages, and lens [B, Hkv] follows (a Selected over the cached rows: its idx and counts;
     all counts of a sequence below 0: it stays).  All int32.  Returns missing [B] int32, as cache_fork."""
     shape = (cache.table.shape[0], cache.k.shape[1])
-    _int32(lens, shape, "lens")
-    _int32(counts, shape, "counts")
     n = idx.shape[-1]
-    _int32(idx, shape + (n,), "idx")
-    return _book("mmshiftkv_cache_compact", cache, missing, workspace, lens, idx, counts, n)
+    args = _int32(lens, shape, "lens"), _int32(idx, shape + (n,), "idx"), _int32(counts, shape, "counts"), n
+    return _book("mmshiftkv_cache_compact", cache, missing, workspace, (lens, idx, counts), *args)
 
 
 @dataclass

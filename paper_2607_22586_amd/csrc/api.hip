@@ -974,6 +974,7 @@ size_t book_layout(int B, int Hkv, int n_pages, int max_pages, char* base, BookA
     a->taken = reinterpret_cast<int32_t*>(part(4));
     a->want = reinterpret_cast<int32_t*>(part(4 * static_cast<size_t>(B)));
     a->free = reinterpret_cast<int32_t*>(part(4 * static_cast<size_t>(book_chunks(n_pages))));
+    a->free_bits = reinterpret_cast<uint64_t*>(part(static_cast<size_t>(book_chunks(n_pages)) * (kBookChunk / 8)));
     a->ids = reinterpret_cast<int32_t*>(part(4 * entries));
     a->items = reinterpret_cast<int2*>(part(8 * entries));
     a->old_table = reinterpret_cast<int32_t*>(part(4 * entries));

@@ -246,13 +246,14 @@ struct BookArgs {
     int32_t* missing;          // [B]
     int B, Hkv, d, n;
     int64_t chunks;            // book_chunks(n_pages)
-    // workspace: of each sequence the pages wanted, of each chunk the free ones; of the
-    // new pages, in order, their number, their ids and (sequence, entry); the table and
-    // the lengths as they were
-    int32_t* want; int32_t* free; int32_t* taken; int32_t* ids; int2* items;
+    // workspace: of each sequence the pages wanted, of each chunk the free ones, each
+    // page's bit among them; of the new pages, in order, their number, their ids and
+    // (sequence, entry); the table and the lengths as they were
+    int32_t* want; int32_t* free; uint64_t* free_bits; int32_t* taken; int32_t* ids; int2* items;
     int32_t* old_table; int32_t* old_lens;
 };
-int64_t book_chunks(int n_pages);
+constexpr int kBookChunk = 2048;           // pages of a chunk
+inline int64_t book_chunks(int n_pages) { return (static_cast<int64_t>(n_pages) + kBookChunk - 1) / kBookChunk; }
 
 // Upper end of the lane sums (keys_per_sum terms of 2^s each) that the score
 // and decode kernels add relative to zero.  A row's total over T keys is

@@ -1,22 +1,27 @@
 // Pages of a paged cache given, taken and copied on gfx950
 // (mmshiftkv_cache_hold, _fork and _compact).  The numbers of rows are the
 // device's (a selection leaves them there), so the pages are assigned there too,
-// without a wait of the host.  Three kernels:
-//   count  what each sequence wants, the free pages of each chunk of the pool,
-//          a copy of the table and the lengths as they were;
-//   plan   each sequence's new row of the table.  The pages wanted are ranked by
-//          sequence and entry, the free ones by number, and rank r gets the r-th
-//          free page: the outcome does not depend on the order of workgroups;
-//   apply  the counters, by the difference of the two tables, and the rows that a
-//          fork or a compaction copies: a unit of work is one head of one new page.
-// The first two are bound by latency, the copies by HBM.
+// without a wait of the host:
+//   count  what each sequence wants, the free pages of the pool as bits and by chunk, a
+//          copy of the table and the lengths as they were;
+//   plan   each sequence's new row of the table, and the counters by the difference of
+//          the two.  The pages wanted are ranked by sequence and entry, the free ones by
+//          number, and rank r gets the r-th free page: the outcome does not depend on the
+//          order of workgroups;
+//   copy   the rows that a fork or a compaction copies: a unit of work is one head of one
+//          new page.
+// For small pools and tables one workgroup does the first two (a launch less: 3 us of the
+// host's time and of the GPU's; 4 to 5 us for 768 entries, 12 for 5000, which the two
+// kernels take 8 for).  They are bound by latency, the copies by HBM: 56 forks' tails of
+// 8 heads of e4m3 rows, 132 MB, 18.5 us; a quarter of 8 x 8 heads of up to 32768 bf16
+// rows, 345 MB, 66 us.
 #include "pages.hpp"
 
 namespace mmskv {
 namespace {
 
 constexpr int kBookThreads = 256;
-constexpr int kChunk = 8 * kBookThreads;   // pages of a chunk
+constexpr int kChunk = kBookChunk;
 
 __device__ __forceinline__ bool named(const Pages& p, int id) {
     return static_cast<uint32_t>(id) < static_cast<uint32_t>(p.n_pages);
@@ -114,6 +119,15 @@ __device__ __forceinline__ int new_len(const BookArgs& a, const Change& c, int b
                            : min(max(a.rows[static_cast<int64_t>(b) * a.Hkv + h], 0), a.n);
 }
 
+// An entry of the table and the counters of the pages that it named and names.  (Nobody
+// else writes the entry; the counters are sums, in any order.)
+__device__ __forceinline__ void change_entry(const BookArgs& a, int64_t e, int old, int now) {
+    if (now == old) return;
+    a.table[e] = now;
+    if (named(a.pages, old)) atomicSub(a.refs + old, 1);
+    if (named(a.pages, now)) atomicAdd(a.refs + now, 1);
+}
+
 template <int OP>
 __global__ void __launch_bounds__(kBookThreads) book_count_kernel(BookArgs a) {
     __shared__ int lds[2 * kBookThreads / kWave];
@@ -121,11 +135,16 @@ __global__ void __launch_bounds__(kBookThreads) book_count_kernel(BookArgs a) {
     int total;
     if (b >= a.B) {
         const int64_t p0 = static_cast<int64_t>(b - a.B) * kChunk;
-        int x = 0;
+        int n[kChunk / kBookThreads], x = 0;
+#pragma unroll
+        for (int j = 0; j < kChunk / kBookThreads; ++j) n[j] = a.refs[min(p0 + j * kBookThreads + tid, static_cast<int64_t>(a.pages.n_pages) - 1)];
 #pragma unroll
         for (int j = 0; j < kChunk / kBookThreads; ++j) {
             const int64_t p = p0 + j * kBookThreads + tid;
-            x += p < a.pages.n_pages && a.refs[p] == 0;
+            const bool is_free = p < a.pages.n_pages && n[j] == 0;
+            const uint64_t word = __ballot(is_free);
+            if (lane_id() == 0) a.free_bits[p / kWave] = word;
+            x += is_free;
         }
         block_scan(x, lds, &total);
         if (tid == 0) a.free[b - a.B] = total;
@@ -170,17 +189,12 @@ __global__ void __launch_bounds__(kBookThreads) book_plan_kernel(BookArgs a) {
         for (int i = i0; i <= i1; ++i) {
             const int before = i ? upto[i - 1] : run;
             if (before == upto[i]) continue;
-            const int64_t p0 = (x0 + i) * kChunk + tid * (kChunk / kBookThreads);
-            int here = 0, all;
-#pragma unroll
-            for (int j = 0; j < kChunk / kBookThreads; ++j) here += p0 + j < a.pages.n_pages && a.refs[p0 + j] == 0;
-            int rank = before + block_scan(here, lds, &all) - here;
-#pragma unroll
-            for (int j = 0; j < kChunk / kBookThreads; ++j) {
-                if (p0 + j >= a.pages.n_pages || a.refs[p0 + j] != 0) continue;
-                if (rank >= lo && rank < hi) a.ids[rank] = static_cast<int>(p0 + j);
-                ++rank;
-            }
+            static_assert(kChunk == 8 * kBookThreads, "a byte of the chunk's bits for each thread");
+            const int64_t byte = (x0 + i) * kBookThreads + tid;
+            uint32_t bits = reinterpret_cast<const uint8_t*>(a.free_bits)[byte];
+            int all, rank = before + block_scan(__popc(bits), lds, &all) - __popc(bits);
+            for (; bits != 0; bits &= bits - 1, ++rank)
+                if (rank >= lo && rank < hi) a.ids[rank] = static_cast<int>(8 * byte + __ffs(bits) - 1);
         }
         run += total;
         __syncthreads();
@@ -202,8 +216,9 @@ __global__ void __launch_bounds__(kBookThreads) book_plan_kernel(BookArgs a) {
         const int at = rank + block_scan(take, lds, &total) - 1;
         rank += total;
         if (j >= a.pages.max_pages) continue;
-        a.table[row + j] = take ? (ok ? a.ids[at] : -1) : stays<OP>(a, c, j, id);
+        const int old = a.old_table[row + j], now = take ? (ok ? a.ids[at] : -1) : stays<OP>(a, c, j, id);
         if (OP != kBookHold && take) a.items[at] = make_int2(b, j);
+        change_entry(a, row + j, old, now);
     }
     if (OP == kBookHold) return;
     for (int h = tid; h < a.Hkv; h += kBookThreads) a.lens[static_cast<int64_t>(b) * a.Hkv + h] = new_len<OP>(a, c, b, h);
@@ -215,8 +230,8 @@ __global__ void __launch_bounds__(kBookThreads) book_plan_kernel(BookArgs a) {
 // of a wanted page is the number of those before it, whatever the sequence.
 constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / kWave;
 constexpr int kSmallSeqs = 1024, kSmallHeads = 64;
-constexpr int kSmallEach = 8;              // pages, and entries, of a thread
-constexpr int kSmallPages = kSmallEach * kSmallThreads, kSmallEntries = kSmallEach * kSmallThreads;
+constexpr int kSmallEach = 4, kSmallFree = 8;      // entries, and pages, of a thread
+constexpr int kSmallPages = kSmallFree * kSmallThreads, kSmallEntries = kSmallEach * kSmallThreads;
 
 template <int OP>
 __global__ void __launch_bounds__(kSmallThreads) book_small_kernel(BookArgs a) {
@@ -241,11 +256,11 @@ __global__ void __launch_bounds__(kSmallThreads) book_small_kernel(BookArgs a) {
     // the free pages, a thread's consecutive ones
     const int per = (a.pages.n_pages + kSmallThreads - 1) / kSmallThreads, p0 = tid * per;
     uint32_t is_free = 0;
-    int count[kSmallEach];
+    int count[kSmallFree];
 #pragma unroll
-    for (int j = 0; j < kSmallEach; ++j) count[j] = a.refs[min(p0 + j, a.pages.n_pages - 1)];
+    for (int j = 0; j < kSmallFree; ++j) count[j] = a.refs[min(p0 + j, a.pages.n_pages - 1)];
 #pragma unroll
-    for (int j = 0; j < kSmallEach; ++j)
+    for (int j = 0; j < kSmallFree; ++j)
         is_free |= static_cast<uint32_t>(j < per && p0 + j < a.pages.n_pages && count[j] == 0) << j;
     if (tid < a.B) {
         const Change c = change_of<OP>(a, tid, a.lens, [&](const int32_t* rows) {
@@ -323,31 +338,14 @@ __global__ void __launch_bounds__(kSmallThreads) book_small_kernel(BookArgs a) {
         if (!c.moves || (OP != kBookHold && !fits)) continue;
         const int now = new_page ? (fits ? free_ids[at] : -1) : stays<OP>(a, c, j, theirs[x]);
         if (OP != kBookHold && new_page) a.items[at] = make_int2(b, j), a.ids[at] = now;
-        if (now == own[x]) continue;
-        a.table[e] = now;
-        if (named(a.pages, own[x])) atomicSub(a.refs + own[x], 1);
-        if (named(a.pages, now)) atomicAdd(a.refs + now, 1);
+        change_entry(a, e, own[x], now);
     }
 }
-
-// Every entry that changed: one naming less of its old page, one more of its new.
-__device__ __forceinline__ void count_changes(const BookArgs& a) {
-    const int64_t entries = static_cast<int64_t>(a.B) * a.pages.max_pages;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kBookThreads;
-    for (int64_t e = static_cast<int64_t>(blockIdx.x) * kBookThreads + threadIdx.x; e < entries; e += step) {
-        const int before = a.old_table[e], after = a.table[e];
-        if (before == after) continue;
-        if (named(a.pages, before)) atomicSub(a.refs + before, 1);
-        if (named(a.pages, after)) atomicAdd(a.refs + after, 1);
-    }
-}
-
-__global__ void __launch_bounds__(kBookThreads) book_hold_kernel(BookArgs a) { count_changes(a); }
 
 // Rows of one head of one new page, 16 bytes a lane: a group of lanes has a row of K
 // and of V.  Fork: the rows of the page that the source has there; compact: the rows
 // that idx names, zeros (scale 1) where it names none.
-template <int OP, int ROW, bool COUNT>     // bytes of a row; whether the counters are left to it
+template <int OP, int ROW>                 // bytes of a row
 __global__ void __launch_bounds__(kBookThreads) book_copy_kernel(BookArgs a) {
     constexpr int kCh = ROW / 16, kPer = kBookThreads / kCh;
     const int page = 1 << a.pages.shift, ch = threadIdx.x % kCh;
@@ -385,7 +383,6 @@ __global__ void __launch_bounds__(kBookThreads) book_copy_kernel(BookArgs a) {
             if (a.pages.dtype != kCacheBf16 && ch == 0) a.pages.k_scale[to + r] = ks, a.pages.v_scale[to + r] = vs;
         }
     }
-    if (COUNT) count_changes(a);
 }
 
 template <int OP>
@@ -398,16 +395,11 @@ hipError_t launch(const BookArgs& a, hipStream_t s) {
         hipLaunchKernelGGL((book_count_kernel<OP>), dim3(static_cast<unsigned>(a.B + a.chunks)), dim3(kBookThreads), 0, s, a);
         hipLaunchKernelGGL((book_plan_kernel<OP>), dim3(a.B), dim3(kBookThreads), 0, s, a);
     }
-    if constexpr (OP == kBookHold) {
-        const int64_t blocks = (entries + kBookThreads - 1) / kBookThreads;
-        if (!small) hipLaunchKernelGGL(book_hold_kernel, dim3(static_cast<unsigned>(blocks < 1024 ? blocks : 1024)), dim3(kBookThreads), 0, s, a);
-    } else {
+    if constexpr (OP != kBookHold) {
         const int64_t units = entries * a.Hkv;         // (as many new pages as there are entries, at most)
-        const dim3 grid(static_cast<unsigned>(units < 8 * kPlanCus ? units : 8 * kPlanCus)), threads(kBookThreads);
+        const dim3 grid(static_cast<unsigned>(units < 8 * kPlanCus ? units : 8 * kPlanCus));
         const auto copy = [&](auto row) {
-            constexpr int ROW = decltype(row)::value;
-            if (small) hipLaunchKernelGGL((book_copy_kernel<OP, ROW, false>), grid, threads, 0, s, a);
-            else hipLaunchKernelGGL((book_copy_kernel<OP, ROW, true>), grid, threads, 0, s, a);
+            hipLaunchKernelGGL((book_copy_kernel<OP, decltype(row)::value>), grid, dim3(kBookThreads), 0, s, a);
         };
         const int row = a.d * (a.pages.dtype == kCacheBf16 ? 2 : 1);
         if (row == 256) copy(Constant<256>{});
@@ -418,8 +410,6 @@ hipError_t launch(const BookArgs& a, hipStream_t s) {
 }
 
 }  // namespace
-
-int64_t book_chunks(int n_pages) { return (static_cast<int64_t>(n_pages) + kChunk - 1) / kChunk; }
 
 hipError_t launch_book(const BookArgs& a, int op, hipStream_t s) {
     return op == kBookHold ? launch<kBookHold>(a, s) : op == kBookFork ? launch<kBookFork>(a, s) : launch<kBookCompact>(a, s);

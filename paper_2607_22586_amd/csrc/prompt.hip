@@ -79,19 +79,22 @@ struct Span {
     int lo, hi;
 };
 
-template <int D, bool LSE, int WAVES>
+// Workgroup: WAVES waves, GROUPS of them with the same 32 rows, each with 64 keys of a
+// tile of its own; their sums are joined at the end.
+template <int D, bool LSE, int WAVES, int GROUPS>
 __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
     constexpr int kWaves = WAVES, kThreads = 64 * WAVES;
-    constexpr int kRows = 32 * WAVES;      // query rows of a workgroup
+    constexpr int kRows = 32 * WAVES / GROUPS;         // query rows of a workgroup
+    constexpr int kTile = kKeys * GROUPS;              // keys of a tile
     constexpr int kWords = kRows / 64;
     constexpr int KC = D / 16;             // 16-dim steps of S
     constexpr int NT = D / 32;             // 32-dim tiles of O
     constexpr int kCh = D / 8;             // 16-byte chunks of a row
-    constexpr int kWaveRows = kKeys / kWaves;
+    constexpr int kWaveRows = kTile / kWaves;
     constexpr int kLoads = kWaveRows * 2 * D / 1024;   // 16-byte loads of a lane of K (and of V)
     // (a variable for each stage: the compiler then sees which reads of LDS need not
     // wait for the loads to it that are under way)
-    __shared__ __align__(16) char kt0[kKeys * 2 * D], kt1[kKeys * 2 * D], vt0[kKeys * 2 * D], vt1[kKeys * 2 * D];
+    __shared__ __align__(16) char kt0[kTile * 2 * D], kt1[kTile * 2 * D], vt0[kTile * 2 * D], vt1[kTile * 2 * D];
     __shared__ unsigned long long begins[kWords];      // tokens of the row tile that begin a sequence
     __shared__ int edge[3];                // last start at or before the tile, first behind it, end of the last sequence
     __shared__ int poisoned[2];            // by buffer: the last tile staged there with values of V that are not finite
@@ -112,11 +115,12 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
     const int tid = threadIdx.x, lane = lane_id();
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane >> 5;
+    const int rows32 = wave % (kWaves / GROUPS), group = wave / (kWaves / GROUPS);
     const int i0 = r0 / a.Gh, i1 = min((r0 + kRows - 1) / a.Gh, a.T - 1);  // tokens of the row tile
 
     // this lane's row and the keys [lo, hi) that it sees; `first`, `last`: tokens of the
     // tile that are in some sequence
-    const int r = r0 + 32 * wave + (lane & 31);
+    const int r = r0 + 32 * rows32 + (lane & 31);
     const int i = r / a.Gh, h = c * a.Gh + (r - i * a.Gh);
     int lo = 0, hi = a.T, first = i0, last = i1, lo_first = 0, lo_last = 0, hi_first = a.T, hi_last = a.T;
     if (a.starts) {
@@ -165,9 +169,9 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
     if (a.causal) hi = i + 1, hi_first = first + 1, hi_last = last + 1;
     const uint32_t sees = there ? hi - lo : 0;
     const int key00 = lo_first;            // the first tile's first key
-    const int tiles = (hi_last - key00 + kKeys - 1) / kKeys;
+    const int tiles = (hi_last - key00 + kTile - 1) / kTile;
     // tiles [clear0, clear1): every row that is there sees all keys
-    const int clear0 = (lo_last - key00 + kKeys - 1) / kKeys, clear1 = (hi_first - key00) / kKeys;
+    const int clear0 = (lo_last - key00 + kTile - 1) / kTile, clear1 = (hi_first - key00) / kTile;
 
     const uint16_t* const kb = a.k + b * a.ksb + c * a.ksh;
     const uint16_t* const vb = a.v + b * a.vsb + c * a.vsh;
@@ -364,21 +368,22 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
     const int masked = tiles - max(clear1 - clear0, 0), ahead = min(clear0, masked);
     const auto key_of = [&](int n) {       // first key of the n-th tile worked on
         const int tile = n < ahead ? n : n < masked ? n + (tiles - masked) : n - masked + ahead;
-        return key00 + tile * kKeys;
+        return key00 + tile * kTile;
     };
     // Tile n, in stage W: K of the next tile and V of this one have landed by the middle
     // of it, where the stages of K of this tile and V of the one before are free again.
     constexpr int kHalf = kKeys / 2 * 2 * D;
+    const int mine = group * kKeys;        // this wave's keys of a tile
     auto step = [&](int n, auto which, auto part) kInline {
         constexpr int W = decltype(which)::value;
-        const int key0 = key_of(n);
-        attend(key0, Constant<0>{}, part, k_tile(which) + kHalf, v_tile(Constant<1 - W>{}) + kHalf);
+        const int key0 = key_of(n) + mine, at = mine * 2 * D;
+        attend(key0, Constant<0>{}, part, k_tile(which) + at + kHalf, v_tile(Constant<1 - W>{}) + at + kHalf);
         wait_vm<0>();
         if (decltype(part)::value) clean(n, which);
         __syncthreads();
         if (n + 2 < tiles) load_k(key_of(n + 2), which);
         if (n + 1 < tiles) load_v(key_of(n + 1), Constant<1 - W>{});
-        attend(key0 + kKeys / 2, Constant<1>{}, part, k_tile(Constant<1 - W>{}), v_tile(which));
+        attend(key0 + kKeys / 2, Constant<1>{}, part, k_tile(Constant<1 - W>{}) + at, v_tile(which) + at);
         if (decltype(part)::value && poisoned[W] == n) add_poison(key0);
     };
     // before the first tile, in stage W: its first half's S, and no weights for the half
@@ -386,8 +391,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
     auto begin = [&](auto which) kInline {
         constexpr int W = decltype(which)::value;
         load_k(key_of(0), which);
-        char* const vt = v_tile(Constant<1 - W>{}) + kHalf;
-        for (int x = 16 * tid; x < kHalf; x += 16 * kThreads) *reinterpret_cast<u32x4*>(vt + x) = u32x4{0u, 0u, 0u, 0u};
+        char* const vt = v_tile(Constant<1 - W>{});
+        for (int x = 16 * tid; x < kTile * 2 * D; x += 16 * kThreads) *reinterpret_cast<u32x4*>(vt + x) = u32x4{0u, 0u, 0u, 0u};
         wait_vm<0>();
         __syncthreads();
         if (tiles > 1) load_k(key_of(1), Constant<1 - W>{});
@@ -395,12 +400,12 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[0][e] = 0.f;
 #pragma unroll
-        for (int j = 0; j < KC; ++j) s[0] = mfma32(k_frag(k_tile(which), ka0, j), qf[j], s[0]);
+        for (int j = 0; j < KC; ++j) s[0] = mfma32(k_frag(k_tile(which) + mine * 2 * D, ka0, j), qf[j], s[0]);
     };
     auto end = [&](auto which) kInline {           // the last half's part of O, of the tile in stage W
 #pragma unroll
         for (int j = 0; j < KC; ++j)
-            o[j % NT] = mfma32(v_frag(v_tile(which) + kHalf, va0, j), p_frag(p[1], j / NT), o[j % NT]);
+            o[j % NT] = mfma32(v_frag(v_tile(which) + mine * 2 * D + kHalf, va0, j), p_frag(p[1], j / NT), o[j % NT]);
     };
     if (tid < 2) poisoned[tid] = -1;       // (seen by all behind the barriers of begin)
     int n = 0;
@@ -426,15 +431,53 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
     }
     l = half_sum(l);
     if (LSE) l_all = half_sum(l_all);
-    if (LSE && there && half == 0)
+    if constexpr (GROUPS > 1) {
+        // the groups' sums to the first one, a float of every lane side by side, by way of
+        // the stages
+        __syncthreads();                   // (the last tile has been read)
+        constexpr int kOne = (16 * NT + 4) * 256, kAll = (GROUPS - 1) * (kWaves / GROUPS), kPer = kTile * 2 * D / kOne;
+        static_assert(kPer >= 1 && kAll <= 4 * kPer, "the sums of the other groups fit the stages");
+        const auto place = [&](int g) kInline {
+            const int x = (g - 1) * (kWaves / GROUPS) + rows32;
+            char* const stage = x < kPer ? kt0 : x < 2 * kPer ? kt1 : x < 3 * kPer ? vt0 : vt1;
+            return reinterpret_cast<float*>(stage + x % kPer * kOne) + lane;
+        };
+        if (group > 0) {
+            float* const to = place(group);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) to[64 * (16 * t + j)] = o[t][j];
+            to[64 * 16 * NT] = m, to[64 * (16 * NT + 1)] = l, to[64 * (16 * NT + 2)] = l_all;
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int g = 1; g < GROUPS; ++g) {
+                const float* const from = place(g);
+                const float m1 = from[64 * 16 * NT], most = fmaxf(m, m1);
+                const float f0 = fast_exp2(m - most), f1 = fast_exp2(m1 - most);
+                m = most;
+                l = l * f0 + from[64 * (16 * NT + 1)] * f1;
+                l_all = l_all * f0 + from[64 * (16 * NT + 2)] * f1;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[t][j] = o[t][j] * f0 + from[64 * (16 * t + j)] * f1;
+            }
+        }
+    }
+    if (LSE && there && group == 0 && half == 0)
         a.lse[(static_cast<int64_t>(b) * a.Hq + h) * a.T + i] = (m + __builtin_amdgcn_logf(l_all)) * 0.6931471805599453f;
     // Results by way of LDS, so that a store writes whole rows: a wave's 32 rows, their
     // chunks permuted by the row.  Value 4 w + j of o[t] is dim 32 t + 8 w + 4 half + j.
     const float inv = 1.f / l;
     const int64_t to = there ? b * a.osb + h * a.osh + i * a.ost : -1;     // this lane's row
-    __syncthreads();                       // (the last tile has been read)
-    static_assert(kWaves * 64 * D <= 2 * kKeys * 2 * D * 2, "rows fit the stages");
-    char* const rows = (wave < kWaves / 2 ? kt0 : vt0) + 64 * D * (wave % (kWaves / 2));
+    __syncthreads();                       // (the last tile, or the sums, have been read)
+    if (group > 0) return;
+    static_assert(kRows <= 4 * kTile, "the rows fit the stages");
+    const int place = 32 * rows32 / kTile;
+    char* const rows = (place == 0 ? kt0 : place == 1 ? kt1 : place == 2 ? vt0 : vt1) + 32 * rows32 % kTile * 2 * D;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -454,20 +497,33 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
 }  // namespace
 
 hipError_t launch_prompt_attention(const PromptArgs& args, hipStream_t s) {
-    constexpr int kLong = 8192;            // tokens of a sequence, on average
     PromptArgs a = args;
-    a.by_head = a.T / (a.starts ? a.n_seq : 1) >= kLong;
-    const auto run = [&](auto d, auto waves) {
-        constexpr int D = decltype(d)::value, W = decltype(waves)::value, kRows = 32 * W;
-        const dim3 grid(static_cast<unsigned>(a.B) * a.Hkv * ((a.rows + kRows - 1) / kRows));
-        if (a.lse) hipLaunchKernelGGL((prompt_kernel<D, true, W>), grid, dim3(64 * W), 0, s, a);
-        else hipLaunchKernelGGL((prompt_kernel<D, false, W>), grid, dim3(64 * W), 0, s, a);
+    const int mean = a.T / (a.starts ? a.n_seq : 1);   // tokens of a sequence
+    a.by_head = mean >= 8192;
+    const auto workgroups = [&](int rows) { return static_cast<int64_t>(a.B) * a.Hkv * ((a.rows + rows - 1) / rows); };
+    const auto run = [&](auto d, auto waves, auto groups) {
+        constexpr int D = decltype(d)::value, W = decltype(waves)::value, G = decltype(groups)::value;
+        const dim3 grid(static_cast<unsigned>(workgroups(32 * W / G)));
+        if (a.lse) hipLaunchKernelGGL((prompt_kernel<D, true, W, G>), grid, dim3(64 * W), 0, s, a);
+        else hipLaunchKernelGGL((prompt_kernel<D, false, W, G>), grid, dim3(64 * W), 0, s, a);
     };
     // Eight waves fetch a tile for twice the rows, which at d = 128 lets the matrix pipe
-    // run at a higher clock; four have twice the workgroups, and less beside the diagonal.
-    if (a.d == 64) run(Constant<64>{}, Constant<4>{});
-    else if (a.by_head) run(Constant<128>{}, Constant<8>{});
-    else run(Constant<128>{}, Constant<4>{});
+    // run at a higher clock (4 x 28 heads of 16384 tokens 7.3 -> 7.1 ms); four have twice
+    // the workgroups, and less beside the diagonal (of 2048 tokens 149 us against 157).
+    // At d = 64 and with at most one workgroup a CU, twice or four times the waves with
+    // keys of their own shorten what each does in turn by more than the join takes, from
+    // some 512 tokens on (16 heads on 2, groups / none: 256 tokens 8.2 / 7.9 us, 512 9.9 /
+    // 11.4, 1024 13.2 / 19.9, 2048 28 / 34; at d = 128 28 heads on 4 of 1024 24.7 / 26,
+    // of 512 16.1 / 15.9).
+    if (a.d == 64) {
+        const bool deep = mean >= 512;
+        if (deep && workgroups(64) <= kPlanCus) run(Constant<64>{}, Constant<8>{}, Constant<4>{});
+        else if (deep && workgroups(128) <= kPlanCus) run(Constant<64>{}, Constant<8>{}, Constant<2>{});
+        else run(Constant<64>{}, Constant<4>{}, Constant<1>{});
+    } else {
+        if (a.by_head) run(Constant<128>{}, Constant<8>{}, Constant<1>{});
+        else run(Constant<128>{}, Constant<4>{}, Constant<1>{});
+    }
     return hipGetLastError();
 }
 

@@ -159,6 +159,30 @@ def test_a_long_row_key_by_key():
     assert torch.equal(out[0, 0], v[0, 0]) and torch.equal(out[0, 1], v[0, 0])
 
 
+@pytest.mark.parametrize("d,Hq,Hkv,T", [(64, 3, 3, 700), (64, 9, 3, 2500), (128, 3, 1, 1500), (128, 28, 4, 2049),
+                                        (128, 9, 9, 8200), (128, 10, 1, 8200)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_as_in_fp32(d, Hq, Hkv, T, causal):
+    """Longer sequences, of each launch shape, against the same formula in fp32 on the GPU: its own error, of sums
+    over T rows, is below the bound that the 64-bit form has for the kernel's (2 T u_fp32 beside bf16 roundings)."""
+    q, k, v = inputs(1, Hq, Hkv, T, d, T, "tokens")
+    out, lse = mm.prompt_attention(q, k, v, causal=causal, with_lse=True)
+    t = torch.arange(T, device=DEV)
+    for h in range(Hq):
+        c = h // (Hq // Hkv)
+        kk, vv = k[0, c].float(), v[0, c].float()
+        x = q[0, h].float() @ kk.t().contiguous() * d ** -0.5
+        size = float((q[0, h].float().abs() @ kk.abs().t().contiguous()).max()) * d ** -0.5
+        if causal:
+            x = x.masked_fill(t > t[:, None], -float("inf"))
+        p = torch.softmax(x, -1)
+        want = p @ vv
+        rel = 4 * ((d + 4) * 2.0 ** -24 * size + 2.0 ** -23) + 4 * T * 2.0 ** -24
+        bound = 2.0 ** -8 * want.abs() + (2.0 ** -8 + rel) * (p @ vv.abs())
+        assert bool(((out[0, h].float() - want).abs() <= bound).all())
+        assert float((lse[0, h] - torch.logsumexp(x, -1)).abs().max()) <= rel + 2.0 ** -22 * (size + 40)
+
+
 def test_rows_behind_four_gib():
     """Strides that put the last tokens past 4 GiB."""
     T, H, d = 70, 2, 64

@@ -499,8 +499,9 @@ int mmshiftkv_chunk_attention(const mmskv_shape *shape, const mmskv_pages *pages
  * fewer sees as many of those.  Otherwise as mmshiftkv_chunk_attention, and to
  * rounding what it gives where both tables name the same rows; an infinity or
  * NaN in a shared row's v may reach the queries of its group that do not see it.
- * B is a multiple of groups (groups = 1: one prompt for all); B / groups * Gh * n
- * and B * Hkv up to 2^22 (more -> MMSKV_EUNSUPPORTED).  T and shared_T are upper
+ * B is a multiple of groups (groups = 1: one prompt for all); B / groups * Gh * n,
+ * B * Hkv and Hkv * (groups * ceil(B / groups * Gh * n / 128) + B * ceil(Gh * n /
+ * 128)) up to 2^22, B * Hq * n up to 2^26 (more -> MMSKV_EUNSUPPORTED).  T and shared_T are upper
  * bounds of lens and shared, which fix how the work is split (shared_T = T is
  * always right, a close bound is faster).
  *   shared        [groups, Hkv] int32
@@ -528,11 +529,13 @@ int mmshiftkv_shared_attention(const mmskv_shape *shape, const mmskv_pages *page
  * bf16 products, fp32 accumulation and softmax, p rounded to bf16 for its
  * product with v, the result rounded once.  A key that a query does not see
  * does not reach it, whatever it holds, infinities and NaN included (another
- * sequence's, a later token's, padding).  Sums are divided last, as in
+ * sequence's, a later token's, padding); of one that it sees the result is not
+ * finite in that dim (of k: as a whole).  Sums are divided last, as in
  * mmshiftkv_chunk_attention.  Rows of out and lse in no sequence (before
  * starts[0], or from starts[n_seq] on) are left as they were.
- * Reads shape->B, Hq, Hkv, T and d (64 or 128); Gh * T and B * Hkv up to 2^22
- * (more -> MMSKV_EUNSUPPORTED).
+ * Reads shape->B, Hq, Hkv, T and d (64 or 128); Gh * T, B * Hkv and B * Hkv *
+ * ceil(Gh * T / 64) up to 2^22, token strides of k and v below 2^28 (more
+ * -> MMSKV_EUNSUPPORTED).
  *   q       [B, Hq, T, d] bf16;  k, v [B, Hkv, T, d] bf16, with their strides
  *   starts  [n_seq + 1] int32, ascending (sequences may be empty), taken as if
  *           clamped to [0, T]; or NULL (n_seq is ignored)

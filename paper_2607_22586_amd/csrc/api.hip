@@ -794,6 +794,7 @@ int check_cache_shape(const mmskv_shape* s) {
 // Rows of a head and (b, c) pairs that a launch of these calls can hold.
 constexpr int kMaxCacheRows = 1 << 27;
 constexpr int64_t kMaxChunkHeads = 1 << 22;
+constexpr int64_t kMaxBlocks = 1 << 22;    // workgroups in one dimension of a grid
 
 // Output rows that are written: a stride of 0 would put rows over each other.
 int check_out_rows(const void* base, const mmskv_strides* st, int eb, int nb, int nh, int nt) {
@@ -1058,7 +1059,9 @@ int mmshiftkv_prompt_attention(const mmskv_shape* shape, const uint16_t* q, cons
     if (!aligned(starts, 4) || !aligned(lse, 4)) return MMSKV_EINVAL;
     if (shape->d != 64 && shape->d != 128) return MMSKV_EUNSUPPORTED;
     const int64_t gh = shape->Hq / shape->Hkv;
-    if (gh * shape->T > (1 << 22) || static_cast<int64_t>(shape->B) * shape->Hkv > kMaxChunkHeads) return MMSKV_EUNSUPPORTED;
+    const int64_t heads = static_cast<int64_t>(shape->B) * shape->Hkv;
+    if (gh * shape->T > (1 << 22) || heads > kMaxChunkHeads) return MMSKV_EUNSUPPORTED;
+    if (heads * ((gh * shape->T + 63) / 64) > kMaxBlocks) return MMSKV_EUNSUPPORTED;
     rc = check_rows(q, q_strides, 2, true);
     if (rc) return rc;
     rc = check_rows(k, k_strides, 2, true);
@@ -1067,6 +1070,8 @@ int mmshiftkv_prompt_attention(const mmskv_shape* shape, const uint16_t* q, cons
     if (rc) return rc;
     rc = check_out_rows(out, out_strides, 2, shape->B, shape->Hq, shape->T);
     if (rc) return rc;
+    // (seven rows fit offsets of 32 bits)
+    if (shape->T > 1 && (k_strides->st >= (1 << 28) || v_strides->st >= (1 << 28))) return MMSKV_EUNSUPPORTED;
     PromptArgs a = {};
     a.q = q;
     a.k = k;
@@ -1077,10 +1082,10 @@ int mmshiftkv_prompt_attention(const mmskv_shape* shape, const uint16_t* q, cons
     a.qst = q_strides->st;
     a.ksb = k_strides->sb;
     a.ksh = k_strides->sh;
-    a.kst = k_strides->st;
+    a.kst = shape->T > 1 ? k_strides->st : 0;
     a.vsb = v_strides->sb;
     a.vsh = v_strides->sh;
-    a.vst = v_strides->st;
+    a.vst = shape->T > 1 ? v_strides->st : 0;
     a.osb = out_strides->sb;
     a.osh = out_strides->sh;
     a.ost = out_strides->st;
@@ -1112,7 +1117,9 @@ int check_groups(const mmskv_shape* s, int32_t groups, int32_t n) {
     const int rc = check_chunk(s, n);
     if (rc) return rc;
     if (groups < 1 || s->B % groups != 0) return MMSKV_EINVAL;
-    if (static_cast<int64_t>(s->B / groups) * (s->Hq / s->Hkv) * n > (1 << 22)) return MMSKV_EUNSUPPORTED;
+    const int64_t own = static_cast<int64_t>(s->Hq / s->Hkv) * n, shared = s->B / groups * own;
+    if (shared > (1 << 22) || static_cast<int64_t>(s->B) * s->Hq * n > (1 << 26)) return MMSKV_EUNSUPPORTED;
+    if (s->Hkv * (groups * ((shared + 127) / 128) + s->B * ((own + 127) / 128)) > kMaxBlocks) return MMSKV_EUNSUPPORTED;
     return MMSKV_OK;
 }
 

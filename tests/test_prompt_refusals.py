@@ -28,7 +28,9 @@ def call(lib, B=1, Hq=4, Hkv=2, T=100, d=64, q=FAKE, k=FAKE, v=FAKE, out=FAKE, q
     (dict(os=bd.Strides(64, 0, 64)), bd.MMSKV_EINVAL), (dict(os=bd.Strides(64, 64, 0)), bd.MMSKV_EINVAL),
     (dict(causal=2), bd.MMSKV_EINVAL), (dict(B=2), bd.MMSKV_EINVAL), (dict(n_seq=0), bd.MMSKV_EINVAL),
     (dict(starts=BAD4), bd.MMSKV_EINVAL), (dict(lse=BAD4), bd.MMSKV_EINVAL),
-    (dict(T=1 << 22), bd.MMSKV_EUNSUPPORTED), (dict(B=65535, Hq=129, Hkv=129, starts=None), bd.MMSKV_EUNSUPPORTED)])
+    (dict(T=1 << 22), bd.MMSKV_EUNSUPPORTED), (dict(ks=bd.Strides(0, 0, 1 << 28)), bd.MMSKV_EUNSUPPORTED),
+    (dict(vs=bd.Strides(0, 0, 1 << 30)), bd.MMSKV_EUNSUPPORTED),
+    (dict(B=1000, T=1 << 20, Hq=2, starts=None), bd.MMSKV_EUNSUPPORTED), (dict(B=65535, Hq=129, Hkv=129, starts=None), bd.MMSKV_EUNSUPPORTED)])
 def test_refusals(lib, bad, code):  # noqa: F811
     assert call(lib, **bad) == code
 

@@ -35,6 +35,8 @@ def call(lib, s=None, p=None, q=FAKE, qs=ST, q_counts=None, lens=FAKE, shared=FA
     (dict(out=None), bd.MMSKV_EINVAL), (dict(out=ODD), bd.MMSKV_EINVAL),
     (dict(os=bd.Strides(64, 64, 0)), bd.MMSKV_EINVAL), (dict(n=1 << 19), bd.MMSKV_EUNSUPPORTED),
     (dict(s=shape(B=65535, Hq=129, Hkv=129), groups=1), bd.MMSKV_EUNSUPPORTED),
+    (dict(s=shape(B=60000, Hq=140, Hkv=70), groups=60000, n=1), bd.MMSKV_EUNSUPPORTED),
+    (dict(s=shape(B=60000, Hq=28, Hkv=1), groups=60000, n=41), bd.MMSKV_EUNSUPPORTED),
     (dict(ws=None), bd.MMSKV_EWORKSPACE), (dict(ws=ODD), bd.MMSKV_EWORKSPACE)])
 def test_refusals(lib, bad, code):  # noqa: F811
     assert call(lib, **bad) == code

@@ -231,6 +231,7 @@ struct PromptArgs {
     int rows;                  // Gh * T query rows of a KV head, row i * Gh + g: token i of its head g
     float scale;               // log2(e) / sqrt(d)
     bool by_head;              // the launch's order of workgroups, by head or by row tile
+    bool cut;                  // two workgroups for a row tile, the first half of them behind its cut
 };
 
 // Changes of the pages that sequences hold.

@@ -183,6 +183,27 @@ def test_as_in_fp32(d, Hq, Hkv, T, causal):
         assert float((lse[0, h] - torch.logsumexp(x, -1)).abs().max()) <= rel + 2.0 ** -22 * (size + 40)
 
 
+@pytest.mark.parametrize("d,Hq,Hkv", [(64, 4, 4), (128, 7, 1), (64, 2, 2)])
+@pytest.mark.parametrize("cuts", [[0, 700, 1500], [3, 900, 1111, 1112, 1130, 1490], [0, 600, 1210, 1500], [100, 1400],
+                                  [0, 1, 1499, 1500]])
+def test_long_packed_sequences(d, Hq, Hkv, cuts):
+    """Sequences that end within a row tile beside long ones, whose rows other workgroups may have."""
+    T = 1500
+    q, k, v = inputs(1, Hq, Hkv, T, d, len(cuts) + d, "tokens")
+    for causal in (True, False):
+        out = torch.full_like(q, 7.0)
+        lse = torch.full((1, Hq, T), 7.0, device=DEV)
+        mm.prompt_attention(q, k, v, starts=int32(cuts[:2] + cuts[1:]), causal=causal, out=out, lse=lse)
+        check(out, q, k, v, cuts, causal, lse)
+        inside = torch.zeros(T, dtype=torch.bool, device=DEV)
+        inside[cuts[0]:cuts[-1]] = True
+        assert bool((out[:, :, ~inside] == 7.0).all()) and bool((lse[:, :, ~inside] == 7.0).all())
+        # (fewer sequences on average: two workgroups for a row tile)
+        if len(cuts) <= 3:
+            again = mm.prompt_attention(q, k, v, starts=int32(cuts), causal=causal)
+            check(again, q, k, v, cuts, causal)
+
+
 def test_rows_behind_four_gib():
     """Strides that put the last tokens past 4 GiB."""
     T, H, d = 70, 2, 64

@@ -82,20 +82,24 @@ __device__ __forceinline__ int staged(int r, int ch) {
     return r * (2 * D) + 16 * (ch ^ swz);
 }
 
-// What a workgroup works on: all rows that a sequence sees (PARTS = false); or one of the
+// What a workgroup works on: all rows that a sequence sees (PARTS = kNoParts); or one of the
 // two parts of an attention over a shared prefix, of which it leaves partial sums: the
 // rows that the sequences of a group share, for the queries of all of them (b is the
 // group, pages.table the groups' and row r = (s * n + i) * Gh + g query i of the group's
 // sequence s), or those behind the shared ones.
-template <bool PARTS>
+// (kShared: a launch of the first part alone, kBoth: of either or both)
+constexpr int kNoParts = 0, kShared = 1, kBoth = 2;
 struct Work {
     ChunkArgs a;
     bool shared;                           // which part
     int bc, slot, slots;                   // (b, c), and the place among the workgroups of it
 };
-template <bool PARTS, class ARGS>
-__device__ __forceinline__ Work<PARTS> work_of(const ARGS& all) {
-    if constexpr (PARTS) {
+template <int PARTS, class ARGS>
+__device__ __forceinline__ Work work_of(const ARGS& all) {
+    if constexpr (PARTS == kShared) {
+        const int heads = all.shared.B * all.shared.Hkv, slot = blockIdx.x / heads;
+        return {all.shared, true, static_cast<int>(blockIdx.x) - slot * heads, slot, static_cast<int>(gridDim.x) / heads};
+    } else if constexpr (PARTS == kBoth) {
         const bool shared = static_cast<int>(blockIdx.x) < all.first_own;
         const ChunkArgs a = shared ? all.shared : all.own;
         const int x = blockIdx.x - (shared ? 0 : all.first_own), heads = a.B * a.Hkv, slot = x / heads;
@@ -132,11 +136,11 @@ __device__ __forceinline__ int last_shared(const ChunkArgs& a, const Query& q, i
     return min(a.causal ? len - nq + q.i : len - 1, shared - 1);
 }
 
-template <int D, int TYPE, bool PARTS = false, class ARGS = ChunkArgs>
+template <int D, int TYPE, int PARTS = kNoParts, class ARGS = ChunkArgs>
 __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
-    const Work<PARTS> job = work_of<PARTS>(all);
+    const Work job = work_of<PARTS>(all);
     const ChunkArgs& a = job.a;
-    const bool shared = PARTS && job.shared;
+    const bool shared = PARTS == kShared || (PARTS == kBoth && job.shared);
     constexpr int KC = D / 16;             // 16-dim steps of S
     constexpr int NT = D / 32;             // 32-dim tiles of O
     constexpr int kRow = D * kCacheBytes<TYPE>;      // bytes of a cached row
@@ -164,8 +168,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
     const int nq = queries_of(a, qr.b);
     const bool there = r < a.rows && i < nq;
     int last, all_see, end, low = 0;
-    __shared__ int most[PARTS ? 2 : 1][kWaves];
-    if (PARTS && shared) {
+    __shared__ int most[PARTS != kNoParts ? 2 : 1][kWaves];
+    if (shared) {
         // keys that all rows of the workgroup see, and that some row sees
         const int rows = shared_rows(a, b, c);
         last = there ? last_shared(a, qr, c, nq, rows) : -1;
@@ -184,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
         // keys that the workgroup's rows see together
         const int i_end = min((min(r0 + kRows, a.rows) - 1) / a.Gh, nq - 1);
         end = i_end < r0 / a.Gh ? 0 : max(a.causal ? len - nq + i_end + 1 : len, 0);
-        if (PARTS) low = shared_rows(a, b / a.each, c);        // the first key
+        if (PARTS == kBoth) low = shared_rows(a, b / a.each, c);       // the first key
     }
     // this split's tiles
     const int tiles0 = low / kKeys, tiles = max((end + kKeys - 1) / kKeys, tiles0);
@@ -278,11 +282,11 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
     // Rows of V behind the last key (and before the first) may hold anything: zeros, for p = 0 to meet
     // (their logits are masked).  By the wave that staged them.
     auto clear_tail = [&](int tile, int buf) {
-        if ((tile + 1) * kKeys <= end && (!PARTS || tile * kKeys >= low)) return;
+        if ((tile + 1) * kKeys <= end && (PARTS != kBoth || tile * kKeys >= low)) return;
         constexpr int kOut = 2 * D / 16;
         for (int x = lane; x < kWaveRows * kOut; x += kWave) {
             const int row = kWaveRows * wave + x / kOut;
-            if (tile * kKeys + row < end && (!PARTS || tile * kKeys + row >= low)) continue;
+            if (tile * kKeys + row < end && (PARTS != kBoth || tile * kKeys + row >= low)) continue;
             *reinterpret_cast<u32x4*>(vt[buf] + row * 2 * D + 16 * (x % kOut)) = u32x4{0u, 0u, 0u, 0u};
             if (kScaled) vsc[buf][row] = 0.f;
         }
@@ -357,8 +361,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
         // logit e of half u, scaled; a masked one is -inf whatever its row's scale
         auto logit = [&](int u, int e, float less) {
             float x = fmaf(s[u][e], kScaled ? kw[e >> 2][e & 3] : scale, -less);
-            if (MASKED && !PARTS) x = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? x : -INFINITY;
-            if (MASKED && PARTS) x = from + (32 * u + 8 * (e >> 2) + (e & 3)) < seen ? x : -INFINITY;
+            if (MASKED && PARTS != kBoth) x = 32 * u + 8 * (e >> 2) + (e & 3) <= rel ? x : -INFINITY;
+            if (MASKED && PARTS == kBoth) x = from + (32 * u + 8 * (e >> 2) + (e & 3)) < seen ? x : -INFINITY;
             return x;
         };
         // p of values 2 j, 2 j + 1 of half u relative to m, as bf16; their sum
@@ -482,14 +486,14 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
         ++tile, buf ^= 1;
     };
     const int whole = min(max(all_see, 0) / kKeys, tile1);
-    if constexpr (PARTS) {
+    if constexpr (PARTS != kNoParts) {
         if (!__any(there)) {               // a wave without rows stages its part of the tiles
             while (tile < tile1) step(Constant<2>{});
             if (half == 0 && r < a.rows)   // (rows that are not there: no weight, whatever their sums hold)
                 a.part_ml[(static_cast<int64_t>(split) * (a.B * a.Hkv) + bc) * a.rows + r] = make_float2(kNone, 0.f);
             return;
         }
-        if (tile < tile1 && tile * kKeys < low) step(Constant<1>{});
+        if (PARTS == kBoth && tile < tile1 && tile * kKeys < low) step(Constant<1>{});
     }
     while (tile < whole) step(Constant<0>{});
     while (tile < tile1) step(Constant<1>{});
@@ -497,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
     if (r >= a.rows) return;
     if (!there) l = 0.f;                   // (took part where nothing is masked)
     // value 4 w + j of o[t] is dim 32 t + 8 w + 4 half + j
-    if (PARTS || a.splits > 1) {
+    if (PARTS != kNoParts || a.splits > 1) {
         const int64_t pr = (static_cast<int64_t>(split) * (a.B * a.Hkv) + bc) * a.rows + r;
         float* po = a.part_o + pr * D + 4 * half;
 #pragma unroll
@@ -617,12 +621,42 @@ __device__ __forceinline__ void load_group(const char* src, char* dst, int row0,
     if constexpr (J + 1 < LOADS) load_group<T, J + 1, LOADS>(src, dst, row0, ld_row, lane, any);
 }
 
+constexpr int kJoinPer = 8;                // splits of a row whose loads are on their way at once
+// kJoinPer splits more of a row's eight dims: their places v, x, y, of which those from
+// `n` on are none.
+struct RowSum {
+    float m = kNone, l = 0.f, o[8] = {};
+};
+__device__ __forceinline__ void add_splits(RowSum& r, float2 (&v)[kJoinPer], const float4 (&x)[kJoinPer],
+                                           const float4 (&y)[kJoinPer], int n) {
+    float mx = r.m;
+#pragma unroll
+    for (int j = 0; j < kJoinPer; ++j) {
+        if (j >= n) v[j] = make_float2(kNone, 0.f);
+        mx = fmaxf(mx, v[j].x);
+    }
+    const float f0 = fast_exp2(r.m - mx);
+    r.m = mx;
+    r.l *= f0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.o[e] *= f0;
+#pragma unroll
+    for (int j = 0; j < kJoinPer; ++j) {
+        const bool any = v[j].y != 0.f;    // a split that saw no key leaves m only (a NaN sum is kept)
+        const float f = any ? fast_exp2(v[j].x - r.m) : 0.f;
+        const float z[8] = {x[j].x, x[j].y, x[j].z, x[j].w, y[j].x, y[j].y, y[j].z, y[j].w};
+        r.l = fmaf(v[j].y, f, r.l);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.o[e] = fmaf(any ? z[e] : 0.f, f, r.o[e]);
+    }
+}
+
 // Workgroup: WAVES waves; (b, c) and a split of its keys.
-template <int D, int TYPE, int NR, int WAVES, bool PARTS = false, class ARGS = ChunkArgs>
+template <int D, int TYPE, int NR, int WAVES, int PARTS = kNoParts, class ARGS = ChunkArgs>
 __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
-    const Work<PARTS> job = work_of<PARTS>(all);
+    const Work job = work_of<PARTS>(all);
     const ChunkArgs& a = job.a;
-    const bool shared = PARTS && job.shared;
+    const bool shared = PARTS == kShared || (PARTS == kBoth && job.shared);
     using T = FewTile<D, TYPE, WAVES>;
     constexpr int kWaves = WAVES, kThreads = 64 * WAVES;
     constexpr int KC = D / 32;             // 32-dim steps of S
@@ -994,6 +1028,38 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
             for (int e = 0; e < 4; ++e) x[e] = fmaf(y0[e], f, x[e]), x[4 + e] = fmaf(y1[e], f, x[4 + e]);
         }
         if (i >= (shared ? queries_of(a, qr.b) : nq)) L = 0.f;    // (a row that is not there took part where nothing is masked)
+        if constexpr (PARTS != kNoParts) {
+            if (a.joins) {                 // the only split of own rows: the shared ones' sums to its own
+                const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;
+                const int grp = b / a.each;
+                const int64_t rd = ((static_cast<int64_t>(grp) * a.Hkv + c) * a.each + (b - grp * a.each)) * a.rows + r;
+                RowSum sum;
+                if (L != 0.f) {
+                    sum.m = M, sum.l = L;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum.o[e] = x[e];
+                }
+                for (int s0 = 0; s0 < all.shared.splits; s0 += kJoinPer) {
+                    float2 v[kJoinPer];
+                    float4 y0[kJoinPer], y1[kJoinPer];
+#pragma unroll
+                    for (int j = 0; j < kJoinPer; ++j) {
+                        const int64_t at = min(s0 + j, all.shared.splits - 1) * rows + rd;
+                        const float* po = all.shared.part_o + at * D + d0;
+                        v[j] = all.shared.part_ml[at];
+                        y0[j] = *reinterpret_cast<const float4*>(po);
+                        y1[j] = *reinterpret_cast<const float4*>(po + 4);
+                    }
+                    add_splits(sum, v, y0, y1, all.shared.splits - s0);
+                }
+                const float inv = sum.l != 0.f ? 1.f / sum.l : 0.f;
+                u32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = pack_bf16(sum.o[2 * j] * inv, sum.o[2 * j + 1] * inv);
+                *reinterpret_cast<u32x4*>(a.out + b * a.osb + (c * a.Gh + qr.g) * a.osh + i * a.ost + d0) = v;
+                continue;
+            }
+        }
         if (PARTS || a.splits > 1) {
             const int64_t pr = (static_cast<int64_t>(split) * (a.B * a.Hkv) + bc) * a.rows + r;
             float* po = a.part_o + pr * D + d0;
@@ -1018,7 +1084,6 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
 // splits at a time, no branch between them) are on their way before the first
 // is needed: a loop that waited for each split took 0.8 us a split.
 constexpr int kJoinThreads = 256;
-constexpr int kJoinPer = 8;
 
 // PARTS: the first a.shared_splits splits are of the rows that the sequences of a group
 // share, in whose order of rows they lie.
@@ -1038,7 +1103,9 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
         const int grp = b / a.each, s = b - grp * a.each;
         rd_shared = ((static_cast<int64_t>(grp) * a.Hkv + c) * a.each + s) * a.rows + (rd - bc * a.rows);
     }
-    float m = kNone, l = 0.f, o[8] = {};
+    RowSum sum;
+    float (&o)[8] = sum.o;
+    float &m = sum.m, &l = sum.l;
     for (int s0 = g; s0 < a.splits; s0 += SG * kJoinPer) {
         float2 v[kJoinPer];
         float4 x[kJoinPer], y[kJoinPer];
@@ -1051,26 +1118,7 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(ChunkArgs a) {
             x[j] = *reinterpret_cast<const float4*>(po);
             y[j] = *reinterpret_cast<const float4*>(po + 4);
         }
-        float mx = m;
-#pragma unroll
-        for (int j = 0; j < kJoinPer; ++j) {
-            if (s0 + j * SG >= a.splits) v[j] = make_float2(kNone, 0.f);
-            mx = fmaxf(mx, v[j].x);
-        }
-        const float f0 = fast_exp2(m - mx);
-        m = mx;
-        l *= f0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] *= f0;
-#pragma unroll
-        for (int j = 0; j < kJoinPer; ++j) {
-            const bool any = v[j].y != 0.f;            // a split that saw no key leaves m only (a NaN sum is kept)
-            const float f = any ? fast_exp2(v[j].x - m) : 0.f;
-            const float z[8] = {x[j].x, x[j].y, x[j].z, x[j].w, y[j].x, y[j].y, y[j].z, y[j].w};
-            l = fmaf(v[j].y, f, l);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf(any ? z[e] : 0.f, f, o[e]);
-        }
+        add_splits(sum, v, x, y, (a.splits - s0 + SG - 1) / SG);
     }
     if constexpr (SG > 1) {
 #pragma unroll
@@ -1148,14 +1196,15 @@ void attend_parts(const ChunkArgs& shared, const ChunkArgs& own, bool do_shared,
     const dim3 grid(static_cast<unsigned>(first + (do_own ? part_blocks(own, few) : 0)));
     const PartsArgs p{shared, own, static_cast<int>(first)};
     if (!few) {
-        hipLaunchKernelGGL((chunk_kernel<D, TYPE, true, PartsArgs>), grid, dim3(kThreads), 0, s, p);
+        if (do_own) hipLaunchKernelGGL((chunk_kernel<D, TYPE, kBoth, PartsArgs>), grid, dim3(kThreads), 0, s, p);
+        else hipLaunchKernelGGL((chunk_kernel<D, TYPE, kShared, PartsArgs>), grid, dim3(kThreads), 0, s, p);
         return;
     }
     const int rows = do_shared ? shared.rows : own.rows;   // (those of a group are at least a sequence's)
     constexpr int W = few_waves(D, TYPE, 1);
-    if (rows <= 16) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 1, W, true, PartsArgs>), grid, dim3(64 * W), 0, s, p);
-    else if (rows <= 32) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 2, W, true, PartsArgs>), grid, dim3(64 * W), 0, s, p);
-    else hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 4, 4, true, PartsArgs>), grid, dim3(kThreads), 0, s, p);
+    if (rows <= 16) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 1, W, kBoth, PartsArgs>), grid, dim3(64 * W), 0, s, p);
+    else if (rows <= 32) hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 2, W, kBoth, PartsArgs>), grid, dim3(64 * W), 0, s, p);
+    else hipLaunchKernelGGL((chunk_few_kernel<D, TYPE, 4, 4, kBoth, PartsArgs>), grid, dim3(kThreads), 0, s, p);
 }
 
 template <int D, bool PARTS = false>
@@ -1198,7 +1247,7 @@ hipError_t launch_parts(const ChunkArgs& shared, const ChunkArgs& own, hipStream
         e = attend_type(true, false, shared.rows <= kFewRows);
         if (e == hipSuccess) e = attend_type(false, true, own.rows <= kFewRows);
     }
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || own.joins) return e;
     ChunkArgs a = own;
     a.part_o = shared.part_o;
     a.part_ml = shared.part_ml;
@@ -1288,6 +1337,9 @@ void plan_parts(ChunkArgs* shared, ChunkArgs* own) {
     own->splits = splits(*own, mine, few);
     own->one_launch = one_launch(*shared, *own);
     if (!own->one_launch) own->splits = splits(*own, mine, own->rows <= kFewRows);
+    // (64 tokens over 32768 shared rows and up to 600 own ones: 114 us, with a launch that
+    // joins 123)
+    own->joins = !own->one_launch && own->rows <= kFewRows && own->splits == 1;
 }
 
 size_t chunk_workspace_bound(int64_t heads, int rows, int T, int d) {

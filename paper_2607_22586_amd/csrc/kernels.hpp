@@ -214,6 +214,7 @@ struct ChunkArgs {
     int shared_max;            // upper bound of shared
     int shared_splits;         // in the join: splits of the shared rows among a.splits
     bool one_launch;           // own rows: in one launch with the shared ones
+    bool joins;                // own rows: their only split adds the shared sums and writes the result
 };
 int chunk_splits(int64_t heads, int rows, int T, int d, int dtype);
 // Workspace bytes that suffice for every plan of a problem and never fall as

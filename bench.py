@@ -394,11 +394,13 @@ PAGED_CHUNK = 1024            # tokens of a prompt's last chunk in the --paged m
 
 
 def paged_bench(args):
-    """A layer's prompt in a paged cache, as a serving program has it: its rows
-    written (and quantised), the attention of its last chunk, the rows read back
-    for the selection, the kept rows written to a small cache, then K steps of
+    """A layer's prompt in a paged cache, as a serving program has it: its attention over
+    itself, its rows written (and quantised), the attention of its last chunk, the rows
+    read back for the selection, the kept rows written to a small cache, then K steps of
     decoding (a captured graph), each a token's row written and its attention over
-    the kept rows; beside it the attention of one token over the whole prompt.  One JSON line:
+    the kept rows; beside it the attention of one token over the whole prompt.  With
+    --answers N the kept rows are forked into N sequences that share them, and each
+    step decodes a token of every answer.  One JSON line:
     decoded tokens per second over all layers, and each call's time."""
     import torch
     from paper_2607_22586_amd import binding as bd
@@ -411,14 +413,18 @@ def paged_bench(args):
     dtype = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}[args.paged]
     n = min(PAGED_CHUNK, T)
     new = args.warmup + args.steps                 # decoded tokens
+    N = args.answers
     log("generating %d layers of %s" % (L, w.name))
     layers = [wl.make_layer(w, l, device=dev) for l in range(L)]
     gen = torch.Generator(device=dev).manual_seed(w.wid)
     full = torch.full((B, Hkv), T, dtype=torch.int32, device=dev)
     prompt = bd.PagedCache.empty(B, Hkv, T, d, dtype, device=dev)
     q = torch.randn((B, n, Hq, d), generator=gen, device=dev).bfloat16().transpose(1, 2)
-    ws = torch.empty(max(bd.chunk_attention_workspace(B, Hq, Hkv, T, d, x) for x in (1, n)), dtype=torch.uint8,
+    ws = torch.empty(max([bd.chunk_attention_workspace(B, Hq, Hkv, T, d, x) for x in (1, n)]
+                         + [bd.shared_attention_workspace(B * N, Hq, Hkv, w.budget + new, d, 1, B)]), dtype=torch.uint8,
                      device=dev)
+    q_all = torch.randn((B, T, Hq, d), generator=gen, device=dev).bfloat16().transpose(1, 2)
+    o_all = torch.empty_like(q_all)
     eb, cb = layers[0]["k"].element_size(), prompt.k.element_size()
     row = 2 * (d * cb + (0 if cb == 2 else 4))     # bytes of a cached row of K and V
     calls = {}                                     # name: (times, bytes, flops)
@@ -431,8 +437,11 @@ def paged_bench(args):
         calls.setdefault(name, ([], nbytes, flops))[0].append((e0, e1))
         return r
 
-    kept, lens = [], []
+    kept, lens, shared = [], [], []
     for l, x in enumerate(layers):
+        if eb == 2:
+            timed("prompt_attention", 4 * B * T * d * (Hq + Hkv), 2 * d * B * Hq * T * (T + 1),
+                  lambda: bd.prompt_attention(q_all, x["k"], x["v"], out=o_all))
         timed("write_prompt", B * Hkv * T * (2 * d * eb + row), 0, lambda: bd.cache_write(prompt, x["k"], x["v"]))
         seen = n * (T - n) + n * (n + 1) // 2
         timed("chunk_attention", B * (Hkv * T * row + 4 * Hq * n * d), 4 * d * B * Hq * seen,
@@ -441,21 +450,42 @@ def paged_bench(args):
               lambda: bd.chunk_attention(q[:, :, -1:], prompt, full, T=T, workspace=ws))
         k, v = timed("read_prompt", B * Hkv * T * (4 * d + row), 0, lambda: bd.cache_read(prompt, full, T))
         sel = bd.select_layer(x["q_win"], k, v, w.budget, bd.SelectionConfig(seed=w.wid, layer=l)).sel
-        cache = bd.PagedCache.empty(B, Hkv, w.budget + new, d, dtype, device=dev)
+        ln = sel.counts.clone()
+        if N == 1:
+            cache = prompts = bd.PagedCache.empty(B, Hkv, w.budget + new, d, dtype, device=dev)
+        else:
+            # the prompts' kept rows in the first sequence of each group, its pages known by its number of rows
+            most = -(-(w.budget + new) // 64) + 1
+            cache = bd.PagedCache.pool(B * N, Hkv, B * N * most, most, d, dtype, device=dev)
+            rows = torch.zeros((B, N, Hkv), dtype=torch.int32, device=dev)
+            rows[:, 0] = ln
+            ln = rows.view(B * N, Hkv)
+            timed("hold", 4 * (2 * B * N * most + B * N * most), 0, lambda: bd.cache_hold(cache, ln))
+            prompts = bd.PagedCache(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.table[::N].contiguous())
         timed("write_kept", B * Hkv * w.budget * (4 * d + row + 4), 0,
-              lambda: bd.cache_write(cache, k, v, counts=sel.counts, idx=sel.idx))
+              lambda: bd.cache_write(prompts, k, v, counts=sel.counts, idx=sel.idx))
+        if N > 1:
+            src = torch.arange(0, B * N, N, dtype=torch.int32, device=dev).repeat_interleave(N)
+            timed("fork", 4 * (2 * B * N * most + B * N * most), 0, lambda: bd.cache_fork(cache, src, ln))
+            bd.cache_hold(cache, ln + new)         # pages for all tokens to come
+            shared.append(sel.counts)
         kept.append(cache)
-        lens.append(sel.counts.clone())
+        lens.append(ln)
         x.clear()
-    kn, vn = (torch.randn((B, 1, Hkv, d), generator=gen, device=dev).bfloat16().transpose(1, 2) for _ in range(2))
-    q1 = q[:, :, :1].contiguous()
+    kn, vn = (torch.randn((B * N, 1, Hkv, d), generator=gen, device=dev).bfloat16().transpose(1, 2) for _ in range(2))
+    q1 = q[:, :, :1].repeat_interleave(N, 0).contiguous()
     out = torch.empty_like(q1)
+    firsts = [cache.table[::N].contiguous() for cache in kept]
 
     def step():
-        for cache, ln in zip(kept, lens):
+        for l, (cache, ln) in enumerate(zip(kept, lens)):
             bd.cache_write(cache, kn, vn, start=ln)
             ln.add_(1)
-            bd.chunk_attention(q1, cache, ln, T=w.budget + new, workspace=ws, out=out)
+            if N == 1:
+                bd.chunk_attention(q1, cache, ln, T=w.budget + new, workspace=ws, out=out)
+            else:
+                bd.shared_attention(q1, cache, ln, shared[l], firsts[l], T=w.budget + new, shared_T=w.budget,
+                                    workspace=ws, out=out)
 
     # launch-bound (three short launches a layer): captured once, replayed for every token
     warm = torch.cuda.Stream(dev)
@@ -477,12 +507,12 @@ def paged_bench(args):
     ms_step = t0.elapsed_time(t1) / args.steps
     us = {k: sorted(a.elapsed_time(b) * 1e3 for a, b in ev)[len(ev) // 2] for k, (ev, _, _) in calls.items()}
     print(json.dumps({
-        "metric": "tokens decoded/sec on kept rows in pages", "value": B / (ms_step * 1e-3), "unit": "tokens/s",
+        "metric": "tokens decoded/sec on kept rows in pages", "value": B * N / (ms_step * 1e-3), "unit": "tokens/s",
         "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": ms_step,
         "us_per_layer": ms_step * 1e3 / L, "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
         "dtype": args.paged, "data": "synthetic",
         "config": {"workload": w.name, "layers": L, "batch": B, "T": T, "Hq": Hq, "Hkv": Hkv, "d": d,
-                   "budget": w.budget, "chunk": n, "page": prompt.k.shape[2]},
+                   "budget": w.budget, "chunk": n, "page": prompt.k.shape[2], "answers": N},
         "calls": {k: {"us": us[k], "GB/s": calls[k][1] / us[k] / 1e3, "TFLOP/s": calls[k][2] / us[k] / 1e6}
                   for k in us},
         "calls_timing": "median over the layers of events around one call",
@@ -515,6 +545,8 @@ def main():
     ap.add_argument("--paged", choices=["bf16", "e4m3", "int8"],
                     help="time a prompt in a paged cache of that type instead: its rows written and read back, "
                          "the attention of its last chunk, decoding on the kept rows")
+    ap.add_argument("--answers", type=int, default=1, metavar="N",
+                    help="with --paged: N answers to each prompt, which share its kept rows")
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="only run a 1 GiB device copy (counter calibration)")
     args = ap.parse_args()
@@ -535,6 +567,8 @@ def main():
     if args.hidden:
         hidden_bench(args)
         return
+    if args.answers < 1 or (args.answers > 1 and not args.paged):
+        ap.error("--answers N >= 1 goes with --paged")
     if args.paged:
         paged_bench(args)
         return

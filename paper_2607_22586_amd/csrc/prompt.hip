@@ -528,15 +528,16 @@ hipError_t launch_prompt_attention(const PromptArgs& args, hipStream_t s) {
     // Eight waves fetch a tile for twice the rows, which at d = 128 lets the matrix pipe
     // run at a higher clock (4 x 28 heads of 16384 tokens 7.3 -> 7.1 ms); four have twice
     // the workgroups, and less beside the diagonal (of 2048 tokens 149 us against 157).
-    // At d = 64 and with at most one workgroup a CU, twice or four times the waves with
-    // keys of their own shorten what each does in turn by more than the join takes, from
-    // some 512 tokens on (16 heads on 2, groups / none: 256 tokens 8.2 / 7.9 us, 512 9.9 /
-    // 11.4, 1024 13.2 / 19.9, 2048 28 / 34; at d = 128 28 heads on 4 of 1024 24.7 / 26,
-    // of 512 16.1 / 15.9).
+    // At d = 64 and with few workgroups, waves with keys of their own shorten what each
+    // does in turn by more than the join takes (16 heads on 2, four groups / none: 512
+    // tokens 9.9 / 11.4 us, 1024 13.2 / 19.9; two groups of eight waves, 2048 28 / 34; of
+    // four, 256 7.2 / 8.1, 64 6.0 / 5.5; 8 heads, 23 sequences in 3001 tokens 13.3 / 15.4;
+    // at d = 128 28 heads on 4 of 1024 24.7 / 26, of 512 16.1 / 15.9).
     if (a.d == 64) {
-        const bool deep = mean >= 512;
-        if (deep && workgroups(64) <= kPlanCus) run(Constant<64>{}, Constant<8>{}, Constant<4>{});
-        else if (deep && workgroups(128) <= kPlanCus) run(Constant<64>{}, Constant<8>{}, Constant<2>{});
+        const int64_t wide = workgroups(128), narrow = workgroups(64);
+        if (mean >= 512 && narrow <= kPlanCus) run(Constant<64>{}, Constant<8>{}, Constant<4>{});
+        else if (mean >= 512 && wide <= kPlanCus) run(Constant<64>{}, Constant<8>{}, Constant<2>{});
+        else if (mean >= 96 && narrow <= 2 * kPlanCus) run(Constant<64>{}, Constant<4>{}, Constant<2>{});
         else run(Constant<64>{}, Constant<4>{}, Constant<1>{});
     } else {
         if (a.by_head) run(Constant<128>{}, Constant<8>{}, Constant<1>{});

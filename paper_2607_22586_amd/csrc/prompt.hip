@@ -1,11 +1,11 @@
 // Attention of whole prompts over themselves on gfx950 (mmshiftkv_prompt_attention).
 //
 // The Gh heads that share a KV head are rows of one problem: row r = i * Gh + g is
-// token i of head g, so that a workgroup's 128 rows (4 waves of 32) span few tokens
-// and its keys end soon behind its own.  It walks the keys from the start of its
-// first token's sequence in tiles of 64, staged in LDS for all waves by
-// loads straight to it (the next tile's are on their way while one is worked on).  One
-// pass with the running reference m and sum l of the softmax, base 2:
+// token i of head g, so that a workgroup's 128 rows (4 waves of 32; 256 where sequences
+// are long) span few tokens and its keys end soon behind its own.  It walks the keys
+// from the start of its first token's sequence in tiles of 64, staged in LDS for all
+// waves by loads straight to it (the next tile's are on their way while one is worked
+// on).  One pass with the running reference m and sum l of the softmax, base 2:
 //   S^T = K Q^T   (v_mfma_f32_32x32x16_bf16: lane = query row, its values = keys,
 //                  so the softmax runs within a lane and its other half-wave)
 //   O^T = O^T 2^(m_old - m) + V^T P^T
@@ -14,6 +14,14 @@
 // Packed sequences need no plan: a row tile that spans several of them walks the
 // keys of all, each row masked to [its sequence's start, its end), both found by
 // counting the starts at or before a token.
+// What bounds it: at d = 128 the matrix pipe, busy for 53 to 56% of the cycles, beside
+// the vector pipe's 57%, at the 1.77 to 1.9 GHz that the chip holds under both (4 x 28
+// heads of 16384 tokens on 4, causal: 6.9 to 7.2 ms, 1070 to 1119 TFLOP/s, box to box; a
+// bf16 product of 8192^3 reaches 1219 to 1389); fewer vector instructions alone change
+// nothing, fewer reads of the tiles do.  At d = 64 the vector pipe: as many exponentials
+// for half the products (4 x 16 heads of 8192 tokens 890 to 910 TFLOP/s).  Short
+// sequences: a chain of latencies, 5 us for one token, 1.2 us more for every tile of 64
+// keys at d = 128 and 0.9 at 64.
 #include "pages.hpp"
 
 namespace mmskv {
@@ -46,7 +54,8 @@ __device__ __forceinline__ float half_sum(float x) {
 }
 
 // sum + the two bf16 values of y, by one instruction (DOT) or two additions: the vector
-// pipe bounds d = 64, at d = 128 the additions let the clock be higher.
+// pipe bounds d = 64 (images of 16 heads 203 -> 195 us by the instruction), at d = 128 the
+// additions let the clock be higher (7.26 against 7.36 ms).
 template <bool DOT>
 __device__ __forceinline__ float add_pair(uint32_t y, float sum) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

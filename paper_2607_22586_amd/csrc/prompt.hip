@@ -137,14 +137,25 @@ __global__ void __launch_bounds__(64 * WAVES, 2) prompt_kernel(PromptArgs a) {
     if (a.starts) {
         if (tid < kWords) begins[tid] = 0;
         if (tid < 3) edge[tid] = tid == 1 ? a.T : tid == 0 ? -1 : 0;
-        __syncthreads();
-        for (int s = tid; s <= a.n_seq; s += kThreads) {
-            const int t = min(max(a.starts[s], 0), a.T);
+        const auto start = [&](int s) { return min(max(a.starts[s], 0), a.T); };
+        // of many starts those between the last of kThreads samples at or before the tile
+        // and the first behind it (they ascend)
+        int s0 = 0, s1 = a.n_seq;
+        if (a.n_seq >= 4 * kThreads) {
+            const int step = a.n_seq / kThreads + 1, t = start(min(tid * step, a.n_seq));
+            const int before = __syncthreads_count(t <= i0), upto = __syncthreads_count(t <= i1);
+            s0 = max(before - 1, 0) * step;
+            if (upto < kThreads) s1 = min(upto * step, a.n_seq);
+        } else {
+            __syncthreads();
+        }
+        for (int s = s0 + tid; s <= s1; s += kThreads) {
+            const int t = start(s);
             if (t <= i0) atomicMax(&edge[0], t);
             else if (t > i1) atomicMin(&edge[1], t);
             else atomicOr(&begins[(t - i0) >> 6], 1ull << ((t - i0) & 63));
-            if (s == a.n_seq) edge[2] = t;
         }
+        if (tid == 0) edge[2] = start(a.n_seq);
         __syncthreads();
         unsigned long long word[kWords];
 #pragma unroll

@@ -77,6 +77,24 @@ def test_packed(d, Hq, Hkv, causal, cuts):
     assert bool((out[:, :, ~inside] == 7.0).all()) and bool((lse[:, :, ~inside] == 7.0).all())
 
 
+@pytest.mark.parametrize("d,Hq,Hkv", [(64, 2, 2), (128, 4, 1)])
+@pytest.mark.parametrize("kind", range(5))
+def test_many_sequences(d, Hq, Hkv, kind):
+    """More starts than threads look at: short sequences, empty ones among them, many at one token or at both ends."""
+    T = 1500
+    rng = np.random.RandomState(kind)
+    cuts = [list(range(0, T + 1)) + [T] * 700, [0] * 2000 + list(range(0, T, 2)) + [T],
+            [5] + sorted(rng.randint(5, 1400, 2500).tolist()) + [1400],
+            sorted(rng.randint(0, T, 1100).tolist()) + [T] * 3000,
+            [0, 700] + [700] * 4000 + [701, 1490]][kind]
+    q, k, v = inputs(1, Hq, Hkv, T, d, kind, "tokens")
+    for causal in (True, False):
+        out = torch.full_like(q, 7.0)
+        mm.prompt_attention(q, k, v, starts=int32(cuts), causal=causal, out=out)
+        check(out, q, k, v, cuts, causal)
+        assert bool((out[:, :, :cuts[0]] == 7.0).all()) and bool((out[:, :, cuts[-1]:] == 7.0).all())
+
+
 @pytest.mark.parametrize("layout", ["tokens", "gaps"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_strides(layout, d):

@@ -80,7 +80,12 @@ def check(got, cache, q, lens, shared, table, **kw):
     (12, 3, 32, 8, 128, 128, 300, 130, 5),
     (3, 1, 30, 1, 128, 64, 150, 90, 4),            # many rows in both parts
     (4, 2, 130, 2, 64, 64, 70, 80, 1),
-    (32, 1, 4, 4, 128, 256, 700, 300, 1)])
+    (32, 1, 4, 4, 128, 256, 700, 300, 1),
+    (12, 1, 8, 1, 64, 64, 500, 3000, 1),           # own rows that are split, after many shared ones
+    (3, 1, 14, 2, 128, 64, 200, 2500, 1),          # ... and few
+    (70, 1, 28, 4, 128, 64, 900, 100, 1),          # a launch for each part, the own one joins
+    (40, 2, 40, 1, 64, 32, 600, 70, 2),            # ... with many own rows
+    (300, 2, 2, 1, 64, 16, 100, 40, 1)])
 def test_shared_attention(dtype, causal, B, G, Hq, Hkv, d, page, prefix, own, n):
     cache, q, lens, shared, table = problem(B, G, Hq, Hkv, d, dtype, page, prefix, own, n, B + n, "tokens")
     got = mm.shared_attention(q, cache, lens, shared, table, causal=causal)

@@ -468,7 +468,8 @@ def paged_bench(args):
             src = torch.arange(0, B * N, N, dtype=torch.int32, device=dev).repeat_interleave(N)
             timed("fork", 4 * (2 * B * N * most + B * N * most), 0, lambda: bd.cache_fork(cache, src, ln))
             bd.cache_hold(cache, ln + new)         # pages for all tokens to come
-            shared.append(sel.counts)
+            # whole pages, which every answer holds: the first one may end
+            shared.append((sel.counts.amin(1, keepdim=True) // 64 * 64).expand(-1, Hkv).contiguous())
         kept.append(cache)
         lens.append(ln)
         x.clear()

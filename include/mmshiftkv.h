@@ -495,6 +495,13 @@ int mmshiftkv_chunk_attention(const mmskv_shape *shape, const mmskv_pages *pages
  * shared_table, row g of which is laid out as a row of the table; the table of
  * `pages` names the rows from shared[g,c] on (its entries before are not used:
  * they may name the same pages, as mmshiftkv_cache_fork leaves them, or none).
+ * The pages that shared_table names have to be held for as long as it is used.
+ * After a fork every sequence of the group holds those of whole pages: the rows
+ * below min over c of lens[src,c] / page * page, of each head.  Those of the rows
+ * behind, the prompt's last ones, are held by their own sequence alone, and are
+ * free as soon as that gives them back; the others have copies.  So `shared` counts
+ * whole pages, or the sequence that shared_table was taken from stays until the
+ * group has ended, or mmshiftkv_shared_table makes the table for each call.
  * lens counts all rows of a sequence, the shared ones among them; a sequence of
  * fewer sees as many of those.  Otherwise as mmshiftkv_chunk_attention, and to
  * rounding what it gives where both tables name the same rows; an infinity or
@@ -516,6 +523,17 @@ int mmshiftkv_shared_attention(const mmskv_shape *shape, const mmskv_pages *page
                                const int32_t *shared, const int32_t *shared_table, int32_t groups, int32_t shared_T,
                                int32_t n, int32_t causal, uint16_t *out, const mmskv_strides *out_strides,
                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* The shared_table of groups whose sequences all have their shared rows by their
+ * own tables, as mmshiftkv_cache_fork leaves them, and end in any order (lens 0, or
+ * a table row emptied by mmshiftkv_cache_hold): entry j of group g, below max over c
+ * of shared[g,c] rows, is that of the first sequence of the group that has all the
+ * shared rows (lens[b,c] >= shared[g,c] for every c) and names a page there; without
+ * one, of the first that has some row of the page and names it; else -1.  Reads
+ * shape->B, Hkv and d, lens, shared and the table of `pages`.
+ *   shared_table  [groups, max_pages] int32 out, not the table itself */
+int mmshiftkv_shared_table(const mmskv_shape *shape, const mmskv_pages *pages, const int32_t *lens,
+                           const int32_t *shared, int32_t groups, int32_t *shared_table, void *stream);
 
 /* ---- Attention of whole prompts over themselves, which gives the hidden states
  * that the next layer's keys come from: each batch row is one sequence of T

@@ -11,4 +11,5 @@ from .binding import (MMSKV_BF16, MMSKV_F32, MMSKV_MASS, MMSKV_VOTE, LayerOut, M
                       chunk_attention_workspace, decode_check, decode_workspace,
                       gather_kv, load_library, prompt_attention,
                       score, score_lse, score_mass, score_workspace, select_layer, select_topk,
-                      select_workspace, shared_attention, shared_attention_workspace, status_string)
+                      select_workspace, shared_attention, shared_attention_workspace, shared_table,
+                      status_string)

@@ -33,7 +33,7 @@ EXPORTED = ("mmshiftkv_build_proxies", "mmshiftkv_score_workspace", "mmshiftkv_s
             "mmshiftkv_chunk_attention_workspace", "mmshiftkv_chunk_attention",
             "mmshiftkv_cache_book_workspace", "mmshiftkv_cache_hold", "mmshiftkv_cache_fork",
             "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention", "mmshiftkv_shared_attention_workspace",
-            "mmshiftkv_shared_attention")
+            "mmshiftkv_shared_attention", "mmshiftkv_shared_table")
 
 
 class Shape(ctypes.Structure):
@@ -119,6 +119,7 @@ def load_library(path: str | None = None):
     lib.mmshiftkv_shared_attention_workspace.argtypes = [PS, I32, I32]
     lib.mmshiftkv_shared_attention_workspace.restype = SZ
     lib.mmshiftkv_shared_attention.argtypes = [PS, PG, V, PT, V, V, V, V, I32, I32, I32, I32, V, PT, V, SZ, V]
+    lib.mmshiftkv_shared_table.argtypes = [PS, PG, V, V, I32, V, V]
     lib.mmshiftkv_prompt_attention.argtypes = [PS, V, PT, V, PT, V, PT, V, I32, I32, V, PT, V, V]
     lib.mmshiftkv_cache_book_workspace.argtypes = [PS, I32, I32]
     lib.mmshiftkv_cache_book_workspace.restype = SZ
@@ -136,7 +137,8 @@ def load_library(path: str | None = None):
                  "mmshiftkv_decode_check", "mmshiftkv_window_rows", "mmshiftkv_shape_scores",
                  "mmshiftkv_score_noalloc", "mmshiftkv_cache_write", "mmshiftkv_cache_read",
                  "mmshiftkv_chunk_attention", "mmshiftkv_cache_hold", "mmshiftkv_cache_fork",
-                 "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention", "mmshiftkv_shared_attention"):
+                 "mmshiftkv_cache_compact", "mmshiftkv_prompt_attention", "mmshiftkv_shared_attention",
+                 "mmshiftkv_shared_table"):
         getattr(lib, name).restype = ctypes.c_int
     if path is None:
         _lib = lib
@@ -829,14 +831,35 @@ def shared_attention_workspace(B, Hq, Hkv, T, d, n, groups) -> int:
         ctypes.byref(_shape(B, Hq, Hkv, T, 0, d)), int(groups), int(n)))
 
 
+def shared_table(cache: PagedCache, lens: torch.Tensor, shared: torch.Tensor) -> torch.Tensor:
+    """mmshiftkv_shared_table: the pages [G, max_pages] int32 of the rows that G groups of sequences share
+    (shared [G, Hkv] int32), each by a sequence of its group that has them, whichever have ended."""
+    i = _same_device(cache.k, lens, shared)
+    pages = cache.c_pages()
+    _, Hkv, _, d = cache.k.shape
+    B, most = cache.table.shape
+    rows, G = _int32(lens, (B, Hkv), "lens"), shared.shape[0]
+    prefix = _int32(shared, (G, Hkv), "shared")
+    if G < 1 or B % G:
+        raise ValueError("the sequences are groups of the same size: %d of %d" % (G, B))
+    out = lens.new_empty((G, most))
+    ref = ctypes.byref
+    _enqueue("mmshiftkv_shared_table", i, ref(Shape(B, 0, Hkv, 0, 0, d)), ref(pages), rows, prefix, G, out.data_ptr())
+    return out
+
+
+_shared_table = shared_table                       # (where an argument has that name)
+
+
 def shared_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, shared: torch.Tensor,
                      shared_table: torch.Tensor | None = None, q_counts: torch.Tensor | None = None,
                      T: int | None = None, shared_T: int | None = None, causal: bool = True,
                      workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """mmshiftkv_shared_attention: chunk_attention for G groups of B / G sequences that share the first
     shared[g, c] rows (shared [G, Hkv] int32), which are read once for a group.  shared_table [G, max_pages]
-    int32 names their pages (None: the table's row of each group's first sequence, as cache_fork leaves
-    it); T and shared_T are upper bounds of lens and shared (None: what the table can hold, and T)."""
+    int32 names their pages, which have to be held for as long as it is used: after a fork all sequences hold
+    those of whole pages, the ones behind only their own (None: what shared_table finds, a short launch more,
+    for groups that cache_fork has made and whose sequences end in any order).  T and shared_T are upper bounds of lens and shared (None: what the table can hold, and T)."""
     i = _same_device(q, cache.k, lens, shared, shared_table, q_counts, workspace, out)
     if q.dtype != torch.bfloat16:
         raise TypeError("q is bf16")
@@ -852,7 +875,7 @@ def shared_attention(q: torch.Tensor, cache: PagedCache, lens: torch.Tensor, sha
     if G < 1 or B % G:
         raise ValueError("the sequences are groups of the same size: %d of %d" % (G, B))
     if shared_table is None:
-        shared_table = cache.table[::B // G].contiguous()
+        shared_table = cache.table if G == B else _shared_table(cache, lens, shared)
     named = _int32(shared_table, (G, cache.table.shape[1]), "shared_table")
     if q_counts is not None:
         q_counts = _int32(q_counts, (B,), "q_counts")

@@ -1131,6 +1131,25 @@ size_t shared_ws(const mmskv_shape* s, int32_t groups, int32_t n) {
 
 }  // namespace
 
+int mmshiftkv_shared_table(const mmskv_shape* shape, const mmskv_pages* pages, const int32_t* lens,
+                           const int32_t* shared, int32_t groups, int32_t* shared_table, void* stream) {
+    if (shape == nullptr) return MMSKV_EINVAL;
+    if (shape->B < 1 || shape->B > 65535 || shape->Hkv < 1 || shape->Hkv > 65535 || shape->d < 1) return MMSKV_EINVAL;
+    if (groups < 1 || shape->B % groups != 0) return MMSKV_EINVAL;
+    SharedTableArgs a = {};
+    const int rc = check_pages(pages, shape->d, &a.pages);
+    if (rc) return rc;
+    if (lens == nullptr || shared == nullptr || shared_table == nullptr) return MMSKV_EINVAL;
+    if (!aligned(lens, 4) || !aligned(shared, 4) || !aligned(shared_table, 4)) return MMSKV_EINVAL;
+    a.lens = lens;
+    a.shared = shared;
+    a.out = shared_table;
+    a.groups = groups;
+    a.each = shape->B / groups;
+    a.Hkv = shape->Hkv;
+    return status_of(launch_shared_table(a, static_cast<hipStream_t>(stream)));
+}
+
 size_t mmshiftkv_shared_attention_workspace(const mmskv_shape* shape, int32_t groups, int32_t n) {
     return check_groups(shape, groups, n) == MMSKV_OK ? shared_ws(shape, groups, n) : 0;
 }

@@ -254,6 +254,14 @@ struct BookArgs {
     int32_t* want; int32_t* free; uint64_t* free_bits; int32_t* taken; int32_t* ids; int2* items;
     int32_t* old_table; int32_t* old_lens;
 };
+// The table of the rows that groups of sequences share.
+struct SharedTableArgs {
+    Pages pages;
+    const int32_t* lens;       // [groups * each, Hkv]
+    const int32_t* shared;     // [groups, Hkv]
+    int32_t* out;              // [groups, max_pages]
+    int groups, each, Hkv;
+};
 constexpr int kBookChunk = 2048;           // pages of a chunk
 inline int64_t book_chunks(int n_pages) { return (static_cast<int64_t>(n_pages) + kBookChunk - 1) / kBookChunk; }
 
@@ -301,5 +309,6 @@ void plan_parts(ChunkArgs* shared, ChunkArgs* own);
 hipError_t launch_shared_attention(const ChunkArgs& shared, const ChunkArgs& own, hipStream_t s);
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s);
 hipError_t launch_book(const BookArgs& a, int op, hipStream_t s);
+hipError_t launch_shared_table(const SharedTableArgs& a, hipStream_t s);
 
 }  // namespace mmskv

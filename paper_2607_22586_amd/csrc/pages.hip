@@ -1,5 +1,5 @@
 // Pages of a paged cache given, taken and copied on gfx950
-// (mmshiftkv_cache_hold, _fork and _compact).  The numbers of rows are the
+// (mmshiftkv_cache_hold, _fork, _compact and mmshiftkv_shared_table).  The numbers of rows are the
 // device's (a selection leaves them there), so the pages are assigned there too,
 // without a wait of the host:
 //   count  what each sequence wants, the free pages of the pool as bits and by chunk, a
@@ -385,6 +385,45 @@ __global__ void __launch_bounds__(kBookThreads) book_copy_kernel(BookArgs a) {
     }
 }
 
+// The table of a group's shared rows (mmshiftkv_shared_table).  A thread has an entry and
+// looks through the group's sequences in order, kBookThreads of them at a time, with a
+// thread to see which of the shared rows each has.  As a rule the first ends the search:
+// a chain of three loads.
+__global__ void __launch_bounds__(kBookThreads) shared_table_kernel(SharedTableArgs a) {
+    __shared__ int longest[kBookThreads], whole[kBookThreads], lds[2 * kBookThreads / kWave];
+    const int tid = threadIdx.x, g = blockIdx.x, entries = a.pages.max_pages;
+    const int32_t* const shared = a.shared + static_cast<int64_t>(g) * a.Hkv;
+    const int most = min(extent(shared, a.Hkv, lds).most, a.pages.cap);
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * kBookThreads; j0 < entries; j0 += gridDim.y * kBookThreads) {
+        const int64_t j = j0 + tid, row = j << a.pages.shift;          // the entry, its first row
+        const bool wanted = j < entries && row < most;
+        int id = -1, part = -1;            // of a sequence with all shared rows, of one with some of this page
+        for (int s0 = 0; s0 < a.each; s0 += kBookThreads) {
+            int rows = 0, has = 0;
+            if (s0 + tid < a.each) {
+                const int32_t* const lens = a.lens + (static_cast<int64_t>(g) * a.each + s0 + tid) * a.Hkv;
+                has = 1;
+                for (int c = 0; c < a.Hkv; ++c) {
+                    const int n = min(max(lens[c], 0), a.pages.cap);
+                    rows = max(rows, n);
+                    has &= n >= min(shared[c], a.pages.cap);
+                }
+            }
+            __syncthreads();               // (those of the last round have been read)
+            longest[tid] = rows;
+            whole[tid] = has;
+            if (!__syncthreads_or(wanted && id < 0)) break;
+            if (!wanted) continue;
+            for (int x = 0; x < min(a.each - s0, kBookThreads) && id < 0; ++x) {
+                if (!whole[x] && (part >= 0 || longest[x] <= row)) continue;
+                const int p = a.pages.table[(static_cast<int64_t>(g) * a.each + s0 + x) * entries + j];
+                if (named(a.pages, p)) (whole[x] ? id : part) = p;
+            }
+        }
+        if (j < entries) a.out[static_cast<int64_t>(g) * entries + j] = id >= 0 ? id : part;
+    }
+}
+
 template <int OP>
 hipError_t launch(const BookArgs& a, hipStream_t s) {
     const int64_t entries = static_cast<int64_t>(a.B) * a.pages.max_pages;
@@ -413,6 +452,13 @@ hipError_t launch(const BookArgs& a, hipStream_t s) {
 
 hipError_t launch_book(const BookArgs& a, int op, hipStream_t s) {
     return op == kBookHold ? launch<kBookHold>(a, s) : op == kBookFork ? launch<kBookFork>(a, s) : launch<kBookCompact>(a, s);
+}
+
+hipError_t launch_shared_table(const SharedTableArgs& a, hipStream_t s) {
+    const int blocks = (a.pages.max_pages + kBookThreads - 1) / kBookThreads;
+    const dim3 grid(a.groups, blocks < 65535 ? blocks : 65535);
+    hipLaunchKernelGGL(shared_table_kernel, grid, dim3(kBookThreads), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace mmskv

@@ -547,10 +547,13 @@ int mmshiftkv_shared_table(const mmskv_shape *shape, const mmskv_pages *pages, c
  * bf16 products, fp32 accumulation and softmax, p rounded to bf16 for its
  * product with v, the result rounded once.  A key that a query does not see
  * does not reach it, whatever it holds, infinities and NaN included (another
- * sequence's, a later token's, padding); of one that it sees the result is not
- * finite in that dim (of k: as a whole).  Sums are divided last, as in
- * mmshiftkv_chunk_attention.  Rows of out and lse in no sequence (before
- * starts[0], or from starts[n_seq] on) are left as they were.
+ * sequence's, a later token's, padding).  Of a key that it sees, an infinity or
+ * NaN in v makes the result not finite in that dim, whatever the weight; a logit
+ * that is NaN (as 0 times an infinity is) or +inf makes the result and lse NaN
+ * as a whole, and one of -inf, of an infinity in k against q's sign, gives the
+ * key the weight 0.  Sums are divided last, as in mmshiftkv_chunk_attention.
+ * Rows of out and lse in no sequence (before starts[0], or from starts[n_seq]
+ * on) are left as they were.
  * Reads shape->B, Hq, Hkv, T and d (64 or 128); Gh * T, B * Hkv and B * Hkv *
  * ceil(Gh * T / 64) up to 2^22, token strides of k and v below 2^28 (more
  * -> MMSKV_EUNSUPPORTED).

@@ -503,9 +503,9 @@ int mmshiftkv_chunk_attention(const mmskv_shape *shape, const mmskv_pages *pages
  * whole pages, or the sequence that shared_table was taken from stays until the
  * group has ended, or mmshiftkv_shared_table makes the table for each call.
  * lens counts all rows of a sequence, the shared ones among them; a sequence of
- * fewer sees as many of those.  Otherwise as mmshiftkv_chunk_attention, and to
- * rounding what it gives where both tables name the same rows; an infinity or
- * NaN in a shared row's v may reach the queries of its group that do not see it.
+ * fewer sees as many of those (read for it alone).  Otherwise as
+ * mmshiftkv_chunk_attention, and to rounding what it gives where both tables name
+ * the same rows.
  * B is a multiple of groups (groups = 1: one prompt for all); B / groups * Gh * n,
  * B * Hkv and Hkv * (groups * ceil(B / groups * Gh * n / 128) + B * ceil(Gh * n /
  * 128)) up to 2^22, B * Hq * n up to 2^26 (more -> MMSKV_EUNSUPPORTED).  T and shared_T are upper

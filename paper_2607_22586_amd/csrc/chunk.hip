@@ -86,7 +86,10 @@ __device__ __forceinline__ int staged(int r, int ch) {
 // two parts of an attention over a shared prefix, of which it leaves partial sums: the
 // rows that the sequences of a group share, for the queries of all of them (b is the
 // group, pages.table the groups' and row r = (s * n + i) * Gh + g query i of the group's
-// sequence s), or those behind the shared ones.
+// sequence s), or those behind the shared ones.  A sequence of fewer rows than are shared
+// is left out of the first part, and has all of its rows in the second, by the group's
+// table: an infinity or NaN in a row of V that it does not see then does not reach it as 0
+// times it, as it would among queries that see the row.
 // (kShared: a launch of the first part alone, kBoth: of either or both)
 constexpr int kNoParts = 0, kShared = 1, kBoth = 2;
 struct Work {
@@ -130,10 +133,24 @@ __device__ __forceinline__ int queries_of(const ChunkArgs& a, int b) {
 __device__ __forceinline__ int shared_rows(const ChunkArgs& a, int g, int c) {
     return min(max(a.shared[static_cast<int64_t>(g) * a.Hkv + c], 0), a.shared_max);
 }
-// The last key that a query that is there sees (below 0: none), of the shared rows.
+__device__ __forceinline__ int length_of(const ChunkArgs& a, int b, int c) {
+    return min(max(a.lens[static_cast<int64_t>(b) * a.Hkv + c], 0), a.max_len);
+}
+// The last of the shared rows that a query that is there sees (below 0: none).
 __device__ __forceinline__ int last_shared(const ChunkArgs& a, const Query& q, int c, int nq, int shared) {
-    const int len = min(max(a.lens[static_cast<int64_t>(q.b) * a.Hkv + c], 0), a.max_len);
+    const int len = length_of(a, q.b, c);
     return min(a.causal ? len - nq + q.i : len - 1, shared - 1);
+}
+// The first row of a sequence's own part and where its rows from there on are found: row
+// `seq` of the table.
+struct Own {
+    int low, seq;
+    const int32_t* table;
+};
+__device__ __forceinline__ Own own_rows(const ChunkArgs& shared, const ChunkArgs& own, int b, int c) {
+    const int g = b / own.each, low = shared_rows(own, g, c);
+    if (length_of(own, b, c) < low) return {0, g, shared.pages.table};
+    return {low, b, own.pages.table};
 }
 
 template <int D, int TYPE, int PARTS = kNoParts, class ARGS = ChunkArgs>
@@ -166,14 +183,15 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
     const Query qr = query_of(a, shared, b, r);
     const int i = qr.i, h = c * a.Gh + qr.g;
     const int nq = queries_of(a, qr.b);
-    const bool there = r < a.rows && i < nq;
-    int last, all_see, end, low = 0;
+    const int prefix = shared ? shared_rows(a, b, c) : 0;
+    const bool there = r < a.rows && i < nq && (!shared || length_of(a, qr.b, c) >= prefix);
+    int last, all_see, end, low = 0, seq = b;
+    Pages pages = a.pages;
     __shared__ int most[PARTS != kNoParts ? 2 : 1][kWaves];
     if (shared) {
         // keys that all rows of the workgroup see, and that some row sees
-        const int rows = shared_rows(a, b, c);
-        last = there ? last_shared(a, qr, c, nq, rows) : -1;
-        int lo = there ? last + 1 : rows, hi = last + 1;
+        last = there ? last_shared(a, qr, c, nq, prefix) : -1;
+        int lo = there ? last + 1 : prefix, hi = last + 1;
 #pragma unroll
         for (int x = 1; x < 32; x *= 2) lo = min(lo, __shfl_xor(lo, x)), hi = max(hi, __shfl_xor(hi, x));
         if (lane == 0) most[0][wave] = lo, most[1][wave] = hi;
@@ -188,7 +206,10 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
         // keys that the workgroup's rows see together
         const int i_end = min((min(r0 + kRows, a.rows) - 1) / a.Gh, nq - 1);
         end = i_end < r0 / a.Gh ? 0 : max(a.causal ? len - nq + i_end + 1 : len, 0);
-        if (PARTS == kBoth) low = shared_rows(a, b / a.each, c);       // the first key
+        if constexpr (PARTS == kBoth) {
+            const Own own = own_rows(all.shared, a, b, c);
+            low = own.low, seq = own.seq, pages.table = own.table;
+        }
     }
     // this split's tiles
     const int tiles0 = low / kKeys, tiles = max((end + kKeys - 1) / kKeys, tiles0);
@@ -202,14 +223,14 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
     float ksr[kLoads], vsr[kLoads];
     auto load = [&](int tile) {
         const int t = tile * kKeys + kWaveRows * wave;
-        const int id = uniform_page(a.pages, b, t);
-        const int64_t pr = pool_row(a.pages, a.Hkv, c, id, t);
+        const int id = uniform_page(pages, seq, t);
+        const int64_t pr = pool_row(pages, a.Hkv, c, id, t);
         typedef const char __attribute__((address_space(1))) * gchar;
         typedef const u32x4 __attribute__((address_space(1))) * gvec;
         typedef const float __attribute__((address_space(1))) * gfloat;
         const gchar none = (gchar)(kNoRows);
-        const gchar ks = id >= 0 ? (gchar)(a.pages.k) + pr * kRow : none;
-        const gchar vs = id >= 0 ? (gchar)(a.pages.v) + pr * kRow : none;
+        const gchar ks = id >= 0 ? (gchar)(pages.k) + pr * kRow : none;
+        const gchar vs = id >= 0 ? (gchar)(pages.v) + pr * kRow : none;
         const int step = id >= 0 ? 1024 : 0;         // (1 KB stands for a page that is not there)
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
@@ -217,8 +238,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
             vr[j] = *(gvec)(vs + j * step + 16 * lane);
         }
         if constexpr (TYPE != kCacheBf16) {
-            const gfloat kss = id >= 0 ? (gfloat)(a.pages.k_scale) + pr : (gfloat)(none);
-            const gfloat vss = id >= 0 ? (gfloat)(a.pages.v_scale) + pr : (gfloat)(none);
+            const gfloat kss = id >= 0 ? (gfloat)(pages.k_scale) + pr : (gfloat)(none);
+            const gfloat vss = id >= 0 ? (gfloat)(pages.v_scale) + pr : (gfloat)(none);
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 ksr[j] = kss[j * (64 / kCh) + lane / kCh];
@@ -499,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
     while (tile < tile1) step(Constant<1>{});
     l = half_sum(l);
     if (r >= a.rows) return;
-    if (!there) l = 0.f;                   // (took part where nothing is masked)
+    if (!there) m = kNone, l = 0.f;        // (took part where nothing is masked)
     // value 4 w + j of o[t] is dim 32 t + 8 w + 4 half + j
     if (PARTS != kNoParts || a.splits > 1) {
         const int64_t pr = (static_cast<int64_t>(split) * (a.B * a.Hkv) + bc) * a.rows + r;
@@ -679,7 +700,14 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
     const int nq = shared ? 0 : queries_of(a, b);
     const int len = shared ? shared_rows(a, b, c) : min(max(a.lens[bc], 0), a.max_len);
     const int end = shared || nq > 0 ? len : 0;        // keys that the rows see together
-    const int low = PARTS && !shared ? shared_rows(a, b / a.each, c) : 0;  // the first of them
+    int low = 0, seq = b;                  // the first of them
+    Pages pages = a.pages;
+    if constexpr (PARTS != kNoParts) {
+        if (!shared) {
+            const Own own = own_rows(all.shared, a, b, c);
+            low = own.low, seq = own.seq, pages.table = own.table;
+        }
+    }
     const int tiles0 = low / T::kKeys, tiles = max((end + T::kKeys - 1) / T::kKeys, tiles0);
     const int per = (tiles - tiles0 + a.splits - 1) / a.splits;
     const int first0 = tiles0 + split * per, tile0 = first0 + wave, tile1 = min(first0 + per, tiles);
@@ -691,7 +719,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
     auto pages_of = [&](int tile) {
         Ids ids;
 #pragma unroll
-        for (int g = 0; g < T::kGroups; ++g) ids.id[g] = uniform_page(a.pages, b, tile * T::kKeys + 16 * g);
+        for (int g = 0; g < T::kGroups; ++g) ids.id[g] = uniform_page(pages, seq, tile * T::kKeys + 16 * g);
         return ids;
     };
     // A load instruction fetches 1 KB, kPer rows of a group; a lane's bytes of it are
@@ -705,9 +733,9 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
 #pragma unroll
         for (int g = 0; g < T::kGroups; ++g) {
             const bool any = ids.id[g] >= 0;
-            const int64_t e = pool_row(a.pages, a.Hkv, c, ids.id[g], t0 + 16 * g) * T::kRow;
-            const char* ks = any ? static_cast<const char*>(a.pages.k) + e : none;
-            const char* vs = any ? static_cast<const char*>(a.pages.v) + e : none;
+            const int64_t e = pool_row(pages, a.Hkv, c, ids.id[g], t0 + 16 * g) * T::kRow;
+            const char* ks = any ? static_cast<const char*>(pages.k) + e : none;
+            const char* vs = any ? static_cast<const char*>(pages.v) + e : none;
             load_group<T, 0, kGroupLoads>(ks, dst + g * 16 * T::kRow, 16 * g, ld_row, lane, any);
             load_group<T, 0, kGroupLoads>(vs, dst + T::kTile + g * 16 * T::kRow, 16 * g, ld_row, lane, any);
         }
@@ -717,11 +745,11 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
             int id = ids.id[0];
 #pragma unroll
             for (int g = 1; g < T::kGroups; ++g) id = t / 16 == g ? ids.id[g] : id;
-            const int64_t pr = pool_row(a.pages, a.Hkv, c, id, t0 + t);
-            const float* one = T::kKeys == 32 && lane >= 32 ? a.pages.v_scale : a.pages.k_scale;
+            const int64_t pr = pool_row(pages, a.Hkv, c, id, t0 + t);
+            const float* one = T::kKeys == 32 && lane >= 32 ? pages.v_scale : pages.k_scale;
             load4_to_lds(id >= 0 ? reinterpret_cast<const char*>(one + pr) : none, dst + 2 * T::kTile);
             if constexpr (T::kKeys == 64)
-                load4_to_lds(id >= 0 ? reinterpret_cast<const char*>(a.pages.v_scale + pr) : none,
+                load4_to_lds(id >= 0 ? reinterpret_cast<const char*>(pages.v_scale + pr) : none,
                              dst + 2 * T::kTile + 256);
         }
     };
@@ -760,7 +788,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
         if (shared) {
             const Query qr = query_of(a, shared, b, r);
             const int n = queries_of(a, qr.b);
-            const bool there = r < a.rows && qr.i < n;
+            const bool there = r < a.rows && qr.i < n && length_of(a, qr.b, c) >= len;
             last[x] = there ? last_shared(a, qr, c, n, len) : -1;
             int lo = there ? last[x] + 1 : len;
 #pragma unroll
@@ -1027,7 +1055,8 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = fmaf(y0[e], f, x[e]), x[4 + e] = fmaf(y1[e], f, x[4 + e]);
         }
-        if (i >= (shared ? queries_of(a, qr.b) : nq)) L = 0.f;    // (a row that is not there took part where nothing is masked)
+        // (a row that is not there took part where nothing is masked)
+        if (shared ? i >= queries_of(a, qr.b) || length_of(a, qr.b, c) < len : i >= nq) M = kNone, L = 0.f;
         if constexpr (PARTS != kNoParts) {
             if (a.joins) {                 // the only split of own rows: the shared ones' sums to its own
                 const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;

@@ -387,10 +387,13 @@ __global__ void __launch_bounds__(kBookThreads) book_copy_kernel(BookArgs a) {
 
 // The table of a group's shared rows (mmshiftkv_shared_table).  A thread has an entry and
 // looks through the group's sequences in order, kBookThreads of them at a time, with a
-// thread to see which of the shared rows each has.  As a rule the first ends the search:
-// a chain of three loads.
+// thread to see what each has of the shared rows; sequences that have ended are passed over
+// by their bits.  As a rule the first one left ends the search, a chain of three loads:
+// 3.3 us for 8 entries of 8 sequences, 4.2 for 520 of 32, 4.7 where 500 of 512 have ended.
 __global__ void __launch_bounds__(kBookThreads) shared_table_kernel(SharedTableArgs a) {
-    __shared__ int longest[kBookThreads], whole[kBookThreads], lds[2 * kBookThreads / kWave];
+    constexpr int kWords = kBookThreads / kWave;
+    __shared__ int rows[kBookThreads], lds[2 * kWords];
+    __shared__ uint64_t whole[kWords], some[kWords];   // sequences with all shared rows, and with any row
     const int tid = threadIdx.x, g = blockIdx.x, entries = a.pages.max_pages;
     const int32_t* const shared = a.shared + static_cast<int64_t>(g) * a.Hkv;
     const int most = min(extent(shared, a.Hkv, lds).most, a.pages.cap);
@@ -399,26 +402,35 @@ __global__ void __launch_bounds__(kBookThreads) shared_table_kernel(SharedTableA
         const bool wanted = j < entries && row < most;
         int id = -1, part = -1;            // of a sequence with all shared rows, of one with some of this page
         for (int s0 = 0; s0 < a.each; s0 += kBookThreads) {
-            int rows = 0, has = 0;
-            if (s0 + tid < a.each) {
+            int longest = 0;
+            bool has = s0 + tid < a.each;
+            if (has) {
                 const int32_t* const lens = a.lens + (static_cast<int64_t>(g) * a.each + s0 + tid) * a.Hkv;
-                has = 1;
                 for (int c = 0; c < a.Hkv; ++c) {
                     const int n = min(max(lens[c], 0), a.pages.cap);
-                    rows = max(rows, n);
-                    has &= n >= min(shared[c], a.pages.cap);
+                    longest = max(longest, n);
+                    has = has && n >= min(shared[c], a.pages.cap);
                 }
             }
+            const uint64_t has_all = __ballot(has), has_some = __ballot(longest > 0);
             __syncthreads();               // (those of the last round have been read)
-            longest[tid] = rows;
-            whole[tid] = has;
+            rows[tid] = longest;
+            if (lane_id() == 0) whole[tid / kWave] = has_all, some[tid / kWave] = has_some;
             if (!__syncthreads_or(wanted && id < 0)) break;
             if (!wanted) continue;
-            for (int x = 0; x < min(a.each - s0, kBookThreads) && id < 0; ++x) {
-                if (!whole[x] && (part >= 0 || longest[x] <= row)) continue;
-                const int p = a.pages.table[(static_cast<int64_t>(g) * a.each + s0 + x) * entries + j];
-                if (named(a.pages, p)) (whole[x] ? id : part) = p;
-            }
+            // the first page that one of these sequences names, of those with a row behind `from`
+            const auto first = [&](const uint64_t* of, int from) {
+                for (int w = 0; w < kWords; ++w)
+                    for (uint64_t bits = of[w]; bits != 0; bits &= bits - 1) {
+                        const int x = w * kWave + __ffsll(static_cast<unsigned long long>(bits)) - 1;
+                        if (rows[x] <= from) continue;
+                        const int p = a.pages.table[(static_cast<int64_t>(g) * a.each + s0 + x) * entries + j];
+                        if (named(a.pages, p)) return p;
+                    }
+                return -1;
+            };
+            if (id < 0) id = first(whole, -1);
+            if (id < 0 && part < 0) part = first(some, static_cast<int>(row));
         }
         if (j < entries) a.out[static_cast<int64_t>(g) * entries + j] = id >= 0 ? id : part;
     }

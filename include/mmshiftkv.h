@@ -529,7 +529,9 @@ int mmshiftkv_shared_attention(const mmskv_shape *shape, const mmskv_pages *page
  * a table row emptied by mmshiftkv_cache_hold): entry j of group g, below max over c
  * of shared[g,c] rows, is that of the first sequence of the group that has all the
  * shared rows (lens[b,c] >= shared[g,c] for every c) and names a page there; without
- * one, of the first that has some row of the page and names it; else -1.  Reads
+ * one, of the first that has some row of the page and names it; else -1.  (What
+ * mmshiftkv_cache_compact has changed, or another prompt has taken, no longer has
+ * the shared rows and is not of the group: there its lens have to be 0.)  Reads
  * shape->B, Hkv and d, lens, shared and the table of `pages`.
  *   shared_table  [groups, max_pages] int32 out, not the table itself */
 int mmshiftkv_shared_table(const mmskv_shape *shape, const mmskv_pages *pages, const int32_t *lens,

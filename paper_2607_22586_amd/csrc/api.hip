@@ -1174,6 +1174,7 @@ int mmshiftkv_shared_attention(const mmskv_shape* shape, const mmskv_pages* page
     if (rc) return rc;
     pack_chunk(shape, q, q_strides, q_counts, lens, n, causal, out, out_strides, &a);
     a.shared = shared;
+    a.group_table = shared_table;
     a.each = shape->B / groups;
     a.shared_max = shared_T < a.max_len ? shared_T : a.max_len;
     ChunkArgs pre = a;

@@ -142,15 +142,16 @@ __device__ __forceinline__ int last_shared(const ChunkArgs& a, const Query& q, i
     return min(a.causal ? len - nq + q.i : len - 1, shared - 1);
 }
 // The first row of a sequence's own part and where its rows from there on are found: row
-// `seq` of the table.
+// `seq` of the table.  (len: its number of rows; selects, so that no load waits for another's
+// outcome)
 struct Own {
     int low, seq;
     const int32_t* table;
 };
-__device__ __forceinline__ Own own_rows(const ChunkArgs& shared, const ChunkArgs& own, int b, int c) {
-    const int g = b / own.each, low = shared_rows(own, g, c);
-    if (length_of(own, b, c) < low) return {0, g, shared.pages.table};
-    return {low, b, own.pages.table};
+__device__ __forceinline__ Own own_rows(const ChunkArgs& a, int b, int c, int len) {
+    const int g = b / a.each, low = shared_rows(a, g, c);
+    const bool fewer = len < low;
+    return {fewer ? 0 : low, fewer ? g : b, fewer ? a.group_table : a.pages.table};
 }
 
 template <int D, int TYPE, int PARTS = kNoParts, class ARGS = ChunkArgs>
@@ -184,7 +185,8 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
     const int i = qr.i, h = c * a.Gh + qr.g;
     const int nq = queries_of(a, qr.b);
     const int prefix = shared ? shared_rows(a, b, c) : 0;
-    const bool there = r < a.rows && i < nq && (!shared || length_of(a, qr.b, c) >= prefix);
+    const bool a_query = r < a.rows && i < nq;         // (loads of q do not wait for the lengths)
+    const bool there = a_query && (!shared || length_of(a, qr.b, c) >= prefix);
     int last, all_see, end, low = 0, seq = b;
     Pages pages = a.pages;
     __shared__ int most[PARTS != kNoParts ? 2 : 1][kWaves];
@@ -207,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
         const int i_end = min((min(r0 + kRows, a.rows) - 1) / a.Gh, nq - 1);
         end = i_end < r0 / a.Gh ? 0 : max(a.causal ? len - nq + i_end + 1 : len, 0);
         if constexpr (PARTS == kBoth) {
-            const Own own = own_rows(all.shared, a, b, c);
+            const Own own = own_rows(a, b, c, len);
             low = own.low, seq = own.seq, pages.table = own.table;
         }
     }
@@ -317,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 2) chunk_kernel(ARGS all) {
     {
         const uint16_t* q = a.q + qr.b * a.qsb + h * a.qsh + i * a.qst + 8 * half;
 #pragma unroll
-        for (int kc = 0; kc < KC; ++kc) qf[kc] = there ? load_bf16x8(q + 16 * kc) : zero_bf16x8();
+        for (int kc = 0; kc < KC; ++kc) qf[kc] = a_query ? load_bf16x8(q + 16 * kc) : zero_bf16x8();
     }
     floatx16 o[NT];
 #pragma unroll
@@ -704,7 +706,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
     Pages pages = a.pages;
     if constexpr (PARTS != kNoParts) {
         if (!shared) {
-            const Own own = own_rows(all.shared, a, b, c);
+            const Own own = own_rows(a, b, c, len);
             low = own.low, seq = own.seq, pages.table = own.table;
         }
     }
@@ -1031,7 +1033,9 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
         const float sum = quarter_sum(l[x]);
-        if (quarter == 0) ml[wave][16 * x + lane] = make_float2(m[x], sum);
+        // (shared: a row that is not there, which took part where nothing is masked, sees no key)
+        if (quarter == 0)
+            ml[wave][16 * x + lane] = shared && last[x] < 0 ? make_float2(kNone, 0.f) : make_float2(m[x], sum);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
             *reinterpret_cast<floatx4*>(ob + (16 * x + (lane & 15)) * kLd + 16 * t + 4 * quarter) = o[x][t];
@@ -1055,8 +1059,7 @@ __global__ void __launch_bounds__(64 * WAVES, 1) chunk_few_kernel(ARGS all) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = fmaf(y0[e], f, x[e]), x[4 + e] = fmaf(y1[e], f, x[4 + e]);
         }
-        // (a row that is not there took part where nothing is masked)
-        if (shared ? i >= queries_of(a, qr.b) || length_of(a, qr.b, c) < len : i >= nq) M = kNone, L = 0.f;
+        if (!shared && i >= nq) L = 0.f;   // (a row that is not there took part where nothing is masked)
         if constexpr (PARTS != kNoParts) {
             if (a.joins) {                 // the only split of own rows: the shared ones' sums to its own
                 const int64_t rows = static_cast<int64_t>(a.B) * a.Hkv * a.rows;

@@ -210,6 +210,7 @@ struct ChunkArgs {
     // attention over a shared prefix: B is the number of groups in the launch over the
     // shared rows, whose rows are each * Gh * n
     const int32_t* shared;     // [groups, Hkv] leading rows that a group's sequences share
+    const int32_t* group_table;            // own rows: the groups' table, for sequences of fewer rows
     int each;                  // sequences of a group
     int shared_max;            // upper bound of shared
     int shared_splits;         // in the join: splits of the shared rows among a.splits

@@ -17,8 +17,8 @@
 // What bounds it: at d = 128 no pipe alone.  Counters show the matrix pipe busy for 53 to
 // 56% of the cycles, the vector one for 57%, 30% of a wave's cycles spent waiting, with two
 // waves a SIMD, and a clock of 1.77 to 1.9 GHz (4 x 28 heads of 16384 tokens on 4, causal:
-// 6.9 to 7.2 ms, 1070 to 1119 TFLOP/s, box to box; a bf16 product of 8192^3 reaches 1219 to
-// 1389).  That fits latencies (of LDS, and from product to exponential to product) that two
+// 6.9 to 7.4 ms, 1040 to 1119 TFLOP/s, card to card; a bf16 product of 8192^3 reaches 1219
+// to 1389).  That fits latencies (of LDS, and from product to exponential to product) that two
 // waves do not cover, and a clock set by power: fewer vector instructions alone change
 // nothing, fewer reads of the tiles do.  At d = 64 the vector pipe: as many exponentials
 // for half the products (4 x 16 heads of 8192 tokens 890 to 910 TFLOP/s).  Short
